@@ -30,6 +30,11 @@ EXPORTS = [
     "pq_set_option", "pq_get_option", "ivf_adc_scan_topk_tightening", "pq_lds_read_probe",
     "ivf_coarse_form", "pq_search_form", "pq_scan_form",
 ]
+# include/qadc_vec.h: the operators on the vectors themselves
+VEC_EXPORTS = [
+    "vec_lookup", "vec_lookup_grad_workspace_bytes", "vec_lookup_grad", "vec_norm", "vec_norm_grad_workspace_bytes",
+    "vec_norm_grad", "vec_quantize_blocks", "vec_matmul_blocks_workspace_bytes", "vec_matmul_blocks",
+]
 PQ_KEY_BOUND_UNKNOWN = 0xFFFFFFFF
 (PQ_OPT_SCAN_BLOCKS, PQ_OPT_PILOT_CODES, PQ_OPT_PILOT_CODES_SINGLE, PQ_OPT_PILOT_BLOCKS, PQ_OPT_IVF_THREADS,
  PQ_OPT_SHARED_PASSES, PQ_OPT_COARSE_FILTER, PQ_OPT_IVF_SHARED_LISTS) = range(8)
@@ -112,6 +117,18 @@ def load() -> ctypes.CDLL:
     lib.pq_scan_form.restype = i32
     lib.ivf_coarse_form.argtypes = [i32, i32, i32, i32, sz]
     lib.ivf_coarse_form.restype = i32
+    f32 = ctypes.c_float
+    lib.vec_lookup.argtypes = [vp, i64, i32, i64, i32, vp, i32, i64, f32, vp, i64, i32, vp]
+    lib.vec_lookup_grad_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.vec_lookup_grad.argtypes = [vp, i64, i32, i64, i32, vp, i32, f32, i32, vp, i64, i64, i32, vp, sz, vp]
+    lib.vec_norm.argtypes = [vp, i64, vp, i64, i32, vp, i32, i64, i32, f32, vp, i64, vp, i64, vp, i64, i32, vp, i64, i32, vp]
+    lib.vec_norm_grad_workspace_bytes.argtypes = [i64, i32]
+    lib.vec_norm_grad.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i32, i64, i32, f32, vp, i64, vp, vp, sz, vp]
+    lib.vec_quantize_blocks.argtypes = [vp, i64, i32, i64, i64, i32, vp, i64, i32, vp, i64, i32, vp]
+    lib.vec_matmul_blocks_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.vec_matmul_blocks.argtypes = [vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, i32, i64, i64, i64, vp, i64, i32, vp, sz, vp]
+    for name in VEC_EXPORTS:
+        getattr(lib, name).restype = sz if name.endswith("_bytes") else i32
     _lib = lib
     return lib
 
@@ -448,3 +465,232 @@ def pq_encode(idx: PqIndex, vectors: torch.Tensor, shift_rows: Optional[torch.Te
     _check(load().pq_encode(idx.handle, _ptr(vectors), n, _ptr(shift_rows), _ptr(shift_ids),
                             _ptr(codes), _stream(stream)))
     return codes
+
+
+# ------------------------------------------- operators on the vectors (qadc_vec.h) --
+# Matrices are two-dimensional, their last stride 1; rows may lie any distance apart.  Outputs that are not given, and workspaces,
+# are allocated for the stream that the call runs on.
+VEC_F32, VEC_BF16, VEC_F16, VEC_E4M3, VEC_E5M2, VEC_E8M0 = range(6)
+VEC_BLOCK = 128
+_VEC_TYPE = {torch.float32: VEC_F32, torch.bfloat16: VEC_BF16, torch.float16: VEC_F16, torch.float8_e4m3fn: VEC_E4M3,
+             torch.float8_e5m2: VEC_E5M2, torch.float8_e8m0fnu: VEC_E8M0}
+
+
+def _refuse(cond: bool, msg: str) -> None:
+    if cond:
+        raise QadcError(PQ_EINVAL, msg)
+
+
+def _vec_type(what: str, dtype) -> int:
+    t = _VEC_TYPE.get(dtype)
+    _refuse(t is None, f"{what}: no operator takes {dtype}")
+    return t
+
+
+class _Call:
+    """The device and the stream of a call, for its checks, allocations and launch."""
+
+    def __init__(self, name: str, first: torch.Tensor, stream):
+        _refuse(not first.is_cuda, f"{name}: tensors of the GPU, got {first.device}")
+        self.name, self.device = name, first.device
+        current = torch.cuda.current_stream(first.device)
+        self.stream = current if stream is None else stream
+        _refuse(self.stream.device != self.device, f"{name}: a stream of {self.stream.device} for tensors of {self.device}")
+        self.elsewhere = self.stream != current or self.device.index != torch.cuda.current_device()
+
+    def empty(self, shape, dtype) -> torch.Tensor:
+        if self.elsewhere:
+            with torch.cuda.stream(self.stream):
+                return torch.empty(shape, dtype=dtype, device=self.device)
+        return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def rows(self, what: str, t: Optional[torch.Tensor], shape=None, dtype=None):
+        """(pointer, distance of rows) of a matrix, checked; (None, 0) without one."""
+        if t is None:
+            return None, 0
+        _refuse(t.device != self.device, f"{self.name}: {what} is on {t.device}, not {self.device}")
+        _refuse(t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)),
+                f"{self.name}: {what} of shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if shape is not None else ""))
+        _refuse(dtype is not None and t.dtype != dtype, f"{self.name}: {what} is {t.dtype}, not {dtype}")
+        n, d = t.shape
+        _refuse(d > 1 and t.stride(1) != 1, f"{self.name}: {what}'s values of a row are {t.stride(1)} apart")
+        ld = t.stride(0) if n > 1 else max(d, 1)
+        _refuse(ld < d, f"{self.name}: {what}'s rows of {d} are {ld} apart")
+        return t.data_ptr(), max(ld, 1)
+
+    def vector(self, what: str, t: torch.Tensor, n: Optional[int] = None, dtype=None) -> int:
+        _refuse(t.device != self.device, f"{self.name}: {what} is on {t.device}, not {self.device}")
+        _refuse(not t.is_contiguous() or (n is not None and (t.dim() != 1 or t.numel() != n)),
+                f"{self.name}: {what} of shape {tuple(t.shape)}, strides {t.stride()}")
+        _refuse(dtype is not None and t.dtype != dtype, f"{self.name}: {what} is {t.dtype}, not {dtype}")
+        return t.data_ptr()
+
+    def workspace(self, t: Optional[torch.Tensor], nbytes: int):
+        """(pointer, bytes); the tensor too, to be kept until the launch."""
+        if t is None:
+            t = self.empty(nbytes, torch.uint8) if nbytes else None
+        if t is None:
+            return None, 0, None
+        return self.vector("workspace", t), t.numel() * t.element_size(), t
+
+    def ids(self, t: torch.Tensor):
+        _refuse(t.dtype not in (torch.int32, torch.int64), f"{self.name}: ids are int32 or int64, got {t.dtype}")
+        return self.vector("ids", t), t.element_size()
+
+    def launch(self, fn, *args) -> None:
+        if self.elsewhere:
+            with torch.cuda.device(self.device):
+                _check(fn(*args, self.stream.cuda_stream or None))
+        else:
+            _check(fn(*args, self.stream.cuda_stream or None))
+
+
+def vec_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype: Optional[torch.dtype] = None,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """scale * table[ids] as [*ids.shape, d]; zeros where an id is outside the table (a search pads with -1)."""
+    call = _Call("vec_lookup", table, stream)
+    ptr, ld = call.rows("table", table)
+    idp, id_bytes = call.ids(ids)
+    n, (rows, d) = ids.numel(), table.shape
+    _refuse(out is not None and dtype is not None and out.dtype != dtype, f"vec_lookup: out is {None if out is None else out.dtype}, not {dtype}")
+    if out is None:
+        out = call.empty((*ids.shape, d), dtype or table.dtype)
+        optr, old = out.data_ptr(), d
+    else:
+        optr, old = call.rows("out", out, (n, d))
+    call.launch(load().vec_lookup, ptr, rows, d, ld, _vec_type("table", table.dtype), idp, id_bytes, n, scale, optr, old,
+                _vec_type("out", out.dtype))
+    return out
+
+
+def vec_lookup_grad_workspace_bytes(n: int, rows: int, d: int) -> int:
+    return int(load().vec_lookup_grad_workspace_bytes(n, rows, d))
+
+
+def vec_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 1.0, dtype: Optional[torch.dtype] = None,
+                    out: Optional[torch.Tensor] = None, accumulate: bool = False, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Gradient [rows, d] of vec_lookup's table from the gradient [n, d] (or [*ids.shape, d]) of its result; with `accumulate` it
+    is added to `out`."""
+    call = _Call("vec_lookup_grad", grad, stream)
+    if grad.dim() != 2:
+        _refuse(not grad.is_contiguous() or grad.dim() == 0, "vec_lookup_grad: grad of other than two dimensions is contiguous")
+        grad = grad.view(-1, grad.shape[-1])
+    d = grad.shape[1]
+    ptr, ld = call.rows("grad", grad, (ids.numel(), d))
+    idp, id_bytes = call.ids(ids)
+    _refuse(accumulate and out is None, "vec_lookup_grad: accumulate needs an out to add to")
+    _refuse(out is not None and dtype is not None and out.dtype != dtype, f"vec_lookup_grad: out is {None if out is None else out.dtype}, not {dtype}")
+    if out is None:
+        out = call.empty((rows, d), dtype or grad.dtype)
+    optr, old = call.rows("out", out, (rows, d))
+    lib = load()
+    wptr, wbytes, keep = call.workspace(workspace, int(lib.vec_lookup_grad_workspace_bytes(ids.numel(), rows, d)))
+    call.launch(lib.vec_lookup_grad, ptr, ids.numel(), d, ld, _vec_type("grad", grad.dtype), idp, id_bytes, scale, int(accumulate),
+                optr, rows, old, _vec_type("out", out.dtype), wptr, wbytes)
+    return out
+
+
+def _blocks_out(call: _Call, n: int, d: int, quant, scale_dtype, out):
+    """8-bit values and scales: those given, or new ones whose rows start at multiples of 16 bytes."""
+    _refuse(scale_dtype not in (torch.float8_e8m0fnu, torch.float32), f"{call.name}: scales of {scale_dtype}")
+    _refuse(quant not in (torch.float8_e4m3fn, torch.float8_e5m2), f"{call.name}: 8-bit values of {quant}")
+    nb = -(-d // VEC_BLOCK)
+    if out is not None:
+        q, scales = out
+    else:
+        q = call.empty((n, -(-d // 16) * 16), quant)
+        if q.shape[1] != d:
+            q = q[:, :d]
+        scales = call.empty((n, nb), scale_dtype)
+    return (q, scales, *call.rows("q", q, (n, d), quant), *call.rows("scales", scales, (n, nb), scale_dtype))
+
+
+def vec_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+             want_y: bool = True, quant: Optional[torch.dtype] = None, scale_dtype: Optional[torch.dtype] = torch.float8_e8m0fnu,
+             out=None, stream=None):
+    """Root-mean-square norm of x + residual.  Returns (y, h, q, scales): y where wanted, h = x + residual where there is one,
+    8-bit values and scales of y where `quant` names their type; else None.  `out`: the same four, to be written (h may be x or
+    residual)."""
+    call = _Call("vec_norm", x, stream)
+    xp, ldx = call.rows("x", x)
+    n, d = x.shape
+    rp, ldr = call.rows("residual", residual, (n, d), x.dtype)
+    wp = call.vector("weight", weight, d)
+    y, h, q, scales = out if out is not None else (None,) * 4
+    if out is None:
+        y = call.empty((n, d), x.dtype) if want_y else None
+        h = call.empty((n, d), x.dtype) if residual is not None else None
+    yp, ldy = call.rows("y", y, (n, d), x.dtype)
+    hp, ldh = call.rows("h", h, (n, d), x.dtype)
+    qp, ldq, sp, lds = None, 0, None, 0
+    if quant is not None or q is not None:
+        if q is not None:
+            quant, scale_dtype = q.dtype, scales.dtype
+        q, scales, qp, ldq, sp, lds = _blocks_out(call, n, d, quant, scale_dtype, None if q is None else (q, scales))
+    call.launch(load().vec_norm, xp, ldx, rp, ldr, _vec_type("x", x.dtype), wp, _vec_type("weight", weight.dtype), n, d, eps, hp, ldh,
+                yp, ldy, qp, ldq, _VEC_TYPE.get(quant, VEC_E4M3), sp, lds, _VEC_TYPE.get(scale_dtype, VEC_E8M0))
+    return y, h, q, scales
+
+
+def vec_norm_grad_workspace_bytes(n: int, d: int) -> int:
+    return int(load().vec_norm_grad_workspace_bytes(n, d))
+
+
+def vec_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, dh: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  out=None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dweight) of vec_norm: h is its second result (x without a residual), dh the gradient that reaches h past the norm.
+    `out`: the same two, to be written (dx may be dy or dh; dweight is float32)."""
+    call = _Call("vec_norm_grad", dy, stream)
+    yp, ldy = call.rows("dy", dy)
+    n, d = dy.shape
+    hp, ldh = call.rows("h", h, (n, d), dy.dtype)
+    ep, lde = call.rows("dh", dh, (n, d), dy.dtype)
+    wp = call.vector("weight", weight, d)
+    dx, dweight = out if out is not None else (call.empty((n, d), dy.dtype), call.empty((d,), torch.float32))
+    xp, ldx = call.rows("dx", dx, (n, d), dy.dtype)
+    dwp = call.vector("dweight", dweight, d, torch.float32)
+    lib = load()
+    wsp, wbytes, keep = call.workspace(workspace, int(lib.vec_norm_grad_workspace_bytes(n, d)))
+    call.launch(lib.vec_norm_grad, yp, ldy, hp, ldh, ep, lde, _vec_type("dy", dy.dtype), wp, _vec_type("weight", weight.dtype), n, d, eps,
+                xp, ldx, dwp, wsp, wbytes)
+    return dx, dweight
+
+
+def vec_quantize_blocks(x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3fn, scale_dtype: torch.dtype = torch.float8_e8m0fnu,
+                        transposed: bool = False, out=None, stream=None):
+    """(q, scales): x in 8 bits with a scale for each 128 values of a row, or, transposed, of a column (q is then x's transpose)."""
+    call = _Call("vec_quantize_blocks", x, stream)
+    xp, ldx = call.rows("x", x)
+    n, d = x.shape
+    q, scales, qp, ldq, sp, lds = _blocks_out(call, *((d, n) if transposed else (n, d)), dtype, scale_dtype, out)
+    call.launch(load().vec_quantize_blocks, xp, ldx, _vec_type("x", x.dtype), n, d, int(transposed), qp, ldq, _VEC_TYPE[dtype], sp, lds,
+                _VEC_TYPE[scale_dtype])
+    return q, scales
+
+
+def vec_matmul_blocks_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(load().vec_matmul_blocks_workspace_bytes(m, n, k))
+
+
+def vec_matmul_blocks(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+                      dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """a b^T of 8-bit matrices [m, k] and [n, k] with their scales [m or n, ceil(k / 128)]; bfloat16 unless `dtype` or `out` says else."""
+    call = _Call("vec_matmul_blocks", a, stream)
+    ap, lda = call.rows("a", a)
+    m, k = a.shape
+    n = b.shape[0]
+    nb = -(-k // VEC_BLOCK)
+    bp, ldb = call.rows("b", b, (n, k))
+    asp, ldas = call.rows("a_scales", a_scales, (m, nb))
+    bsp, ldbs = call.rows("b_scales", b_scales, (n, nb), a_scales.dtype)
+    _refuse(out is not None and dtype is not None and out.dtype != dtype, f"vec_matmul_blocks: out is {None if out is None else out.dtype}, not {dtype}")
+    if out is None:
+        out = call.empty((m, n), dtype or torch.bfloat16)
+    cp, ldc = call.rows("out", out, (m, n))
+    lib = load()
+    wptr, wbytes, keep = call.workspace(workspace, int(lib.vec_matmul_blocks_workspace_bytes(m, n, k)))
+    call.launch(lib.vec_matmul_blocks, ap, lda, _vec_type("a", a.dtype), asp, ldas, bp, ldb, _vec_type("b", b.dtype), bsp, ldbs,
+                _vec_type("scales", a_scales.dtype), m, n, k, cp, ldc, _vec_type("out", out.dtype), wptr, wbytes)
+    return out

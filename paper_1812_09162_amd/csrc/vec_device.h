@@ -1,0 +1,169 @@
+// Shared by the operators on vectors (qadc_vec.h): element types, loads and stores of eight elements at any
+// alignment, sums over groups of lanes, scales of 8-bit blocks; and the host's checks of arguments.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "qadc_internal.h"
+#include "qadc_vec.h"
+
+typedef float vec_f4 __attribute__((ext_vector_type(4)));
+typedef float vec_f8 __attribute__((ext_vector_type(8)));
+typedef int vec_i4 __attribute__((ext_vector_type(4)));
+typedef int vec_i8 __attribute__((ext_vector_type(8)));
+
+// Eight elements as they lie in memory.  Global loads and stores work at any byte address here; the types only promise
+// the alignment of one element.
+template <class T>
+struct VecPack;
+template <>
+struct VecPack<float> {
+    typedef float type __attribute__((ext_vector_type(8), aligned(4)));
+};
+template <>
+struct VecPack<__bf16> {
+    typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2)));
+};
+template <>
+struct VecPack<_Float16> {
+    typedef _Float16 type __attribute__((ext_vector_type(8), aligned(2)));
+};
+
+template <class T>
+using vec_pack = typename VecPack<T>::type;
+
+// left: elements of the row from p on (those beyond it read as zero and are not touched)
+template <class T>
+__device__ __forceinline__ vec_pack<T> vec_load(const T *p, int64_t left) {
+    if (left >= 8) return *(const vec_pack<T> *)p;
+    vec_pack<T> v = (vec_pack<T>)(T)0.0f;
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) v[i] = p[i];
+    return v;
+}
+template <class T>
+__device__ __forceinline__ vec_f8 vec_wide(vec_pack<T> v) {
+    return __builtin_convertvector(v, vec_f8);
+}
+template <class T>
+__device__ __forceinline__ void vec_store(T *p, int64_t left, vec_f8 f) {
+    const vec_pack<T> v = __builtin_convertvector(f, vec_pack<T>);
+    if (left >= 8) {
+        *(vec_pack<T> *)p = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) p[i] = v[i];
+}
+// eight bytes
+__device__ __forceinline__ void vec_store_bytes(uint8_t *p, int64_t left, uint64_t v) {
+    typedef uint64_t any64 __attribute__((aligned(1)));
+    if (left >= 8) {
+        *(any64 *)p = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+        if (i < left) p[i] = (uint8_t)(v >> (8 * i));
+}
+
+// Sum, or largest, over the LANES (16, 32 or 64) neighbouring lanes of a row; every one of them has the result.
+template <int LANES>
+__device__ __forceinline__ float vec_sum(float v) {
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+__device__ __forceinline__ float vec_max16(float v) {
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// The largest finite magnitude of eight values.
+__device__ __forceinline__ float vec_top(vec_f8 f) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float a = fabsf(f[i]);
+        m = fmaxf(m, a < INFINITY ? a : 0.0f);
+    }
+    return m;
+}
+
+// A block's scale from its largest finite magnitude.  448 = 1.75 * 2^8 and 57344 = 1.75 * 2^15, so that the smallest power of
+// two that brings a = f * 2^e within range is 2^(e - 8) or 2^(e - 15), one more where f exceeds 1.75.
+struct VecScale {
+    float scale;     // F32
+    uint32_t e8m0;   // E8M0: the byte
+    float inverse;   // ... and one over the power
+};
+__device__ __forceinline__ VecScale vec_scale(float top, bool e5m2, bool pow2) {
+    VecScale s;
+    const uint32_t u = __float_as_uint(top);
+    int e = (int)(u >> 23) - (e5m2 ? 15 : 8) + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e = top == 0.0f ? 127 : (e < 0 ? 0 : e);
+    s.e8m0 = (uint32_t)e;
+    s.inverse = __uint_as_float((uint32_t)(254 - e) << 23);
+    s.scale = 1.0f;
+    if (!pow2 && top != 0.0f) s.scale = fmaxf(top / (e5m2 ? 57344.0f : 448.0f), 1.17549435e-38f);
+    return s;
+}
+// Eight values over the scale, to 8 bits each (an infinity is made NaN where the type has none).
+__device__ __forceinline__ uint64_t vec_to8(vec_f8 f, const VecScale &s, bool e5m2, bool pow2) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = pow2 ? f[i] * s.inverse : f[i] / s.scale;
+    int lo = 0, hi = 0;
+    if (e5m2) {
+        lo = __builtin_amdgcn_cvt_pk_bf8_f32(v[0], v[1], lo, false);
+        lo = __builtin_amdgcn_cvt_pk_bf8_f32(v[2], v[3], lo, true);
+        hi = __builtin_amdgcn_cvt_pk_bf8_f32(v[4], v[5], hi, false);
+        hi = __builtin_amdgcn_cvt_pk_bf8_f32(v[6], v[7], hi, true);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fabsf(v[i]) < INFINITY ? v[i] : NAN;
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
+        lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
+        hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
+    }
+    return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
+}
+__device__ __forceinline__ void vec_put_scale(void *scales, int64_t at, const VecScale &s, bool pow2) {
+    if (pow2) ((uint8_t *)scales)[at] = (uint8_t)s.e8m0;
+    else ((float *)scales)[at] = s.scale;
+}
+
+// ---------------------------------------------------------------------- host
+static inline bool vec_is_wide(int t) { return t == VEC_F32 || t == VEC_BF16 || t == VEC_F16; }
+static inline bool vec_is_8bit(int t) { return t == VEC_E4M3 || t == VEC_E5M2; }
+static inline bool vec_is_scale(int t) { return t == VEC_E8M0 || t == VEC_F32; }
+static inline size_t vec_bytes(int t) { return t == VEC_F32 ? 4 : (t == VEC_BF16 || t == VEC_F16 ? 2 : 1); }
+static inline size_t vec_up256(size_t x) { return (x + 255) & ~(size_t)255; }
+static inline bool vec_aligned(const void *p, int t) { return ((uintptr_t)p & (vec_bytes(t) - 1)) == 0; }
+
+#define VEC_REQUIRE(cond, ...)           \
+    do {                                 \
+        if (!(cond)) {                   \
+            qadc_set_error(__VA_ARGS__); \
+            return PQ_EINVAL;            \
+        }                                \
+    } while (0)
+
+// Calls BODY with T the C++ type of the element type t.
+#define VEC_TYPED(t, T, ...)             \
+    do {                                 \
+        if ((t) == VEC_F32) {            \
+            using T = float;             \
+            __VA_ARGS__;                 \
+        } else if ((t) == VEC_BF16) {    \
+            using T = __bf16;            \
+            __VA_ARGS__;                 \
+        } else {                         \
+            using T = _Float16;          \
+            __VA_ARGS__;                 \
+        }                                \
+    } while (0)

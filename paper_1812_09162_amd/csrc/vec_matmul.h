@@ -1,0 +1,367 @@
+// vec_matmul_blocks: the kernels.  c = a b^T over 8-bit factors whose rows carry a scale for each 128 values.
+//
+// The matrix cores' own 8-bit products add eight terms at a time after aligning them to the largest and dropping what lies
+// below 2^-13 of it (measured, e4m3 and e5m2, with and without scales): a sum is then 1.5e-5 of its size off, not the 1e-7 of
+// float32, and a result in float32 shows it.  So the factors are read and kept as bytes and become bfloat16 in registers, which holds
+// every one of them exactly (with its power of two, if scales are E8M0), and v_mfma_f32_16x16x32_bf16 adds their products
+// in float32.  F32 scales multiply each block's sum.  b's rows are the instruction's first factor, so that a lane holds
+// four neighbouring columns of c.  Lane l holds 32 of the 128 values of row l % 16; which 32 is the same for both factors, so that
+// their order does not matter.
+#pragma once
+#include "vec_device.h"
+
+struct MatArgs {
+    const uint8_t *a, *b;
+    const void *a_scales, *b_scales;
+    int64_t ld_a, ld_b, ld_as, ld_bs;
+    int64_t m, n, k;
+    void *c;
+    int64_t ld_c;
+    int c_type;
+    float *part;          // split products: [split][m][n], joined by k_vec_mat_join
+    int splits, per;      // per: blocks of k per split
+    int tm, tn;           // tiles
+};
+
+typedef __bf16 vec_b2 __attribute__((ext_vector_type(2)));
+typedef __bf16 vec_b8 __attribute__((ext_vector_type(8)));
+
+// Eight 8-bit values times a power of two, given by the exponent of `scale` (E5: E5M2).  What falls below 2^-126 becomes zero.
+template <int E5>
+__device__ __forceinline__ vec_b8 mat_widen(int lo, int hi, float scale) {
+    vec_b2 v[4];
+    if constexpr (E5) {
+        v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, false);
+        v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, true);
+        v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false);
+        v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
+    } else {
+        v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+        v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+        v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+        v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    }
+    return __builtin_shufflevector(__builtin_shufflevector(v[0], v[1], 0, 1, 2, 3), __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Sixteen bytes of a lane's row, as two factors of a product step.
+struct MatHalf {
+    vec_b8 v[2];
+};
+template <int E5>
+__device__ __forceinline__ MatHalf mat_half(vec_i4 x, float scale) {
+    return {{mat_widen<E5>(x[0], x[1], scale), mat_widen<E5>(x[2], x[3], scale)}};
+}
+__device__ __forceinline__ vec_f4 mat_mul(const MatHalf &b, const MatHalf &a, vec_f4 c) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[0], a.v[0], c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[1], a.v[1], c, 0, 0, 0);
+}
+// E8M0 as the float32 whose exponent it is (0, 2^-127, is a zero there: mat_widen looks at the exponent alone).
+__device__ __forceinline__ uint32_t mat_scale_bits(const void *scales, int64_t at, bool pow2) {
+    return pow2 ? (uint32_t)((const uint8_t *)scales)[at] << 23 : ((const uint32_t *)scales)[at];
+}
+
+// Sixteen bytes of a row from column k on, at any address; zeros beyond column `end`.
+__device__ __forceinline__ vec_i4 mat_chunk(const uint8_t *row, int64_t k, int64_t end) {
+    typedef int any128 __attribute__((ext_vector_type(4), aligned(1)));
+    if (k + 16 <= end) return *(const any128 *)(row + k);
+    vec_i4 v = {0, 0, 0, 0};
+    for (int i = 0; i < 16 && k + i < end; ++i) v[i >> 2] |= (int)row[k + i] << (8 * (i & 3));
+    return v;
+}
+
+__device__ __forceinline__ vec_i4 mat_chunk(const uint8_t *p) {
+    typedef int any128 __attribute__((ext_vector_type(4), aligned(1)));
+    return *(const any128 *)p;
+}
+
+__device__ __forceinline__ void mat_store(const MatArgs &p, int64_t row, int64_t col, vec_f4 v) {
+    typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+    typedef __bf16 b4u __attribute__((ext_vector_type(4), aligned(2)));
+    typedef _Float16 h4u __attribute__((ext_vector_type(4), aligned(2)));
+    const int64_t at = row * p.ld_c + col;
+    if (col + 4 <= p.n) {
+        if (p.c_type == VEC_F32) *(f4u *)((float *)p.c + at) = v;
+        else if (p.c_type == VEC_BF16) *(b4u *)((__bf16 *)p.c + at) = __builtin_convertvector(v, b4u);
+        else *(h4u *)((_Float16 *)p.c + at) = __builtin_convertvector(v, h4u);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (col + i < p.n) {
+            if (p.c_type == VEC_F32) ((float *)p.c)[at + i] = v[i];
+            else if (p.c_type == VEC_BF16) ((__bf16 *)p.c)[at + i] = (__bf16)v[i];
+            else ((_Float16 *)p.c)[at + i] = (_Float16)v[i];
+        }
+}
+
+// ------------------------------------------------------------------- tiles --
+// A block of WM x WN waves makes a tile of c; a wave 16 MI rows by 16 NI columns of it.  Blocks of k pass through two buffers
+// of LDS: while one is multiplied, the next is on its way to the other, from memory to LDS without registers (ASYNC: rows
+// that start at multiples of 16 bytes) or through them.  A row of a buffer is 128 bytes, its sixteen-byte pieces exchanged by
+// the row's low three bits, so that eight lanes that read the same piece of eight rows meet eight different banks.
+// A last block of fewer than 128 columns always comes through registers, with zeros behind.
+// Rows beyond the matrix are the last row again; what comes of them is not stored.
+template <int FA, int FB, bool P2, bool ASYNC, int WM, int WN, int MI, int NI>
+__global__ void __launch_bounds__(64 * WM * WN)
+k_vec_mat(const MatArgs p) {
+    constexpr int BM = WM * MI * 16, BN = WN * NI * 16, ROWS = BM + BN, WAVES = WM * WN, NT = 64 * WAVES;
+    constexpr int PER = ROWS / 8 / WAVES;  // wave instructions per step: eight rows each
+    constexpr int STAGE = ROWS * 132;      // bytes of a buffer: values and scales
+    static_assert(ROWS <= NT && (ROWS / 8) % WAVES == 0 && BM % (8 * PER) == 0, "a thread brings one scale; a wave's rows are of one factor");
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+
+    // tile: neighbouring blocks are dealt out over the eight dies, so each die gets a run of tiles of its own; within it, eight rows
+    // of tiles at a time share the columns' factors in the die's cache
+    int id = blockIdx.x;
+    {
+        const int total = gridDim.x, q = total / 8, r = total % 8, x = id & 7;
+        id = x * q + (x < r ? x : r) + (id >> 3);
+    }
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int group = id / (8 * p.tn), in_group = id - group * 8 * p.tn;
+    const int high = p.tm - group * 8 < 8 ? p.tm - group * 8 : 8;
+    const int64_t m0 = (int64_t)(group * 8 + in_group % high) * BM, n0 = (int64_t)(in_group / high) * BN;
+
+    const int steps = (int)((p.k + VEC_BLOCK - 1) / VEC_BLOCK);
+    const int s0 = split * p.per, s1 = s0 + p.per < steps ? s0 + p.per : steps;
+    const int whole = (int)(p.k / VEC_BLOCK) < s1 ? (int)(p.k / VEC_BLOCK) : s1;  // steps before this one are of 128 columns
+
+    // this wave's rows of the buffer: wave * 8 PER ..
+    const bool is_b = wave * 8 * PER >= BM;
+    const int64_t ld = is_b ? p.ld_b : p.ld_a;
+    const int64_t first = is_b ? n0 + wave * 8 * PER - BM : m0 + wave * 8 * PER, last = (is_b ? p.n : p.m) - 1;
+    const int64_t from = first < last ? first : last;
+    const uint8_t *mat = (is_b ? p.b : p.a) + from * ld;
+    const int most = (int)(last - from < ROWS ? last - from : ROWS);  // rows from there on
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // the columns that this lane's place in a row holds
+    auto delta = [&](int i) { return i * 8 + (lane >> 3) < most ? i * 8 + (lane >> 3) : most; };
+    uint32_t off[ASYNC ? PER : 1];  // (ASYNC: rows are less than 2^23 apart)
+    if constexpr (ASYNC)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) off[i] = (uint32_t)delta(i) * (uint32_t)ld + piece;
+    // ... and the thread's scale
+    const bool sc = (int)threadIdx.x < ROWS, sc_b = (int)threadIdx.x >= BM;
+    const int64_t sr = sc_b ? n0 + threadIdx.x - BM : m0 + threadIdx.x, sl = (sc_b ? p.n : p.m) - 1;
+    const int64_t srow = (sr < sl ? sr : sl) * (sc_b ? p.ld_bs : p.ld_as);
+    const void *const sp = sc_b ? p.b_scales : p.a_scales;
+    // (E8M0: a lane needs its row's in tiles of sixteen rows, and those of four tiles lie side by side.  F32: b's are needed for four
+    // neighbouring rows, a's for one.)
+    const int t = threadIdx.x, st = ROWS * 128 + 4 * (P2 ? (t & ~63) + (t & 15) * 4 + (t >> 4 & 3) : t);
+
+    vec_f4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = (vec_f4)0.0f;
+
+    const int wm = wave / WN, wn = wave % WN;
+    const int frag = (lane & 15) * 128 + (((lane >> 4) * 2) ^ (lane & 7)) * 16;  // its first sixteen bytes of sixteen rows; the second: ^ 16
+
+    uint32_t scale_next = 0;
+    vec_i4 regs[ASYNC ? 1 : PER];
+    auto request_scale = [&](int s) {
+        if (sc) scale_next = mat_scale_bits(sp, srow + s, P2);
+    };
+    auto put_scale = [&](int buf) {
+        if (sc) *(uint32_t *)(lds + buf + st) = scale_next;
+    };
+    auto request = [&](int s, int buf) {  // a whole step
+        request_scale(s);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if constexpr (ASYNC)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(mat + (int64_t)s * 128 + off[i]),
+                                                 (__attribute__((address_space(3))) void *)(lds + buf + (wave * PER + i) * 1024), 16, 0, 0);
+            else
+                regs[i] = mat_chunk(mat + delta(i) * ld, (int64_t)s * 128 + piece, p.k);
+        }
+    };
+    auto put = [&](int buf) {
+        put_scale(buf);
+        if constexpr (!ASYNC)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) *(vec_i4 *)(lds + buf + (wave * PER + i) * 1024 + lane * 16) = regs[i];
+    };
+    auto multiply = [&](int buf) {
+        const int fa = buf + wm * MI * 2048 + frag, fb = buf + BM * 128 + wn * NI * 2048 + frag;
+        const int sca = buf + ROWS * 128, scb = sca + BM * 4;
+        // (bit 4 tells a lane's two pieces apart, and no tile's offset has it)
+        auto load = [&](int at, int half) { return *(const vec_i4 *)(lds + (half ? at ^ 16 : at)); };
+        if constexpr (P2) {
+            vec_f4 sa[MI / 4], sb[NI / 4];
+#pragma unroll
+            for (int i = 0; i < MI / 4; ++i) sa[i] = *(const vec_f4 *)(lds + sca + ((wm * MI / 4 + i) * 64 + (lane & 15) * 4) * 4);
+#pragma unroll
+            for (int j = 0; j < NI / 4; ++j) sb[j] = *(const vec_f4 *)(lds + scb + ((wn * NI / 4 + j) * 64 + (lane & 15) * 4) * 4);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                MatHalf b[NI];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) b[j] = mat_half<FB>(load(fb + j * 2048, half), sb[j / 4][j % 4]);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const MatHalf a = mat_half<FA>(load(fa + i * 2048, half), sa[i / 4][i % 4]);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = mat_mul(b[j], a, acc[i][j]);
+                }
+            }
+        } else {
+            MatHalf b[2][NI];
+            vec_f4 sb[NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                b[0][j] = mat_half<FB>(load(fb + j * 2048, 0), 1.0f);
+                b[1][j] = mat_half<FB>(load(fb + j * 2048, 1), 1.0f);
+                sb[j] = *(const vec_f4 *)(lds + scb + ((wn * NI + j) * 16 + (lane >> 4) * 4) * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const MatHalf a0 = mat_half<FA>(load(fa + i * 2048, 0), 1.0f), a1 = mat_half<FA>(load(fa + i * 2048, 1), 1.0f);
+                const float sa = *(const float *)(lds + sca + ((wm * MI + i) * 16 + (lane & 15)) * 4);
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    const vec_f4 q = mat_mul(b[1][j], a1, mat_mul(b[0][j], a0, (vec_f4)0.0f));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = __fmaf_rn(q[r], sa * sb[j][r], acc[i][j][r]);
+                }
+            }
+        }
+    };
+    auto landed = [&]() {  // the buffer on its way is whole, and nobody reads the other any more
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+
+    int now = 0, other = STAGE;
+    if (s0 < whole) {
+        request(s0, now);
+        put(now);
+        for (int s = s0; s < whole; ++s) {
+            landed();
+            if (s + 1 < whole) request(s + 1, other);
+            multiply(now);
+            if (s + 1 < whole) put(other);
+            now = other;
+            other = STAGE - now;
+        }
+    }
+    if (whole < s1) {  // fewer than 128 columns are left
+        request_scale(whole);
+        put_scale(now);
+#pragma unroll 1
+        for (int i = 0; i < PER; ++i)
+            *(vec_i4 *)(lds + now + (wave * PER + i) * 1024 + lane * 16) = mat_chunk(mat + delta(i) * ld, (int64_t)whole * 128 + piece, p.k);
+        __syncthreads();
+        multiply(now);
+    }
+
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int64_t r = m0 + (wm * MI + i) * 16 + (lane & 15);
+        if (r >= p.m) continue;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int64_t c = n0 + (wn * NI + j) * 16 + (lane >> 4) * 4;
+            if (p.splits == 1) {
+                mat_store(p, r, c, acc[i][j]);
+            } else {
+                float *q = p.part + ((int64_t)split * p.m + r) * p.n + c;
+                typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+                if (c + 4 <= p.n) *(f4u *)q = acc[i][j];
+                else
+                    for (int e = 0; e < 3; ++e)
+                        if (c + e < p.n) q[e] = acc[i][j][e];
+            }
+        }
+    }
+}
+
+// -------------------------------------------------------------- few rows of a --
+// Up to 16 MF rows of a: b is read once, straight from memory to the registers of the lanes that multiply it; a wave takes
+// sixteen rows of b and a share of k, and the shares of a block's waves are joined in LDS.  Bound by reading b.
+#define MAT_FEW_WAVES 8
+template <int FA, int FB, bool P2, int MF>
+__global__ void __launch_bounds__(64 * MAT_FEW_WAVES)
+k_vec_mat_few(const MatArgs p, int kshare) {
+    __shared__ vec_f4 sums[MAT_FEW_WAVES][MF][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t tile = (int64_t)blockIdx.x * (MAT_FEW_WAVES / kshare) + wave / kshare;
+    const int share = wave % kshare;
+    const int steps = (int)((p.k + VEC_BLOCK - 1) / VEC_BLOCK);
+    const int64_t n0 = tile * 16, nr = n0 + (lane & 15) < p.n ? n0 + (lane & 15) : p.n - 1;
+    const uint8_t *rb = p.b + nr * p.ld_b;
+    const uint8_t *ra[MF];
+    int64_t ma[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        ma[f] = f * 16 + (lane & 15) < p.m ? f * 16 + (lane & 15) : p.m - 1;
+        ra[f] = p.a + ma[f] * p.ld_a;
+    }
+    vec_f4 acc[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) acc[f] = (vec_f4)0.0f;
+    const int col = (lane >> 4) * 32;
+    // chunk(row, k): sixteen bytes
+    auto step = [&](int s, auto &&chunk) {
+        const int64_t k = (int64_t)s * VEC_BLOCK + col;
+        if constexpr (P2) {
+            const float sb = __uint_as_float(mat_scale_bits(p.b_scales, nr * p.ld_bs + s, true));
+            const MatHalf b0 = mat_half<FB>(chunk(rb, k), sb), b1 = mat_half<FB>(chunk(rb, k + 16), sb);
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                const float sa = __uint_as_float(mat_scale_bits(p.a_scales, ma[f] * p.ld_as + s, true));
+                acc[f] = mat_mul(b0, mat_half<FA>(chunk(ra[f], k), sa), acc[f]);
+                acc[f] = mat_mul(b1, mat_half<FA>(chunk(ra[f], k + 16), sa), acc[f]);
+            }
+        } else {
+            const MatHalf b0 = mat_half<FB>(chunk(rb, k), 1.0f), b1 = mat_half<FB>(chunk(rb, k + 16), 1.0f);
+            vec_f4 sb;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t c = n0 + (lane >> 4) * 4 + r;
+                sb[r] = ((const float *)p.b_scales)[(c < p.n ? c : p.n - 1) * p.ld_bs + s];
+            }
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                const float sa = ((const float *)p.a_scales)[ma[f] * p.ld_as + s];
+                vec_f4 q = mat_mul(b0, mat_half<FA>(chunk(ra[f], k), 1.0f), (vec_f4)0.0f);
+                q = mat_mul(b1, mat_half<FA>(chunk(ra[f], k + 16), 1.0f), q);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[f][r] = __fmaf_rn(q[r], sa * sb[r], acc[f][r]);
+            }
+        }
+    };
+    if (n0 < p.n) {
+        const int whole = (int)(p.k / VEC_BLOCK);
+#pragma unroll 2
+        for (int s = share; s < whole; s += kshare) step(s, [&](const uint8_t *row, int64_t k) { return mat_chunk(row + k); });
+        if (whole < steps && whole % kshare == share) step(whole, [&](const uint8_t *row, int64_t k) { return mat_chunk(row, k, p.k); });
+    }
+    if (kshare > 1) {
+#pragma unroll
+        for (int f = 0; f < MF; ++f) sums[wave][f][lane] = acc[f];
+        __syncthreads();
+        if (share != 0) return;
+        for (int w = 1; w < kshare; ++w)
+#pragma unroll
+            for (int f = 0; f < MF; ++f) acc[f] += sums[wave + w][f][lane];
+    }
+    if (n0 >= p.n) return;
+#pragma unroll
+    for (int f = 0; f < MF; ++f)
+        if (f * 16 + (lane & 15) < p.m) mat_store(p, f * 16 + (lane & 15), n0 + (lane >> 4) * 4, acc[f]);
+}
+
+// The host's choice of a form.
+struct MatPlan {
+    int few;       // 0: tiles; 1, 2, 4: sixteens of rows of a
+    int kshare;    // few: waves that share a tile's k
+    bool big;      // tiles of 256 x 256 instead of 128 x 128
+    int tm, tn, splits, per;
+    size_t workspace;
+};
+// launches of one pair of factor types (vec_matmul.hip, compiled once for each)
+template <int FA, int FB>
+int qadc_vec_mat_launch(const MatArgs &p, const MatPlan &plan, bool pow2, bool async, hipStream_t s);

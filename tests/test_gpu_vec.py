@@ -1,0 +1,566 @@
+"""The operators on vectors against their definitions in 64 bits.  Tolerances count roundings: half a step of the result's
+type for the last one, and 2^-24 for each float32 operation before it, times the sum of magnitudes where terms can cancel."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+E4M3, E5M2, E8M0 = torch.float8_e4m3fn, torch.float8_e5m2, torch.float8_e8m0fnu
+WIDE = [F32, BF16, F16]
+LARGEST = {E4M3: 448.0, E5M2: 57344.0}
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def qb():
+    from paper_1812_09162_amd import binding
+    binding.load()
+    return binding
+
+
+def dev():
+    return torch.device("cuda:0")
+
+
+def rnd(shape, seed, dtype=F32, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * spread).to(dtype).to(dev())
+
+
+def half_step(ref, dtype):
+    """Half a step of dtype at ref (with the subnormal steps of the type)."""
+    return ref.abs() * (torch.finfo(dtype).eps / 2) + torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2
+
+
+def close(got, ref, tol):
+    tol = tol.expand_as(ref)
+    if got.dtype in WIDE:  # what the type cannot hold is an infinity in it
+        most = torch.finfo(got.dtype).max * (1 + torch.finfo(got.dtype).eps / 4)
+        over = ref.abs() + tol >= most
+        assert bool((got.double()[over] - ref[over].clamp(-most, most)).abs().le(tol[over] * 2).logical_or(got[over].double() == torch.sign(ref[over]) * math.inf).all())
+        got, ref, tol = got[~over], ref[~over], tol[~over]
+    off = (got.double() - ref).abs() - tol
+    bad = int((~(off <= 0)).sum())
+    assert bad == 0, f"{bad} of {off.numel()} too far off, by up to {float(off.max())}"
+
+
+def framed(x, before=3, after=5, fill=float("nan")):
+    """x as a view of a larger matrix whose other elements are `fill`: (view, storage)."""
+    n, d = x.shape
+    raw = x.element_size() == 1 and x.dtype != torch.uint8
+    s = torch.full((n + 2, d + before + after), 0x7F if raw else fill, dtype=torch.uint8 if raw else x.dtype, device=dev())
+    if raw:
+        s = s.view(x.dtype)
+    v = s[1:n + 1, before:before + d]
+    if raw:
+        v.view(torch.uint8).copy_(x.view(torch.uint8))
+    else:
+        v.copy_(x)
+    return v, s
+
+
+def untouched(view, storage, was):
+    """Nothing outside the view has changed."""
+    a, b = storage.clone().view(torch.uint8), was.view(torch.uint8)
+    n, d = view.shape
+    es, at = storage.element_size(), view.storage_offset() - storage.shape[1]
+    a[1:n + 1, at * es:(at + d) * es] = 0
+    b = b.clone()
+    b[1:n + 1, at * es:(at + d) * es] = 0
+    return torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- look-up --
+@pytest.mark.parametrize("to", WIDE)
+@pytest.mark.parametrize("t", WIDE)
+@pytest.mark.parametrize("rows,d,n,idt", [(1, 1, 1, torch.int64), (10, 7, 33, torch.int32), (1000, 96, 257, torch.int64), (77, 129, 1025, torch.int32),
+                                          (5, 5000, 3, torch.int64), (50, 9001, 7, torch.int32), (300, 16, 5000, torch.int64)])
+def test_lookup(qb, rows, d, n, idt, t, to):
+    table, store = framed(rnd((rows, d), 1, t))
+    ids = torch.randint(-2, rows + 2, (n,), generator=torch.Generator().manual_seed(2)).to(idt).to(dev())
+    scale = 1.37
+    want = torch.zeros((n, d), dtype=torch.float64, device=dev())
+    ok = (ids >= 0) & (ids < rows)
+    want[ok] = table.double()[ids[ok].long()] * float(torch.tensor(scale, dtype=F32))
+    got = qb.vec_lookup(table, ids, scale=scale, dtype=to)
+    close(got, want, half_step(want, to) + 2 * U * want.abs())
+    assert bool((got[~ok] == 0).all())
+    out, os = framed(torch.zeros((n, d), dtype=to, device=dev()))
+    was = os.clone()
+    qb.vec_lookup(table, ids, scale=scale, out=out)
+    assert torch.equal(out, got) and untouched(out, os, was)
+
+
+def test_lookup_shapes_and_nothing(qb):
+    table = rnd((20, 8), 1)
+    ids = torch.arange(12, device=dev()).view(3, 4)
+    assert torch.equal(qb.vec_lookup(table, ids), table[ids])
+    assert qb.vec_lookup(table, ids[:0]).shape == (0, 4, 8)
+    assert bool((qb.vec_lookup(table[:0], ids) == 0).all())
+    inf = torch.tensor([[math.inf, -math.inf, math.nan, 1.0]], device=dev())
+    got = qb.vec_lookup(inf, torch.zeros(1, dtype=torch.int32, device=dev()), scale=2.0)
+    assert got[0, 0] == math.inf and got[0, 1] == -math.inf and bool(got[0, 2].isnan()) and got[0, 3] == 2
+
+
+def test_lookup_and_gradient_beyond_32_bits(qb):
+    """Elements past 2^32 of the table."""
+    rows, d = 4_300_000, 1024
+    table = torch.empty((rows, d), dtype=BF16, device=dev())
+    at = torch.tensor([0, 1, 2_097_151, 2_097_152, 4_194_303, 4_194_304, 4_299_999, 4_300_000, -1], device=dev())
+    vals = rnd((7, d), 3, BF16)
+    table[at[:7]] = vals
+    got = qb.vec_lookup(table, at)
+    assert torch.equal(got[:7], vals) and bool((got[7:] == 0).all())
+    for n in (9, 5000):  # both forms of the gradient
+        ids = at[:9].repeat(n // 9 + 1)[:n].contiguous()
+        g = torch.ones((n, d), dtype=BF16, device=dev())
+        qb.vec_lookup_grad(g, ids, rows, out=table)
+        for i in range(7):
+            assert bool((table[at[i]] == float((ids == at[i]).sum())).all())
+        assert bool((table[at[:7] - 1 + 2 * (at[:7] == 0)][[2, 4, 6]] == 0).all())
+
+
+# --------------------------------------------------------------- gradient --
+@pytest.mark.parametrize("t,to,idt", [(F32, F32, torch.int64), (BF16, F32, torch.int32), (F16, F16, torch.int64), (BF16, BF16, torch.int64)])
+@pytest.mark.parametrize("rows,d,n,kind", [
+    (1, 1, 1, "same"), (5, 3, 0, "even"), (7, 9, 100, "even"), (1000, 96, 4096, "skew"), (1000, 96, 4097, "skew"), (70_000, 40, 3000, "even"),
+    (3, 24, 9000, "even"), (1, 20, 6000, "same"), (1023, 33, 10_001, "skew"), (1024, 33, 10_001, "skew"), (2000, 513, 20_000, "skew"),
+    (300_001, 8, 50_000, "skew"), (64, 1030, 4500, "skew"), (1500, 16, 65_536, "one"), (9, 700, 4000, "one"), (40, 5, 70_000, "outside")])
+def test_lookup_grad(qb, rows, d, n, kind, t, to, idt):
+    gen = torch.Generator().manual_seed(rows + n)
+    u = torch.rand((n,), generator=gen, dtype=torch.float64)
+    ids = {"even": (u * rows).long(), "skew": (rows ** u - 1).long().clamp(0, rows - 1), "same": torch.zeros(n, dtype=torch.long),
+           "one": torch.where(u < 0.9, rows // 2, (u * rows).long()), "outside": torch.where(u < 0.5, -1, ((u * 2 - 1) * 2 * rows).long())}[kind]
+    ids = ids.to(idt).to(dev())
+    g, _ = framed(rnd((n, d), 5, t))
+    scale = 0.77
+    s32 = float(torch.tensor(scale, dtype=F32))
+    ok = ((ids >= 0) & (ids < rows)).nonzero()[:, 0]
+    want, size, count = (torch.zeros((rows, k), dtype=torch.float64, device=dev()) for k in (d, d, 1))
+    want.index_add_(0, ids[ok].long(), g[ok].double() * s32)
+    size.index_add_(0, ids[ok].long(), g[ok].double().abs() * s32)
+    count.index_add_(0, ids[ok].long(), torch.ones((len(ok), 1), dtype=torch.float64, device=dev()))
+    got = qb.vec_lookup_grad(g, ids, rows, scale=scale, dtype=to)
+    # count - 1 additions (pieces joined: no more), one product, the last rounding
+    close(got, want, U * (count + 1) * size * 1.001 + half_step(want, to))
+    assert bool((got[count[:, 0] == 0] == 0).all())
+    assert torch.equal(got, qb.vec_lookup_grad(g, ids, rows, scale=scale, dtype=to))
+    base, store = framed(rnd((rows, d), 6, to))
+    was, old = store.clone(), base.clone()
+    qb.vec_lookup_grad(g, ids, rows, scale=scale, out=base, accumulate=True)
+    ref = old.double() + want
+    close(base, ref, U * ((count + 2) * size + old.double().abs()) * 1.001 + half_step(ref, to))
+    assert torch.equal(base[count[:, 0] == 0], old[count[:, 0] == 0]) and untouched(base, store, was)
+
+
+def test_lookup_grad_is_the_gradient(qb):
+    """<G, dT> = <g, lookup(dT)> for any dT: the look-up is linear."""
+    ids = torch.randint(0, 50, (400,), generator=torch.Generator().manual_seed(1)).to(dev())
+    g, step = rnd((400, 24), 2), rnd((50, 24), 3)
+    left = (qb.vec_lookup_grad(g, ids, 50, scale=3.0).double() * step.double()).sum()
+    right = (g.double() * qb.vec_lookup(step, ids, scale=3.0).double()).sum()
+    size = (g.double().abs() * 3 * step.double()[ids].abs()).sum()
+    assert abs(float(left - right)) <= float(size) * U * 403
+
+
+# -------------------------------------------------------------- quantizer --
+def blocks_of(x):
+    n, d = x.shape
+    return torch.nn.functional.pad(x, (0, -d % 128)).view(n, -1, 128)
+
+
+def quantized(x, qt, st):
+    """8-bit values and scales of float32 x by definition, on the host (float32 divisions there are correctly rounded)."""
+    x = x.cpu().float()
+    b = blocks_of(x)
+    top = torch.where(b.isfinite(), b.abs(), 0.0).amax(2)
+    if st == E8M0:
+        f, e = torch.frexp(top.double())
+        f8, e8 = math.frexp(LARGEST[qt])
+        power = torch.where(top == 0, 0, (e - e8 + (f > f8)).clamp(-127, 127))
+        scale = torch.ldexp(torch.ones((), dtype=torch.float64), power)
+    else:
+        scale = torch.where(top == 0, 1.0, (top / torch.full_like(top, LARGEST[qt])).clamp(min=2.0 ** -126)).double()
+    v = (b.double() / scale[:, :, None]).float().view(x.shape[0], -1)[:, :x.shape[1]]
+    return v.to(qt), scale
+
+
+def same_values(a, b):
+    a, b = a.cpu().float(), b.cpu().float()
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(torch.where(a.isnan(), 0.0, a), torch.where(b.isnan(), 0.0, b))
+
+
+@pytest.mark.parametrize("qt,st", [(E4M3, E8M0), (E4M3, F32), (E5M2, E8M0), (E5M2, F32)])
+@pytest.mark.parametrize("t", WIDE)
+@pytest.mark.parametrize("n,d", [(1, 1), (3, 127), (130, 128), (128, 129), (257, 400), (64, 1000), (1, 5003)])
+def test_quantize_both_ways(qb, n, d, t, qt, st):
+    x = rnd((n, d), n + d, F32) * torch.exp(3 * rnd((1, d), 8)) * 1e-3
+    x[:, d // 2] *= 2.0 ** -20
+    x = x.clamp(-6e4, 6e4).to(t)
+    x, _ = framed(x)
+    for transposed in (False, True):
+        src = x.t() if transposed else x
+        want, ws = quantized(src, qt, st)
+        q, s = qb.vec_quantize_blocks(x, dtype=qt, scale_dtype=st, transposed=transposed)
+        assert torch.equal(s.cpu().double(), ws) and same_values(q, want)
+        out = [framed(torch.zeros(q.shape, dtype=torch.uint8, device=dev()).view(qt)), framed(torch.zeros(s.shape, device=dev(), dtype=torch.uint8 if st == E8M0 else F32).view(st))]
+        was = [o[1].clone() for o in out]
+        qb.vec_quantize_blocks(x, dtype=qt, scale_dtype=st, transposed=transposed, out=(out[0][0], out[1][0]))
+        assert same_values(out[0][0], want) and torch.equal(out[1][0].cpu().double(), ws)
+        assert untouched(*out[0], was[0]) and untouched(*out[1], was[1])
+
+
+@pytest.mark.parametrize("st", [E8M0, F32])
+@pytest.mark.parametrize("qt", [E4M3, E5M2])
+def test_quantize_borders(qb, qt, st):
+    """Magnitudes around the powers at which the scale changes, halfway cases, zeros, the smallest and largest numbers, infinities, NaN."""
+    L = LARGEST[qt]
+    rows = []
+    for top in (L, L * (1 + 2 ** -7), L * (1 - 2 ** -8), 2 * L, 1.0, 2.0 ** -100, 2.0 ** -126, 2.0 ** -149, 3e38, 1.75, 1.7500001, 0.0, 5e-45):
+        v = torch.linspace(-1, 1, 128, dtype=torch.float64) * top
+        v[0], v[1] = top, -top
+        rows.append(v.float())
+    halves = torch.arange(128).float() * (2.0 ** -5) + 1 + 2.0 ** -5
+    halves[0] = L
+    rows += [halves, -halves]
+    bad = torch.linspace(-2, 2, 128)
+    bad[3], bad[5], bad[9] = math.inf, -math.inf, math.nan
+    rows += [bad, torch.full((128,), math.inf), torch.full((128,), math.nan)]
+    x = torch.stack(rows)
+    q, s = qb.vec_quantize_blocks(x.to(dev()), dtype=qt, scale_dtype=st)
+    want, ws = quantized(x, qt, st)
+    assert torch.equal(s.cpu().double(), ws)
+    assert same_values(q, want)
+    qt2, st2 = qb.vec_quantize_blocks(x.t().contiguous().to(dev()), dtype=qt, scale_dtype=st, transposed=True)
+    assert same_values(qt2, want) and torch.equal(st2.cpu().double(), ws)
+
+
+# ------------------------------------------------------------------- norm --
+# float32 roundings behind y: at most 64 products-and-sums of a lane and 10 of the join, half of them in the root; the mean, eps, the
+# root (2), two products
+NORM_U = 48 * U
+
+
+def norm64(x, r, w, eps):
+    h = x if r is None else (x.float() + r.float()).to(x.dtype)
+    hd = h.double()
+    rms = 1.0 / torch.sqrt((hd * hd).mean(1, keepdim=True) + eps)
+    return h, hd * rms * w.double()
+
+
+@pytest.mark.parametrize("t,wt", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("n,d", [(1, 1), (5, 8), (9, 100), (17, 128), (3, 129), (10, 256), (7, 300), (5, 520), (6, 1001), (4, 1024), (5, 2048), (3, 2055),
+                                 (3, 4100), (2, 8192), (3, 9000), (1, 16_384), (10_000, 96), (2500, 2048)])
+def test_norm(qb, n, d, t, wt):
+    x, _ = framed(rnd((n, d), d, t))
+    r, _ = framed(rnd((n, d), d + 1, t, 2.0))
+    w = (1 + 0.3 * rnd((d,), d + 2)).to(wt)
+    eps = float(torch.tensor(1e-5, dtype=F32))
+    for res in (None, r):
+        h, want = norm64(x, res, w, eps)
+        y, gh, _, _ = qb.vec_norm(x, w, residual=res, eps=eps)
+        assert (gh is None) == (res is None) and (gh is None or torch.equal(gh, h))
+        close(y, want, NORM_U * want.abs() + half_step(want, t))
+        for qt, st in ((E4M3, E8M0), (E5M2, F32)):
+            y2, gh, q, s = qb.vec_norm(x, w, residual=res, eps=eps, want_y=qt == E5M2, quant=qt, scale_dtype=st)
+            assert (y2 is None) == (qt == E4M3) and (y2 is None or torch.equal(y2, y)) and (gh is None or torch.equal(gh, h))
+            top = blocks_of(want.abs()).amax(2)
+            sd = s.double()
+            if st == E8M0:  # the smallest power that holds the block, up to y's roundings
+                assert bool((top * (1 - NORM_U) <= LARGEST[qt] * sd).all()) and bool((top * (1 + NORM_U) * 2 > LARGEST[qt] * sd).all())
+            else:
+                close(s, top / LARGEST[qt], (NORM_U + 2 * U) * top / LARGEST[qt])
+            sr = sd.repeat_interleave(128, 1)[:, :d]
+            step = torch.maximum(want.abs() * (torch.finfo(qt).eps / 2), sr * torch.finfo(qt).smallest_normal * torch.finfo(qt).eps / 2)
+            close(q.double() * sr, want, step * (1 + 2 * NORM_U) + 2 * NORM_U * want.abs())
+
+
+def test_norm_in_place_and_views(qb):
+    n, d = 37, 200
+    for t in (BF16, F32):
+        x, xs = framed(rnd((n, d), 1, t))
+        r, rs = framed(rnd((n, d), 2, t))
+        w = rnd((d,), 3, t)
+        y, h, q, s = qb.vec_norm(x, w, residual=r, quant=E4M3)
+        for into_x in (True, False):
+            a, b = framed(x.clone()), framed(r.clone())
+            target = a if into_x else b
+            was = target[1].clone()
+            y2, yst = framed(torch.zeros_like(y))
+            qb.vec_norm(a[0], w, residual=b[0], out=(y2, target[0], None, None))
+            assert torch.equal(target[0], h) and torch.equal(y2, y) and untouched(target[0], target[1], was)
+        q2, qs = framed(torch.zeros_like(q.view(torch.uint8)).view(E4M3), before=5, after=6)
+        s2, ss = framed(torch.zeros_like(s.view(torch.uint8)).view(E8M0), before=1, after=2)
+        wq, wss = qs.clone(), ss.clone()
+        qb.vec_norm(x, w, residual=r, out=(None, h, q2, s2))
+        assert same_values(q2, q) and same_values(s2, s) and untouched(q2, qs, wq) and untouched(s2, ss, wss)
+
+
+def test_norm_of_zeros_and_nan(qb):
+    x = torch.zeros((4, 256), device=dev())
+    x[1] = 5.0
+    x[2, 7] = math.nan
+    w = torch.ones(256, device=dev())
+    y, _, q, s = qb.vec_norm(x, w, eps=1e-6, quant=E4M3)
+    assert bool((y[0] == 0).all()) and bool((s[0].float() == 1).all()) and bool((q[0].float() == 0).all())
+    assert bool((y[3] == 0).all()) and torch.isfinite(y[1]).all() and torch.isfinite(q[1].float()).all()
+    assert bool(y[2].isnan().all()) and bool(q[2].float().isnan().all())
+    assert qb.vec_norm(x[:0], w)[0].shape == (0, 256)
+
+
+@pytest.mark.parametrize("t,wt", [(F32, F32), (BF16, BF16), (F16, F32)])
+@pytest.mark.parametrize("n,d", [(1, 1), (1, 128), (5, 100), (300, 96), (33, 129), (700, 256), (45, 500), (600, 513), (6, 1024), (1025, 1500), (5, 2048), (70, 2049),
+                                 (600, 4096), (4, 8000), (3, 16_384), (20_000, 128)])
+def test_norm_grad(qb, n, d, t, wt):
+    h, _ = framed(rnd((n, d), d, t, 2.0))
+    dy, _ = framed(rnd((n, d), d + 1, t, 0.1))
+    dh, _ = framed(rnd((n, d), d + 2, t, 0.1))
+    w = (1 + 0.3 * rnd((d,), d + 3)).to(wt)
+    eps = float(torch.tensor(1e-5, dtype=F32))
+    hd, yd = h.double(), dy.double()
+    r = 1 / torch.sqrt((hd * hd).mean(1, keepdim=True) + eps)
+    u = yd * w.double()
+    dot, size = (u * hd).mean(1, keepdim=True), (u * hd).abs().mean(1, keepdim=True)
+    dwant, dsize = (yd * hd * r).sum(0), (yd * hd * r).abs().sum(0)
+    for past in (None, dh):
+        want = r * u - hd * r ** 3 * dot + (0 if past is None else past.double())
+        mag = (r * u).abs() + hd.abs() * r ** 3 * size + (0 if past is None else past.double().abs())
+        dx, dw = qb.vec_norm_grad(dy, h, w, dh=past, eps=eps)
+        # r to the third has three times the root's error, the dot product its own 74 additions
+        close(dx, want, (3 * NORM_U + 80 * U) * mag + half_step(want, t))
+        close(dw, dwant, (NORM_U + (n + 3) * U) * dsize)
+        again = qb.vec_norm_grad(dy, h, w, dh=past, eps=eps)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+    # in place: over dh, over dy; a view as output
+    a, st = framed(dh.clone())
+    was = st.clone()
+    qb.vec_norm_grad(dy, h, w, dh=a, eps=eps, out=(a, dw))
+    assert torch.equal(a, dx) and untouched(a, st, was)
+    b, st = framed(dy.clone())
+    qb.vec_norm_grad(b, h, w, dh=dh, eps=eps, out=(b, dw))
+    assert torch.equal(b, dx)
+
+
+def test_norm_grad_against_differences(qb):
+    """The formula in 64 bits against central differences of the norm in 64 bits."""
+    n, d, eps = 3, 40, 1e-5
+    g = torch.Generator().manual_seed(0)
+    x, w, dy = (torch.randn(s, generator=g, dtype=torch.float64) for s in ((n, d), (d,), (n, d)))
+
+    def loss(x, w):
+        return (x / torch.sqrt((x * x).mean(1, keepdim=True) + eps) * w * dy).sum()
+
+    dx, dw = qb.vec_norm_grad(*(v.float().to(dev()) for v in (dy, x, w)), eps=eps)
+    x, w, dy = (v.float().double() for v in (x, w, dy))
+    e = 1e-5  # differences are off by about e^2 / 6 third derivatives and 2^-53 |loss| / e: 1e-9 of values near 1
+    for v, got in ((x, dx), (w, dw)):
+        for at in range(0, v.numel(), 7):
+            step = torch.zeros_like(v).view(-1)
+            step[at] = e
+            step = step.view(v.shape)
+            diff = (loss(x + step, w) - loss(x - step, w)) / (2 * e) if v is x else (loss(x, w + step) - loss(x, w - step)) / (2 * e)
+            assert abs(float(got.view(-1)[at]) - float(diff)) <= 1e-7 + 300 * U * float(dy.abs().max() * w.abs().max() * 4)
+
+
+def test_norm_grad_of_nothing(qb):
+    dx, dw = qb.vec_norm_grad(torch.empty((0, 40), device=dev()), torch.empty((0, 40), device=dev()), torch.ones(40, device=dev()))
+    assert dx.shape == (0, 40) and bool((dw == 0).all())
+
+
+# ---------------------------------------------------------------- product --
+def factor(n, k, seed, qt, st, whole=False):
+    """8-bit values and scales; `whole`: small whole numbers and powers near one, so that every sum is exact."""
+    g = torch.Generator().manual_seed(seed)
+    nb = -(-k // 128)
+    if whole:
+        q = torch.randint(-3, 4, (n, k), generator=g).float().to(qt)
+        p = torch.randint(-1, 2, (n, nb), generator=g).float()
+        s = torch.exp2(p)
+    else:
+        q = (torch.randn((n, k), generator=g) * 60).clamp(-440, 440).to(qt)
+        s = torch.exp(torch.randn((n, nb), generator=g))
+        if st == E8M0:
+            s = torch.exp2(torch.round(torch.log2(s)))
+    return q.to(dev()), s.to(st).to(dev())
+
+
+def product64(a, sa, b, sb):
+    k = a.shape[1]
+    x, y = (v.double() * s.double().repeat_interleave(128, 1)[:, :k] for v, s in ((a, sa), (b, sb)))
+    return x @ y.t().contiguous(), x.abs() @ y.abs().t().contiguous()
+
+
+def check_product(qb, m, n, k, ta, tb, st, to, frame=False, aligned=True):
+    for whole in (True, False):
+        (a, sa), (b, sb) = factor(m, k, m + k, ta, st, whole), factor(n, k, n + k + 1, tb, st, whole)
+        if frame:  # rows that lie apart, what is between them NaN
+            pad = (-k - 16) % 16 if aligned else 0
+            a, _ = framed(a, 16 if aligned else 3, pad if aligned else 4)
+            b, _ = framed(b, 16 if aligned else 1, pad if aligned else 7)
+            sa, _ = framed(sa, 1, 3)
+            sb, _ = framed(sb, 2, 2)
+        want, size = product64(a, sa, b, sb)
+        got = qb.vec_matmul_blocks(a, sa, b, sb, dtype=to)
+        if whole:
+            assert float(size.max() if k else 0) < 2 ** 22
+            assert torch.equal(got, want.to(F32).to(to)), (m, n, k)
+        # k additions that may cut off instead of rounding, three more operations per block with F32 scales
+        close(got, want, (2 * k + 8) * U * size + half_step(want, to))
+        out, store = framed(torch.zeros((m, n), dtype=to, device=dev()), 1, 2)
+        was = store.clone()
+        qb.vec_matmul_blocks(a, sa, b, sb, out=out)
+        assert torch.equal(out, got) and untouched(out, store, was)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 16, 128), (2, 17, 100), (16, 100, 256), (17, 33, 129), (33, 513, 1000), (64, 40, 127), (1, 4096, 2048), (5, 3, 3000),
+                                   (65, 1, 16), (65, 130, 128), (100, 127, 640), (129, 128, 96), (128, 257, 15), (300, 200, 1024), (255, 385, 1041), (130, 200, 8200),
+                                   (66, 64, 31), (200, 1000, 300), (3, 5, 0), (70, 90, 0)])
+@pytest.mark.parametrize("st,to", [(E8M0, BF16), (F32, F32)])
+def test_matmul(qb, m, n, k, st, to):
+    check_product(qb, m, n, k, E4M3, E4M3, st, to)
+
+
+@pytest.mark.parametrize("ta,tb", [(E4M3, E5M2), (E5M2, E4M3), (E5M2, E5M2)])
+@pytest.mark.parametrize("m,n,k,st,to", [(9, 70, 300, E8M0, F16), (150, 140, 400, E8M0, F32), (20, 90, 500, F32, BF16), (200, 140, 2000, F32, F32)])
+def test_matmul_types(qb, ta, tb, m, n, k, st, to):
+    check_product(qb, m, n, k, ta, tb, st, to)
+
+
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("m,n,k", [(1, 50, 97), (20, 33, 256), (60, 70, 400), (100, 140, 128), (140, 150, 200), (260, 140, 1300), (140, 130, 5000)])
+@pytest.mark.parametrize("st", [E8M0, F32])
+def test_matmul_of_views(qb, m, n, k, st, aligned):
+    check_product(qb, m, n, k, E4M3, E4M3, st, F32, frame=True, aligned=aligned)
+
+
+@pytest.mark.parametrize("st", [E8M0, F32])
+@pytest.mark.parametrize("m,n,k", [(3600, 3700, 300), (3590, 3841, 1024), (257, 50_000, 96), (3600, 3700, 129)])
+def test_matmul_of_many_tiles(qb, m, n, k, st):
+    check_product(qb, m, n, k, E4M3, E4M3, st, BF16 if k > 300 else F32)
+    check_product(qb, m, n, k, E5M2, E4M3, st, F16, frame=True, aligned=k % 2 == 0)
+
+
+def test_matmul_scales_at_the_ends(qb):
+    """Powers far from one (their product within float32), and NaN as a scale or a value: it stays in its row."""
+    a, b = torch.ones((70, 256), device=dev()).to(E4M3), torch.ones((90, 256), device=dev()).to(E4M3)
+    sa, sb = torch.full((70, 2), 2.0 ** -120, device=dev()).to(E8M0), torch.full((90, 2), 2.0 ** 100, device=dev()).to(E8M0)
+    for rows in (5, 70):
+        got = qb.vec_matmul_blocks(a[:rows], sa[:rows], b, sb, dtype=F32)
+        assert bool((got == 256 * 2.0 ** -20).all())
+    a.view(torch.uint8)[3, 200] = 0x7F
+    sb.view(torch.uint8)[8, 1] = 255
+    for rows in (5, 70):
+        got = qb.vec_matmul_blocks(a[:rows], sa[:rows], b, sb, dtype=F32)
+        bad = torch.zeros((rows, 90), dtype=torch.bool, device=dev())
+        bad[3], bad[:, 8] = True, True
+        assert torch.equal(got.isnan(), bad)
+
+
+def test_matmul_beyond_32_bits(qb):
+    """Bytes past 2^32 of a factor, elements past 2^31 of the result."""
+    n, k = 4_300_000, 1024
+    b = torch.zeros((n, k), dtype=torch.uint8, device=dev())
+    at = [0, 1, 2_097_152, 4_194_303, 4_194_304, n - 1]
+    bits = factor(len(at), k, 5, E4M3, E8M0, True)[0].view(torch.uint8)
+    for i, r in enumerate(at):
+        b[r] = bits[i]
+    b = b.view(E4M3)
+    sb = torch.ones((n, 8), device=dev()).to(E8M0)
+    for m in (3, 600):
+        a, sa = factor(m, k, 6, E4M3, E8M0, True)
+        want, _ = product64(a, sa, bits.view(E4M3), sb[:len(at)])
+        got = qb.vec_matmul_blocks(a, sa, b, sb)
+        assert torch.equal(got[:, at], want.to(F32).to(BF16)) and bool((got[:, 2_000_000:2_000_100] == 0).all())
+        del got
+
+
+# ------------------------------------------------ gradients of a layer, paths --
+def test_layer_gradients(qb):
+    """y = x W^T in 8 bits and both its gradients, each against 64 bits on the same 8-bit factors, and against the gradients without
+    8 bits within what their roundings (2^-4 and 2^-3 of a value at most, independent) explain."""
+    n, din, dout = 700, 260, 390
+    x, w, dy = rnd((n, din), 1, BF16), rnd((dout, din), 2, BF16, 0.1), rnd((n, dout), 3, BF16, 0.01)
+    for a, b, ta, plain in (((x, False), (w, False), E4M3, x.double() @ w.double().t()), ((dy, False), (w, True), E5M2, dy.double() @ w.double()),
+                            ((dy, True), (x, True), E5M2, dy.double().t() @ x.double())):
+        qa, sa = qb.vec_quantize_blocks(a[0], dtype=ta, transposed=a[1])
+        q2, s2 = qb.vec_quantize_blocks(b[0], transposed=b[1])
+        got = qb.vec_matmul_blocks(qa, sa, q2, s2, dtype=F32)
+        want, size = product64(qa, sa, q2, s2)
+        close(got, want, (2 * qa.shape[1] + 8) * U * size)
+        left, right = (v[0].double().t() if v[1] else v[0].double() for v in (a, b))
+        bound = left.abs() @ right.abs().t().contiguous() * (2.0 ** -4 + (2.0 ** -3 if ta == E5M2 else 2.0 ** -4) + 2.0 ** -7)
+        assert bool(((got.double() - plain).abs() <= bound + 1e-6).all())
+
+
+def chain(qb, ids, table, w, r, qw, sw, dy):
+    x = qb.vec_lookup(table, ids, scale=2.0)
+    y, h, q, s = qb.vec_norm(x, w, residual=r, quant=E4M3)
+    z = qb.vec_matmul_blocks(q, s, qw, sw, dtype=F32)
+    qy, sy = qb.vec_quantize_blocks(dy, dtype=E5M2, transposed=True)
+    qx, sx = qb.vec_quantize_blocks(y, scale_dtype=E8M0, transposed=True)
+    gw = qb.vec_matmul_blocks(qy, sy, qx, sx, dtype=F32)
+    dx, dw = qb.vec_norm_grad(y, h, w, dh=h)
+    gt = qb.vec_lookup_grad(dx, ids, table.shape[0], scale=2.0, dtype=F32)
+    return x, y, h, q.view(torch.uint8), s.view(torch.uint8), z, gw, dx, dw, gt
+
+
+@pytest.mark.parametrize("n", [50, 6000])
+def test_streams_and_graph(qb, n):
+    """The same bits on another stream, given or current, and from a graph replayed over changing inputs."""
+    rows, d, dout = 3000, 320, 192
+    table, w, r, dy = rnd((rows, d), 1, BF16), rnd((d,), 2, BF16), rnd((n, d), 3, BF16), rnd((n, dout), 4, BF16)
+    qw, sw = qb.vec_quantize_blocks(rnd((dout, d), 5, BF16))
+    sets = [torch.randint(-1, rows, (n,), generator=torch.Generator().manual_seed(s)).to(dev()) for s in range(3)]
+    ids = sets[0].clone()
+    args = (ids, table, w, r, qw, sw, dy)
+    want = []
+    for s in sets:
+        ids.copy_(s)
+        want.append([t.clone() for t in chain(qb, *args)])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = chain(qb, *args)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want[2]))
+    x = qb.vec_lookup(table, ids, scale=2.0, stream=side)
+    gt = qb.vec_lookup_grad(x, ids, rows, stream=side)
+    side.synchronize()
+    assert torch.equal(x, want[2][0]) and torch.equal(gt, qb.vec_lookup_grad(x, ids, rows))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        held = chain(qb, *args)
+    for i in (0, 1, 2, 1, 0):
+        ids.copy_(sets[i])
+        eager = chain(qb, *args)
+        torch.cuda.synchronize()
+        for t in held:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want[i])) and all(torch.equal(a, b) for a, b in zip(eager, want[i]))
+
+
+def test_binding_refuses(qb):
+    x = rnd((8, 256), 1, BF16)
+    w = rnd((256,), 2, BF16)
+    q, s = qb.vec_quantize_blocks(x)
+    ids = torch.zeros(8, dtype=torch.int64, device=dev())
+    for call, text in (
+            (lambda: qb.vec_lookup(x.t(), ids), "apart"), (lambda: qb.vec_lookup(x, ids.float()), "ids"), (lambda: qb.vec_lookup(x, ids.cpu()), "cpu"),
+            (lambda: qb.vec_lookup(x, ids[::2]), "ids"), (lambda: qb.vec_lookup(x, ids, out=x[:3]), "shape"), (lambda: qb.vec_lookup(x[:1].expand(8, 256), ids), "0 apart"),
+            (lambda: qb.vec_lookup(x.double(), ids), "float64"), (lambda: qb.vec_lookup(x, ids, dtype=F32, out=torch.empty_like(x)), "not"),
+            (lambda: qb.vec_lookup_grad(x, ids[:7], 5), "shape"), (lambda: qb.vec_lookup_grad(x, ids, 5, accumulate=True), "accumulate"),
+            (lambda: qb.vec_lookup_grad(x[:1].expand(8, 256), ids, 5), "0 apart"),
+            (lambda: qb.vec_norm(x, w[:255]), "weight"), (lambda: qb.vec_norm(x, w, residual=x.float()), "residual"), (lambda: qb.vec_norm(x, w, quant=BF16), "8-bit"),
+            (lambda: qb.vec_norm(x, w, want_y=False), "neither"), (lambda: qb.vec_norm(x, w, quant=E4M3, scale_dtype=BF16), "scales"),
+            (lambda: qb.vec_norm_grad(x, x[:7], w), "shape"), (lambda: qb.vec_norm_grad(x, x, w, out=(x, w)), "dweight"),
+            (lambda: qb.vec_quantize_blocks(x, dtype=torch.int8), "8-bit"), (lambda: qb.vec_quantize_blocks(q), "type"),
+            (lambda: qb.vec_matmul_blocks(q, s, q[:, :100], s), "shape"), (lambda: qb.vec_matmul_blocks(q, s, q, s.float()), "b_scales"),
+            (lambda: qb.vec_matmul_blocks(x, s, q, s), "types"), (lambda: qb.vec_matmul_blocks(q, s[:, :1], q, s), "shape")):
+        with pytest.raises(qb.QadcError) as e:
+            call()
+        assert e.value.code == qb.PQ_EINVAL and text in str(e.value), str(e.value)
