@@ -476,90 +476,112 @@ _VEC_TYPE = {torch.float32: VEC_F32, torch.bfloat16: VEC_BF16, torch.float16: VE
              torch.float8_e5m2: VEC_E5M2, torch.float8_e8m0fnu: VEC_E8M0}
 
 
-def _refuse(cond: bool, msg: str) -> None:
-    if cond:
-        raise QadcError(PQ_EINVAL, msg)
-
-
-def _vec_type(what: str, dtype) -> int:
-    t = _VEC_TYPE.get(dtype)
-    _refuse(t is None, f"{what}: no operator takes {dtype}")
-    return t
+def _refuse(name: str, msg: str):
+    raise QadcError(PQ_EINVAL, f"{name}: {msg}")
 
 
 class _Call:
-    """The device and the stream of a call, for its checks, allocations and launch."""
+    """The device and the stream of a call, for its checks, allocations and launch.  (A call of a few microseconds on the GPU waits
+    for what is done here, so messages are only put together for a refusal, and outputs made here are not looked over.)"""
+    __slots__ = ("name", "device", "index", "stream", "raw")
 
     def __init__(self, name: str, first: torch.Tensor, stream):
-        _refuse(not first.is_cuda, f"{name}: tensors of the GPU, got {first.device}")
-        self.name, self.device = name, first.device
-        current = torch.cuda.current_stream(first.device)
-        self.stream = current if stream is None else stream
-        _refuse(self.stream.device != self.device, f"{name}: a stream of {self.stream.device} for tensors of {self.device}")
-        self.elsewhere = self.stream != current or self.device.index != torch.cuda.current_device()
+        if not first.is_cuda:
+            _refuse(name, f"tensors of the GPU, got {first.device}")
+        self.name, self.index, self.stream = name, first.get_device(), None
+        if stream is not None and stream.device.index != self.index:
+            _refuse(name, f"a stream of {stream.device} for tensors of {first.device}")
+        self.raw = torch._C._cuda_getCurrentRawStream(self.index)
+        self.device = first.device
+        if (stream is not None and stream.cuda_stream != self.raw) or torch.cuda.current_device() != self.index:
+            self.stream = stream if stream is not None else torch.cuda.current_stream(self.index)  # (entered around allocations and the launch)
+            self.raw = self.stream.cuda_stream
 
     def empty(self, shape, dtype) -> torch.Tensor:
-        if self.elsewhere:
+        if self.stream is not None:
             with torch.cuda.stream(self.stream):
                 return torch.empty(shape, dtype=dtype, device=self.device)
         return torch.empty(shape, dtype=dtype, device=self.device)
 
-    def rows(self, what: str, t: Optional[torch.Tensor], shape=None, dtype=None):
-        """(pointer, distance of rows) of a matrix, checked; (None, 0) without one."""
-        if t is None:
-            return None, 0
-        _refuse(t.device != self.device, f"{self.name}: {what} is on {t.device}, not {self.device}")
-        _refuse(t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)),
-                f"{self.name}: {what} of shape {tuple(t.shape)}" + (f", not {tuple(shape)}" if shape is not None else ""))
-        _refuse(dtype is not None and t.dtype != dtype, f"{self.name}: {what} is {t.dtype}, not {dtype}")
+    def rows(self, what: str, t: torch.Tensor, n: int, d: int, dtype):
+        """Address of a matrix [n, d] and the distance of its rows, checked."""
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 2 and shape[0] == n and shape[1] == d and t.dtype == dtype and t.get_device() == self.index:
+            ld = stride[0] if n > 1 else (d or 1)
+            if ld >= d and (stride[1] == 1 or d <= 1):
+                return t.data_ptr(), ld or 1
+            _refuse(self.name, f"{what}'s rows of {d} are {ld} apart, the values of a row {stride[1]}")
+        if t.get_device() != self.index:
+            _refuse(self.name, f"{what} is on {t.device}, not {self.device}")
+        if t.dtype != dtype:
+            _refuse(self.name, f"{what} is {t.dtype}, not {dtype}")
+        _refuse(self.name, f"{what} of shape {tuple(shape)}, not {(n, d)}")
+
+    def first_rows(self, what: str, t: torch.Tensor):
+        if t.dim() != 2:
+            _refuse(self.name, f"{what} of shape {tuple(t.shape)}, not a matrix")
         n, d = t.shape
-        _refuse(d > 1 and t.stride(1) != 1, f"{self.name}: {what}'s values of a row are {t.stride(1)} apart")
-        ld = t.stride(0) if n > 1 else max(d, 1)
-        _refuse(ld < d, f"{self.name}: {what}'s rows of {d} are {ld} apart")
-        return t.data_ptr(), max(ld, 1)
+        return (n, d, *self.rows(what, t, n, d, t.dtype))
 
     def vector(self, what: str, t: torch.Tensor, n: Optional[int] = None, dtype=None) -> int:
-        _refuse(t.device != self.device, f"{self.name}: {what} is on {t.device}, not {self.device}")
-        _refuse(not t.is_contiguous() or (n is not None and (t.dim() != 1 or t.numel() != n)),
-                f"{self.name}: {what} of shape {tuple(t.shape)}, strides {t.stride()}")
-        _refuse(dtype is not None and t.dtype != dtype, f"{self.name}: {what} is {t.dtype}, not {dtype}")
+        if t.get_device() != self.index or (dtype is not None and t.dtype != dtype) or not t.is_contiguous() or (
+                n is not None and (t.dim() != 1 or t.numel() != n)):
+            _refuse(self.name, f"{what}: {t.dtype} of shape {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         return t.data_ptr()
 
     def workspace(self, t: Optional[torch.Tensor], nbytes: int):
-        """(pointer, bytes); the tensor too, to be kept until the launch."""
+        """Address, bytes, and the tensor, to be kept until the launch."""
         if t is None:
-            t = self.empty(nbytes, torch.uint8) if nbytes else None
-        if t is None:
-            return None, 0, None
+            if nbytes == 0:
+                return None, 0, None
+            t = self.empty(nbytes, torch.uint8)
+            return t.data_ptr(), nbytes, t
         return self.vector("workspace", t), t.numel() * t.element_size(), t
 
+    def type(self, what: str, dtype) -> int:
+        t = _VEC_TYPE.get(dtype)
+        if t is None:
+            _refuse(self.name, f"{what}: no operator takes {dtype}")
+        return t
+
     def ids(self, t: torch.Tensor):
-        _refuse(t.dtype not in (torch.int32, torch.int64), f"{self.name}: ids are int32 or int64, got {t.dtype}")
+        if t.dtype != torch.int64 and t.dtype != torch.int32:
+            _refuse(self.name, f"ids are int32 or int64, got {t.dtype}")
         return self.vector("ids", t), t.element_size()
 
+    def out_type(self, out: Optional[torch.Tensor], dtype, default):
+        """The type of a result that may be given, named, or left to the default."""
+        if out is None:
+            return dtype or default
+        if dtype is not None and out.dtype != dtype:
+            _refuse(self.name, f"out is {out.dtype}, not {dtype}")
+        return out.dtype
+
     def launch(self, fn, *args) -> None:
-        if self.elsewhere:
-            with torch.cuda.device(self.device):
-                _check(fn(*args, self.stream.cuda_stream or None))
+        if self.stream is None:
+            rc = fn(*args, self.raw)
         else:
-            _check(fn(*args, self.stream.cuda_stream or None))
+            with torch.cuda.device(self.index):
+                rc = fn(*args, self.raw)
+        if rc != PQ_OK:
+            _check(rc)
 
 
 def vec_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype: Optional[torch.dtype] = None,
                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """scale * table[ids] as [*ids.shape, d]; zeros where an id is outside the table (a search pads with -1)."""
     call = _Call("vec_lookup", table, stream)
-    ptr, ld = call.rows("table", table)
+    rows, d, ptr, ld = call.first_rows("table", table)
     idp, id_bytes = call.ids(ids)
-    n, (rows, d) = ids.numel(), table.shape
-    _refuse(out is not None and dtype is not None and out.dtype != dtype, f"vec_lookup: out is {None if out is None else out.dtype}, not {dtype}")
+    n = ids.numel()
+    to = call.out_type(out, dtype, table.dtype)
     if out is None:
-        out = call.empty((*ids.shape, d), dtype or table.dtype)
+        out = call.empty((*ids.shape, d), to)
         optr, old = out.data_ptr(), d
     else:
-        optr, old = call.rows("out", out, (n, d))
-    call.launch(load().vec_lookup, ptr, rows, d, ld, _vec_type("table", table.dtype), idp, id_bytes, n, scale, optr, old,
-                _vec_type("out", out.dtype))
+        optr, old = call.rows("out", out, n, d, to)
+    call.launch((_lib or load()).vec_lookup, ptr, rows, d, ld, call.type("table", table.dtype), idp, id_bytes, n, scale, optr, old,
+                call.type("out", to))
     return out
 
 
@@ -574,36 +596,40 @@ def vec_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: flo
     is added to `out`."""
     call = _Call("vec_lookup_grad", grad, stream)
     if grad.dim() != 2:
-        _refuse(not grad.is_contiguous() or grad.dim() == 0, "vec_lookup_grad: grad of other than two dimensions is contiguous")
+        if not grad.is_contiguous() or grad.dim() == 0:
+            _refuse(call.name, "grad of other than two dimensions is contiguous")
         grad = grad.view(-1, grad.shape[-1])
-    d = grad.shape[1]
-    ptr, ld = call.rows("grad", grad, (ids.numel(), d))
+    n, d = ids.numel(), grad.shape[1]
+    ptr, ld = call.rows("grad", grad, n, d, grad.dtype)
     idp, id_bytes = call.ids(ids)
-    _refuse(accumulate and out is None, "vec_lookup_grad: accumulate needs an out to add to")
-    _refuse(out is not None and dtype is not None and out.dtype != dtype, f"vec_lookup_grad: out is {None if out is None else out.dtype}, not {dtype}")
+    if accumulate and out is None:
+        _refuse(call.name, "accumulate needs an out to add to")
+    to = call.out_type(out, dtype, grad.dtype)
     if out is None:
-        out = call.empty((rows, d), dtype or grad.dtype)
-    optr, old = call.rows("out", out, (rows, d))
-    lib = load()
-    wptr, wbytes, keep = call.workspace(workspace, int(lib.vec_lookup_grad_workspace_bytes(ids.numel(), rows, d)))
-    call.launch(lib.vec_lookup_grad, ptr, ids.numel(), d, ld, _vec_type("grad", grad.dtype), idp, id_bytes, scale, int(accumulate),
-                optr, rows, old, _vec_type("out", out.dtype), wptr, wbytes)
+        out = call.empty((rows, d), to)
+        optr, old = out.data_ptr(), d
+    else:
+        optr, old = call.rows("out", out, rows, d, to)
+    lib = _lib or load()
+    wptr, wbytes, keep = call.workspace(workspace, lib.vec_lookup_grad_workspace_bytes(n, rows, d))
+    call.launch(lib.vec_lookup_grad, ptr, n, d, ld, call.type("grad", grad.dtype), idp, id_bytes, scale, int(accumulate), optr, rows,
+                old, call.type("out", to), wptr, wbytes)
     return out
 
 
 def _blocks_out(call: _Call, n: int, d: int, quant, scale_dtype, out):
-    """8-bit values and scales: those given, or new ones whose rows start at multiples of 16 bytes."""
-    _refuse(scale_dtype not in (torch.float8_e8m0fnu, torch.float32), f"{call.name}: scales of {scale_dtype}")
-    _refuse(quant not in (torch.float8_e4m3fn, torch.float8_e5m2), f"{call.name}: 8-bit values of {quant}")
+    """8-bit values and scales with their addresses and distances: those given, or new ones whose rows start at multiples of 16 bytes."""
+    if scale_dtype != torch.float8_e8m0fnu and scale_dtype != torch.float32:
+        _refuse(call.name, f"scales of {scale_dtype}")
+    if quant != torch.float8_e4m3fn and quant != torch.float8_e5m2:
+        _refuse(call.name, f"8-bit values of {quant}")
     nb = -(-d // VEC_BLOCK)
     if out is not None:
         q, scales = out
-    else:
-        q = call.empty((n, -(-d // 16) * 16), quant)
-        if q.shape[1] != d:
-            q = q[:, :d]
-        scales = call.empty((n, nb), scale_dtype)
-    return (q, scales, *call.rows("q", q, (n, d), quant), *call.rows("scales", scales, (n, nb), scale_dtype))
+        return (q, scales, *call.rows("q", q, n, d, quant), *call.rows("scales", scales, n, nb, scale_dtype))
+    ld = -(-d // 16) * 16
+    q, scales = call.empty((n, ld), quant), call.empty((n, nb), scale_dtype)
+    return (q if ld == d else q[:, :d]), scales, q.data_ptr(), ld or 1, scales.data_ptr(), nb or 1
 
 
 def vec_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
@@ -613,22 +639,33 @@ def vec_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
     8-bit values and scales of y where `quant` names their type; else None.  `out`: the same four, to be written (h may be x or
     residual)."""
     call = _Call("vec_norm", x, stream)
-    xp, ldx = call.rows("x", x)
-    n, d = x.shape
-    rp, ldr = call.rows("residual", residual, (n, d), x.dtype)
+    n, d, xp, ldx = call.first_rows("x", x)
+    t = x.dtype
+    rp = hp = yp = qp = sp = None
+    ldr = ldh = ldy = ldq = lds = 0
+    if residual is not None:
+        rp, ldr = call.rows("residual", residual, n, d, t)
     wp = call.vector("weight", weight, d)
-    y, h, q, scales = out if out is not None else (None,) * 4
+    y = h = q = scales = None
     if out is None:
-        y = call.empty((n, d), x.dtype) if want_y else None
-        h = call.empty((n, d), x.dtype) if residual is not None else None
-    yp, ldy = call.rows("y", y, (n, d), x.dtype)
-    hp, ldh = call.rows("h", h, (n, d), x.dtype)
-    qp, ldq, sp, lds = None, 0, None, 0
-    if quant is not None or q is not None:
+        if want_y:
+            y = call.empty((n, d), t)
+            yp, ldy = y.data_ptr(), d
+        if residual is not None:
+            h = call.empty((n, d), t)
+            hp, ldh = h.data_ptr(), d
+        if quant is not None:
+            q, scales, qp, ldq, sp, lds = _blocks_out(call, n, d, quant, scale_dtype, None)
+    else:
+        y, h, q, scales = out
+        if y is not None:
+            yp, ldy = call.rows("y", y, n, d, t)
+        if h is not None:
+            hp, ldh = call.rows("h", h, n, d, t)
         if q is not None:
             quant, scale_dtype = q.dtype, scales.dtype
-        q, scales, qp, ldq, sp, lds = _blocks_out(call, n, d, quant, scale_dtype, None if q is None else (q, scales))
-    call.launch(load().vec_norm, xp, ldx, rp, ldr, _vec_type("x", x.dtype), wp, _vec_type("weight", weight.dtype), n, d, eps, hp, ldh,
+            q, scales, qp, ldq, sp, lds = _blocks_out(call, n, d, quant, scale_dtype, (q, scales))
+    call.launch((_lib or load()).vec_norm, xp, ldx, rp, ldr, call.type("x", t), wp, call.type("weight", weight.dtype), n, d, eps, hp, ldh,
                 yp, ldy, qp, ldq, _VEC_TYPE.get(quant, VEC_E4M3), sp, lds, _VEC_TYPE.get(scale_dtype, VEC_E8M0))
     return y, h, q, scales
 
@@ -642,18 +679,22 @@ def vec_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, dh: O
     """(dx, dweight) of vec_norm: h is its second result (x without a residual), dh the gradient that reaches h past the norm.
     `out`: the same two, to be written (dx may be dy or dh; dweight is float32)."""
     call = _Call("vec_norm_grad", dy, stream)
-    yp, ldy = call.rows("dy", dy)
-    n, d = dy.shape
-    hp, ldh = call.rows("h", h, (n, d), dy.dtype)
-    ep, lde = call.rows("dh", dh, (n, d), dy.dtype)
+    n, d, yp, ldy = call.first_rows("dy", dy)
+    t = dy.dtype
+    hp, ldh = call.rows("h", h, n, d, t)
+    ep, lde = call.rows("dh", dh, n, d, t) if dh is not None else (None, 0)
     wp = call.vector("weight", weight, d)
-    dx, dweight = out if out is not None else (call.empty((n, d), dy.dtype), call.empty((d,), torch.float32))
-    xp, ldx = call.rows("dx", dx, (n, d), dy.dtype)
-    dwp = call.vector("dweight", dweight, d, torch.float32)
-    lib = load()
-    wsp, wbytes, keep = call.workspace(workspace, int(lib.vec_norm_grad_workspace_bytes(n, d)))
-    call.launch(lib.vec_norm_grad, yp, ldy, hp, ldh, ep, lde, _vec_type("dy", dy.dtype), wp, _vec_type("weight", weight.dtype), n, d, eps,
-                xp, ldx, dwp, wsp, wbytes)
+    if out is None:
+        dx, dweight = call.empty((n, d), t), call.empty((d,), torch.float32)
+        xp, ldx, dwp = dx.data_ptr(), d, dweight.data_ptr()
+    else:
+        dx, dweight = out
+        xp, ldx = call.rows("dx", dx, n, d, t)
+        dwp = call.vector("dweight", dweight, d, torch.float32)
+    lib = _lib or load()
+    wsp, wbytes, keep = call.workspace(workspace, lib.vec_norm_grad_workspace_bytes(n, d))
+    call.launch(lib.vec_norm_grad, yp, ldy, hp, ldh, ep, lde, call.type("dy", t), wp, call.type("weight", weight.dtype), n, d, eps, xp, ldx,
+                dwp, wsp, wbytes)
     return dx, dweight
 
 
@@ -661,11 +702,10 @@ def vec_quantize_blocks(x: torch.Tensor, dtype: torch.dtype = torch.float8_e4m3f
                         transposed: bool = False, out=None, stream=None):
     """(q, scales): x in 8 bits with a scale for each 128 values of a row, or, transposed, of a column (q is then x's transpose)."""
     call = _Call("vec_quantize_blocks", x, stream)
-    xp, ldx = call.rows("x", x)
-    n, d = x.shape
-    q, scales, qp, ldq, sp, lds = _blocks_out(call, *((d, n) if transposed else (n, d)), dtype, scale_dtype, out)
-    call.launch(load().vec_quantize_blocks, xp, ldx, _vec_type("x", x.dtype), n, d, int(transposed), qp, ldq, _VEC_TYPE[dtype], sp, lds,
-                _VEC_TYPE[scale_dtype])
+    n, d, xp, ldx = call.first_rows("x", x)
+    q, scales, qp, ldq, sp, lds = _blocks_out(call, d if transposed else n, n if transposed else d, dtype, scale_dtype, out)
+    call.launch((_lib or load()).vec_quantize_blocks, xp, ldx, call.type("x", x.dtype), n, d, int(transposed), qp, ldq, _VEC_TYPE[dtype], sp,
+                lds, _VEC_TYPE[scale_dtype])
     return q, scales
 
 
@@ -678,19 +718,19 @@ def vec_matmul_blocks(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, 
                       stream=None) -> torch.Tensor:
     """a b^T of 8-bit matrices [m, k] and [n, k] with their scales [m or n, ceil(k / 128)]; bfloat16 unless `dtype` or `out` says else."""
     call = _Call("vec_matmul_blocks", a, stream)
-    ap, lda = call.rows("a", a)
-    m, k = a.shape
-    n = b.shape[0]
-    nb = -(-k // VEC_BLOCK)
-    bp, ldb = call.rows("b", b, (n, k))
-    asp, ldas = call.rows("a_scales", a_scales, (m, nb))
-    bsp, ldbs = call.rows("b_scales", b_scales, (n, nb), a_scales.dtype)
-    _refuse(out is not None and dtype is not None and out.dtype != dtype, f"vec_matmul_blocks: out is {None if out is None else out.dtype}, not {dtype}")
+    m, k, ap, lda = call.first_rows("a", a)
+    n, nb, st = b.shape[0], -(-k // VEC_BLOCK), a_scales.dtype
+    bp, ldb = call.rows("b", b, n, k, b.dtype)
+    asp, ldas = call.rows("a_scales", a_scales, m, nb, st)
+    bsp, ldbs = call.rows("b_scales", b_scales, n, nb, st)
+    to = call.out_type(out, dtype, torch.bfloat16)
     if out is None:
-        out = call.empty((m, n), dtype or torch.bfloat16)
-    cp, ldc = call.rows("out", out, (m, n))
-    lib = load()
-    wptr, wbytes, keep = call.workspace(workspace, int(lib.vec_matmul_blocks_workspace_bytes(m, n, k)))
-    call.launch(lib.vec_matmul_blocks, ap, lda, _vec_type("a", a.dtype), asp, ldas, bp, ldb, _vec_type("b", b.dtype), bsp, ldbs,
-                _vec_type("scales", a_scales.dtype), m, n, k, cp, ldc, _vec_type("out", out.dtype), wptr, wbytes)
+        out = call.empty((m, n), to)
+        cp, ldc = out.data_ptr(), n or 1
+    else:
+        cp, ldc = call.rows("out", out, m, n, to)
+    lib = _lib or load()
+    wptr, wbytes, keep = call.workspace(workspace, lib.vec_matmul_blocks_workspace_bytes(m, n, k))
+    call.launch(lib.vec_matmul_blocks, ap, lda, call.type("a", a.dtype), asp, ldas, bp, ldb, call.type("b", b.dtype), bsp, ldbs,
+                call.type("scales", st), m, n, k, cp, ldc, call.type("out", to), wptr, wbytes)
     return out

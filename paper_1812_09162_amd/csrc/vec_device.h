@@ -12,49 +12,42 @@ typedef float vec_f8 __attribute__((ext_vector_type(8)));
 typedef int vec_i4 __attribute__((ext_vector_type(4)));
 typedef int vec_i8 __attribute__((ext_vector_type(8)));
 
-// Eight elements as they lie in memory.  Global loads and stores work at any byte address here; the types only promise
-// the alignment of one element.
-template <class T>
-struct VecPack;
-template <>
-struct VecPack<float> {
-    typedef float type __attribute__((ext_vector_type(8), aligned(4)));
+// E elements (eight, unless said otherwise) as they lie in memory.  Global loads and stores work at any byte address here; the
+// types only promise the alignment of one element.
+template <class T, int E = 8>
+struct VecPack {
+    typedef T type __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    typedef float wide __attribute__((ext_vector_type(E)));
 };
-template <>
-struct VecPack<__bf16> {
-    typedef __bf16 type __attribute__((ext_vector_type(8), aligned(2)));
-};
-template <>
-struct VecPack<_Float16> {
-    typedef _Float16 type __attribute__((ext_vector_type(8), aligned(2)));
-};
-
-template <class T>
-using vec_pack = typename VecPack<T>::type;
+template <class T, int E = 8>
+using vec_pack = typename VecPack<T, E>::type;
+template <int E>
+using vec_f = typename VecPack<float, E>::wide;
 
 // left: elements of the row from p on (those beyond it read as zero and are not touched)
-template <class T>
-__device__ __forceinline__ vec_pack<T> vec_load(const T *p, int64_t left) {
-    if (left >= 8) return *(const vec_pack<T> *)p;
-    vec_pack<T> v = (vec_pack<T>)(T)0.0f;
+template <class T, int E = 8>
+__device__ __forceinline__ vec_pack<T, E> vec_load(const T *p, int64_t left) {
+    if (left >= E) return *(const vec_pack<T, E> *)p;
+    vec_pack<T, E> v = (vec_pack<T, E>)(T)0.0f;
 #pragma unroll
-    for (int i = 0; i < 7; ++i)
+    for (int i = 0; i < E - 1; ++i)
         if (i < left) v[i] = p[i];
     return v;
 }
-template <class T>
-__device__ __forceinline__ vec_f8 vec_wide(vec_pack<T> v) {
-    return __builtin_convertvector(v, vec_f8);
+template <class T, int E = 8>
+__device__ __forceinline__ vec_f<E> vec_wide(vec_pack<T, E> v) {
+    return __builtin_convertvector(v, vec_f<E>);
 }
-template <class T>
-__device__ __forceinline__ void vec_store(T *p, int64_t left, vec_f8 f) {
-    const vec_pack<T> v = __builtin_convertvector(f, vec_pack<T>);
-    if (left >= 8) {
-        *(vec_pack<T> *)p = v;
+template <class T, int E = 8>
+__device__ __forceinline__ void vec_store(T *p, int64_t left, vec_f<E> f) {
+    typedef vec_pack<T, E> pack;
+    const pack v = __builtin_convertvector(f, pack);
+    if (left >= E) {
+        *(pack *)p = v;
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 7; ++i)
+    for (int i = 0; i < E - 1; ++i)
         if (i < left) p[i] = v[i];
 }
 // eight bytes

@@ -67,18 +67,35 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 
 // ----------------------------------------------------------------- gradient --
 // table_grad[v] = base + scale * sum of the rows of grad whose id is v.  Positions with the same id are summed in ascending
-// order in float32, so that a result does not depend on which block ran first.
+// order in float32, in pieces that do not depend on which block ran first.
 //
-// Few ids (n <= GRAD_FEW): one launch.  Every block owns a range of table rows, goes through all ids, keeps the positions
-// of its own in order, and writes its rows, zeros or sums.  The ids are read once per block, from the L2 cache.
+// Few ids (n <= GRAD_FEW): one launch.  Every block owns some rows of the table, dealt out in turn since frequent ids are often
+// neighbours; it goes through all ids, keeps the positions of its own in order, and writes its rows, zeros or sums.  The ids
+// are read once per block, from the L2 cache.
 //
 // Many: the positions are sorted by id (a stable radix sort of up to 2^GRAD_BITS buckets a pass), then summed in pieces
 // of GRAD_CHUNK sorted positions, whatever ids they hold, so that a frequent id is no wave's alone; sums of ids that cross
 // a piece's ends are joined by the kernel that also writes the rows without an id.
+//
+// A row is spread over the 64 lanes of a wave, E elements each (2, 4 or 8, the fewest that hold it, else 64 E columns at a time).
 #define GRAD_FEW 4096
 #define GRAD_BITS 10
 #define GRAD_TILE 1024   // keys a block of the sort takes: four per thread
 #define GRAD_CHUNK 64
+
+#define GRAD_WIDTHS(d, ...)          \
+    do {                             \
+        if ((d) <= 128) {            \
+            constexpr int E = 2;     \
+            __VA_ARGS__;             \
+        } else if ((d) <= 256) {     \
+            constexpr int E = 4;     \
+            __VA_ARGS__;             \
+        } else {                     \
+            constexpr int E = 8;     \
+            __VA_ARGS__;             \
+        }                            \
+    } while (0)
 
 struct GradPlan {
     bool few;
@@ -117,98 +134,127 @@ extern "C" size_t vec_lookup_grad_workspace_bytes(int64_t n, int64_t rows, int d
     return n <= 0 || rows <= 0 || d <= 0 || n > 0x7fffffffLL || rows > 0x7ffffffeLL ? 0 : grad_plan(n, rows, d).total;
 }
 
-// Adds the rows of grad at the positions pos(0) .. pos(m - 1), eight columns from col on, in this order to acc.
-template <class TG, class POS>
-__device__ __forceinline__ void grad_sum(const TG *__restrict__ grad, int64_t ld, int64_t col, int64_t left, int m, POS pos, vec_f8 &acc) {
-    int i = 0;
-    for (; i + 8 <= m; i += 8) {
-        vec_pack<TG> v[8];
+template <class TT, int E>
+__device__ __forceinline__ void grad_write(TT *__restrict__ row, int64_t col, int64_t left, vec_f<E> acc, float scale, int accumulate) {
+    if (left <= 0) return;
+    vec_f<E> f;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = vec_load(grad + (int64_t)pos(i + u) * ld + col, left);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) acc += vec_wide<TG>(v[u]);
-    }
-    for (; i < m; ++i) acc += vec_wide<TG>(vec_load(grad + (int64_t)pos(i) * ld + col, left));
+    for (int i = 0; i < E; ++i) f[i] = acc[i] * scale;
+    if (accumulate) f += vec_wide<TT, E>(vec_load<TT, E>(row + col, left));
+    vec_store<TT, E>(row + col, left, f);
 }
 
-template <class TT>
-__device__ __forceinline__ void grad_write(TT *__restrict__ row, int64_t col, int64_t left, vec_f8 acc, float scale, int accumulate) {
-    vec_f8 f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = acc[i] * scale;
-    if (accumulate) f += vec_wide<TT>(vec_load(row + col, left));
-    vec_store(row + col, left, f);
-}
-
-// Zeros in the rows lo .. lo + nrow - 1 whose bit of `has` is not set.
-template <class TT>
-__device__ __forceinline__ void grad_zeros(TT *__restrict__ table, int64_t lo, int nrow, int d, int64_t ld, const uint32_t *has) {
+// Zeros in those of `nrow` rows whose bit of `has` is not set; row(r): address of the r-th.
+template <class TT, class ROW>
+__device__ __forceinline__ void grad_zeros(int nrow, int d, const uint32_t *has, ROW row) {
     const int pieces = (d + 7) / 8;
     int r = threadIdx.x / pieces, c = threadIdx.x - r * pieces;
     const int dr = 256 / pieces, dc = 256 - dr * pieces;
-    for (; r < nrow;) {
-        if (!(has[r >> 5] >> (r & 31) & 1)) vec_store<TT>(table + (lo + r) * ld + c * 8, d - c * 8, (vec_f8)0.0f);
+    while (r < nrow) {
+        if (!(has[r >> 5] >> (r & 31) & 1)) vec_store<TT>(row(r) + c * 8, d - c * 8, (vec_f8)0.0f);
         r += dr;
         c += dc;
         if (c >= pieces) c -= pieces, ++r;
     }
 }
 
-template <class TG, class TT, class ID>
+// Adds to acc the rows of grad at the positions (low 12 bits) of those of list[0 .. m - 1] that are of row r (the bits above), in order.
+template <class TG, int E>
+__device__ __forceinline__ void grad_pick(const TG *__restrict__ grad, int64_t ld, int64_t col, int64_t left, const uint32_t *list, int m,
+                                          uint32_t r, vec_f<E> &acc) {
+    const int lane = threadIdx.x & 63;
+    for (int i0 = 0; i0 < m; i0 += 64) {
+        const uint32_t e = i0 + lane < m ? list[i0 + lane] : 0xffffffffu;
+        uint64_t hits = __ballot(e >> 12 == r);
+        while (hits) {
+            vec_pack<TG, E> v[8];
+            int k = 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int at = hits ? __builtin_ctzll(hits) : 0;
+                const bool more = hits != 0;
+                hits &= hits - 1;
+                const uint32_t pos = __builtin_amdgcn_readlane(e, at) & 4095u;
+                k += more;
+                v[u] = vec_load<TG, E>(grad + (int64_t)pos * ld + col, more ? left : 0);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (u < k) acc += vec_wide<TG, E>(v[u]);
+        }
+    }
+}
+
+// The block's rows: groups of 2^group neighbouring rows are dealt out over 2^deal blocks.
+template <class TG, class TT, class ID, int E>
 __global__ void __launch_bounds__(256)
 k_vec_grad_few(const TG *__restrict__ grad, int n, int d, int64_t ld_grad, const ID *__restrict__ ids, float scale,
-               int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int rpb) {
+               int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int group, int deal, int rpb) {
     extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t *has = (uint32_t *)smem;                      // [(rpb + 31) / 32]
-    uint32_t *list = has + (rpb + 31) / 32;                // [GRAD_FEW] row of the block << 12 | position
-    uint16_t *picked = (uint16_t *)(list + GRAD_FEW);      // [4 waves][GRAD_FEW / 4 ...] see below
+    uint32_t *has = (uint32_t *)smem;           // [(rpb + 31) / 32]
+    uint32_t *list = has + (rpb + 31) / 32;     // [GRAD_FEW] row of the block << 12 | position
     __shared__ int count[4];
-    const int64_t lo = (int64_t)blockIdx.x * rpb;
-    const int nrow = (int)(rows - lo < rpb ? rows - lo : rpb);
+    __shared__ vec_f<E> quarter[4][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    // row r of the block is row of(r) of the table; its rows below `rows` come first
+    auto of = [&](int r) { return ((((int64_t)(r >> group) << deal) + blockIdx.x) << group) + (r & ((1 << group) - 1)); };
+    int nrow = rpb;
+    while (nrow > 0 && of(nrow - 1) >= rows) --nrow;
     for (int i = threadIdx.x; i < (rpb + 31) / 32; i += 256) has[i] = 0;
+    // each wave takes a quarter of the positions, all loads at once, and keeps the block's own, in order, in its quarter of the list
+    const int per = (n + 255) / 256 * 64, from = wave * per;
+    int64_t id[GRAD_FEW / 256];
+#pragma unroll
+    for (int u = 0; u < GRAD_FEW / 256; ++u) {
+        const int i = from + u * 64 + lane;
+        id[u] = u * 64 < per && i < n ? (int64_t)ids[i] : -1;
+    }
     __syncthreads();
-    // each wave takes a quarter of the positions and keeps the block's own, in order, in its quarter of the list
-    const int quarter = (n + 3) / 4;
-    const int from = wave * quarter, to = from + quarter < n ? from + quarter : n;
     int m = 0;
-    for (int i0 = from; i0 < to; i0 += 64) {
-        const int i = i0 + lane;
-        const int64_t id = i < to ? (int64_t)ids[i] : -1;
-        const bool mine = id >= lo && id < lo + nrow;
+#pragma unroll
+    for (int u = 0; u < GRAD_FEW / 256; ++u) {
+        const bool mine = id[u] >= 0 && id[u] < rows && ((id[u] >> group) & ((1 << deal) - 1)) == blockIdx.x;
         const uint64_t b = __ballot(mine);
+        if (!b) continue;
         if (mine) {
-            const int r = (int)(id - lo);
-            list[from + m + __popcll(b & ((1ull << lane) - 1))] = (uint32_t)r << 12 | (uint32_t)i;
+            const int r = (int)(id[u] >> (group + deal) << group) + (int)(id[u] & ((1 << group) - 1));
+            list[from + m + __popcll(b & ((1ull << lane) - 1))] = (uint32_t)r << 12 | (uint32_t)(from + u * 64 + lane);
             atomicOr(&has[r >> 5], 1u << (r & 31));
         }
         m += __popcll(b);
     }
     if (lane == 0) count[wave] = m;
     __syncthreads();
-    if (!accumulate) grad_zeros(table, lo, nrow, d, ld_table, has);
-    // rows with an id: one per wave in turn.  A wave picks the row's positions out of the lists, then sums.
-    uint16_t *mine = picked + wave * GRAD_FEW;
+    if (!accumulate) grad_zeros<TT>(nrow, d, has, [&](int r) { return table + of(r) * ld_table; });
+    const int all = count[0] + count[1] + count[2] + count[3];
+    if (all == 0) return;
     int turn = 0;
     for (int w = 0; w < (nrow + 31) / 32; ++w) {
-        uint32_t bits = has[w];
-        while (bits) {
+        for (uint32_t bits = has[w]; bits; bits &= bits - 1) {
             const int r = w * 32 + __builtin_ctz(bits);
-            bits &= bits - 1;
-            if ((turn++ & 3) != wave) continue;
-            int k = 0;
-            for (int q = 0; q < 4; ++q)
-                for (int i0 = 0; i0 < count[q]; i0 += 64) {
-                    const uint32_t e = i0 + lane < count[q] ? list[q * quarter + i0 + lane] : 0xffffffffu;
-                    const bool hit = e >> 12 == (uint32_t)r;
-                    const uint64_t b = __ballot(hit);
-                    if (hit) mine[k + __popcll(b & ((1ull << lane) - 1))] = (uint16_t)(e & 4095u);
-                    k += __popcll(b);
+            TT *row = table + of(r) * ld_table;
+            if (all <= 64) {  // a wave per row
+                if ((turn++ & 3) != wave) continue;
+                for (int col0 = 0; col0 < d; col0 += 64 * E) {
+                    const int col = col0 + lane * E;
+                    vec_f<E> acc = (vec_f<E>)0.0f;
+                    for (int q = 0; q < 4; ++q) grad_pick<TG, E>(grad, ld_grad, col, d - col, list + q * per, count[q], r, acc);
+                    grad_write<TT, E>(row, col, d - col, acc, scale, accumulate);
                 }
-            for (int col = lane * 8; col < d; col += 512) {
-                vec_f8 acc = (vec_f8)0.0f;
-                grad_sum(grad, ld_grad, col, d - col, k, [&](int i) { return mine[i]; }, acc);
-                grad_write(table + (lo + r) * ld_table, col, d - col, acc, scale, accumulate);
+            } else {  // frequent ids: each wave its quarter of the positions
+                for (int col0 = 0; col0 < d; col0 += 64 * E) {
+                    const int col = col0 + lane * E;
+                    vec_f<E> acc = (vec_f<E>)0.0f;
+                    grad_pick<TG, E>(grad, ld_grad, col, d - col, list + from, m, r, acc);
+                    quarter[wave][lane] = acc;
+                    __syncthreads();
+                    if (wave == 0) {
+#pragma unroll
+                        for (int q = 1; q < 4; ++q) acc += quarter[q][lane];
+                        grad_write<TT, E>(row, col, d - col, acc, scale, accumulate);
+                    }
+                    __syncthreads();
+                }
             }
         }
     }
@@ -336,10 +382,10 @@ k_vec_grad_place(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, 
     }
 }
 
-// --- the sums.  A wave per piece of GRAD_CHUNK sorted positions and 512 columns: ids that lie within the piece are written to
-// the table; the sum of the one that the piece begins with, if it began before, goes to part[chunk][0]; that of the one it ends
-// with, if it goes on, to part[chunk][1] (to [0] if it is the same).  bounds[v]: first and last + 1 sorted position of id v.
-template <class TG, class TT>
+// --- the sums.  A wave per piece of GRAD_CHUNK sorted positions and 64 E columns: ids that lie within the piece are written to
+// the table; the sum of one that began before goes to part[chunk][0], that of one that begins here and goes on to part[chunk][1].  bounds[v]: first and last + 1 sorted position of id v.
+// Rows are requested eight at a time, whatever ids they are of, eight ahead of those that are added.
+template <class TG, class TT, int E>
 __global__ void __launch_bounds__(256)
 k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uint32_t *__restrict__ keys,
                   const uint32_t *__restrict__ pos, int64_t n, int64_t rows, float scale, int accumulate,
@@ -347,7 +393,7 @@ k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uin
     const int chunk = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (chunk >= chunks) return;
     const int64_t first = (int64_t)chunk * GRAD_CHUNK;
-    const int m = (int)(n - first < GRAD_CHUNK ? n - first : GRAD_CHUNK);
+    int m = (int)(n - first < GRAD_CHUNK ? n - first : GRAD_CHUNK);
     const uint32_t none = 0xffffffffu;
     const uint32_t key = lane < m ? keys[first + lane] : none, p = lane < m ? pos[first + lane] : 0;
     const uint32_t prev = lane < m && first + lane > 0 ? keys[first + lane - 1] : none;
@@ -357,68 +403,88 @@ k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uin
         if (begins) bounds[key].x = (uint32_t)(first + lane);
         if (ends) bounds[key].y = (uint32_t)(first + lane) + 1;
     }
-    uint64_t heads = __ballot(begins) | 1ull;  // where an id's run within the piece starts
-    const bool first_whole = __ballot(begins) & 1, last_whole = __ballot(ends) >> (m - 1) & 1;
-    const int col = blockIdx.y * 512 + lane * 8;
-    while (heads) {
-        const int at = __builtin_ctzll(heads);
-        heads &= heads - 1;
-        const int to = heads ? __builtin_ctzll(heads) : m;
-        const uint32_t k = __builtin_amdgcn_readlane(key, at);
-        if (k >= (uint64_t)rows) break;  // ids that take no part come last
-        vec_f8 acc = (vec_f8)0.0f;
-        if (col < d) grad_sum(grad, ld_grad, col, d - col, to - at, [&](int i) { return __builtin_amdgcn_readlane(p, at + i); }, acc);
-        const bool whole = (at > 0 || first_whole) && (to < m || last_whole);
-        if (col >= d) continue;
-        if (whole) grad_write(table + (int64_t)k * ld_table, col, d - col, acc, scale, accumulate);
-        else *(vec_f8 *)(part + ((int64_t)chunk * 2 + (at > 0)) * dpad + col) = acc;
+    const uint64_t heads = __ballot(begins), tails = __ballot(ends);
+    m = __popcll(__ballot(key < (uint64_t)rows));  // (ids that take no part come last)
+    const int col = (int)blockIdx.y * 64 * E + lane * E, left = d - col;
+    const TG *g = grad + col;
+    vec_pack<TG, E> v[8], ahead[8];
+    auto request = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            ahead[u] = vec_load<TG, E>(g + (int64_t)__builtin_amdgcn_readlane(p, (i0 + u) & 63) * ld_grad, i0 + u < m ? left : 0);
+    };
+    vec_f<E> acc = (vec_f<E>)0.0f;
+    bool whole = heads & 1;  // the run that is being added has begun here
+    if (m > 0) request(0);
+    for (int i0 = 0; i0 < m; i0 += 8) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = ahead[u];
+        if (i0 + 8 < m) request(i0 + 8);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = i0 + u;
+            if (i >= m) break;
+            acc += vec_wide<TG, E>(v[u]);
+            if (tails >> i & 1) {
+                if (whole) grad_write<TT, E>(table + (int64_t)__builtin_amdgcn_readlane(key, i) * ld_table, col, left, acc, scale, accumulate);
+                else if (left > 0) *(vec_f<E> *)(part + (int64_t)chunk * 2 * dpad + col) = acc;  // (began before this piece)
+                acc = (vec_f<E>)0.0f;
+                whole = true;
+            }
+        }
     }
+    if (m > 0 && !(tails >> (m - 1) & 1) && left > 0)  // goes on behind this piece
+        *(vec_f<E> *)(part + ((int64_t)chunk * 2 + (whole ? 1 : 0)) * dpad + col) = acc;
 }
 
-// Rows without an id, and those whose run crosses the end of a piece: partial sums in order, a quarter of them per wave.
+// The first `chunks` blocks of a row of the grid: the run that ends in the piece and began before it, its partial sums added in order, a
+// quarter of them per wave if they are many.  The other blocks: the rows without an id, GRAD_END_ROWS each.
 #define GRAD_END_ROWS 64
-template <class TT>
+template <class TT, int E>
 __global__ void __launch_bounds__(256)
-k_vec_grad_end(const uint2 *__restrict__ bounds, const float *__restrict__ part, int dpad, int d, float scale,
-               int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table) {
-    __shared__ uint32_t has[GRAD_END_ROWS / 32], cross[GRAD_END_ROWS / 32];
-    __shared__ uint2 bound[GRAD_END_ROWS];
-    __shared__ vec_f8 quarter[4][64];
-    const int64_t lo = (int64_t)blockIdx.x * GRAD_END_ROWS;
-    const int nrow = (int)(rows - lo < GRAD_END_ROWS ? rows - lo : GRAD_END_ROWS);
+k_vec_grad_end(const uint32_t *__restrict__ keys, int64_t n, const uint2 *__restrict__ bounds, const float *__restrict__ part, int dpad,
+               int d, float scale, int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int chunks) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (threadIdx.x < 64) {
-        const uint2 b = lane < nrow ? bounds[lo + lane] : make_uint2(0, 0);
-        bound[lane] = b;
-        const uint64_t h = __ballot(b.y > b.x), c = __ballot(b.y > b.x && b.x / GRAD_CHUNK != (b.y - 1) / GRAD_CHUNK);
-        if (lane < 2) has[lane] = (uint32_t)(h >> (32 * lane)), cross[lane] = (uint32_t)(c >> (32 * lane));
+    if ((int64_t)blockIdx.x >= chunks) {
+        __shared__ uint32_t has[GRAD_END_ROWS / 32];
+        const int64_t lo = ((int64_t)blockIdx.x - chunks) * GRAD_END_ROWS;
+        const int nrow = (int)(rows - lo < GRAD_END_ROWS ? rows - lo : GRAD_END_ROWS);
+        if (threadIdx.x < 64) {
+            const uint2 b = lane < nrow ? bounds[lo + lane] : make_uint2(0, 0);
+            const uint64_t h = __ballot(b.y > b.x);
+            if (lane < 2) has[lane] = (uint32_t)(h >> (32 * lane));
+        }
+        __syncthreads();
+        grad_zeros<TT>(nrow, d, has, [&](int r) { return table + (lo + r) * ld_table; });
+        return;
     }
-    __syncthreads();
-    if (!accumulate) grad_zeros(table, lo, nrow, d, ld_table, has);
-    for (int r = 0; r < nrow; ++r) {
-        if (!(cross[r >> 5] >> (r & 31) & 1)) continue;
-        const int c0 = (int)(bound[r].x / GRAD_CHUNK), c1 = (int)((bound[r].y - 1) / GRAD_CHUNK);
-        // a run is the piece's second part where it starts within it, else its first
-        const int slot0 = bound[r].x % GRAD_CHUNK ? 1 : 0;
-        const int cnt = c1 - c0 + 1, each = (cnt + 3) / 4;
-        const int a = c0 + wave * each, b = a + each < c1 + 1 ? a + each : c1 + 1;
-        for (int col0 = 0; col0 < d; col0 += 512) {
-            const int col = col0 + lane * 8;
-            vec_f8 acc = (vec_f8)0.0f;
-            if (col < d) {
-                const float *p = part + col;
-#pragma unroll 4
-                for (int c = a; c < b; ++c) acc += *(const vec_f8 *)(p + ((int64_t)c * 2 + (c == c0 ? slot0 : 0)) * dpad);
-            }
+    __shared__ vec_f<E> quarter[4][64];
+    const int chunk = blockIdx.x;
+    const int64_t first = (int64_t)chunk * GRAD_CHUNK;
+    const uint32_t key = keys[first];
+    if (chunk == 0 || key >= (uint64_t)rows || keys[first - 1] != key) return;
+    const uint2 b = bounds[key];
+    if ((b.y - 1) / GRAD_CHUNK != (uint32_t)chunk) return;  // (a later block's)
+    const int c0 = (int)(b.x / GRAD_CHUNK);
+    const int cnt = chunk - c0 + 1, each = cnt <= 8 ? cnt : (cnt + 3) / 4;
+    if (cnt <= 8 && wave > 0) return;
+    const int from = c0 + wave * each, to = from + each < chunk + 1 ? from + each : chunk + 1;
+    for (int col0 = 0; col0 < d; col0 += 64 * E) {
+        const int col = col0 + lane * E;
+        vec_f<E> acc = (vec_f<E>)0.0f;
+        if (col < d) {
+#pragma unroll 8
+            for (int c = from; c < to; ++c) acc += *(const vec_f<E> *)(part + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * dpad + col);
+        }
+        if (cnt > 8) {
             quarter[wave][lane] = acc;
             __syncthreads();
-            if (wave == 0 && col < d) {
+            if (wave == 0)
 #pragma unroll
                 for (int w = 1; w < 4; ++w) acc += quarter[w][lane];
-                grad_write(table + (lo + r) * ld_table, col, d - col, acc, scale, accumulate);
-            }
-            __syncthreads();
         }
+        if (wave == 0) grad_write<TT, E>(table + (int64_t)key * ld_table, col, d - col, acc, scale, accumulate);
+        if (cnt > 8) __syncthreads();
     }
 }
 
@@ -444,20 +510,18 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     }
     hipStream_t s = (hipStream_t)stream;
     if (p.few) {
-        // 1024 blocks, four per CU; the row of a block and a position share a word, so at most 2^19 rows a block
-        int64_t rpb = (rows + 1023) / 1024;
-        if (rpb < 8) rpb = 8;
-        if (rpb > 65536) rpb = 65536;
-        const int64_t blocks = (rows + rpb - 1) / rpb;
-        const size_t lds = (size_t)((rpb + 31) / 32) * 4 + GRAD_FEW * 4 + 4 * GRAD_FEW * 2;
-#define GO(TG, TT, ID)                                                                                                     \
-    do {                                                                                                                   \
-        if (lds > 64 * 1024)                                                                                               \
-            QADC_HIP_TRY(hipFuncSetAttribute((const void *)k_vec_grad_few<TG, TT, ID>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)); \
-        hipLaunchKernelGGL((k_vec_grad_few<TG, TT, ID>), dim3((unsigned)blocks), dim3(256), lds, s, (const TG *)grad, (int)n, d, \
-                           ld_grad, (const ID *)ids, scale, accumulate, (TT *)table_grad, rows, ld_table, (int)rpb);        \
-    } while (0)
-        VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, if (id_bytes == 4) GO(TG, TT, int32_t); else GO(TG, TT, int64_t)));
+        // 512 bytes of neighbouring rows together; about 1024 blocks (at most 2^16 rows each: a row of a block shares a word with a position)
+        int group = 0, deal = 0;
+        while (group < 5 && ((int64_t)vec_bytes(table_type) * d << group) < 512) ++group;
+        while (deal < 10 && ((int64_t)4 << group << deal) < rows) ++deal;
+        while ((rows >> (deal + 15)) > 0) ++deal;
+        const int64_t groups = (rows + ((int64_t)1 << group) - 1) >> group, each = (groups + ((int64_t)1 << deal) - 1) >> deal;
+        const int rpb = (int)(each << group);
+        const size_t lds = (size_t)((rpb + 31) / 32) * 4 + GRAD_FEW * 4;
+#define GO(TG, TT, ID, E)                                                                                                  \
+    hipLaunchKernelGGL((k_vec_grad_few<TG, TT, ID, E>), dim3(1u << deal), dim3(256), lds, s, (const TG *)grad, (int)n, d,  \
+                       ld_grad, (const ID *)ids, scale, accumulate, (TT *)table_grad, rows, ld_table, group, deal, rpb)
+        VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, if (id_bytes == 4) GO(TG, TT, int32_t, E); else GO(TG, TT, int64_t, E))));
 #undef GO
         QADC_LAUNCH_CHECK("k_vec_grad_few");
         return PQ_OK;
@@ -484,12 +548,12 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
 #undef GO
     }
     const uint32_t *ks = key[(p.passes - 1) & 1], *ps = pos[(p.passes - 1) & 1];
-    const dim3 grid((unsigned)((p.chunks + 3) / 4), (unsigned)((d + 511) / 512));
-    VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, hipLaunchKernelGGL((k_vec_grad_chunks<TG, TT>), grid, dim3(256), 0, s, (const TG *)grad, d,
-                                                                         ld_grad, ks, ps, n, rows, scale, accumulate, (TT *)table_grad, ld_table,
-                                                                         bounds, part, p.dpad, p.chunks)));
-    VEC_TYPED(table_type, TT, hipLaunchKernelGGL((k_vec_grad_end<TT>), dim3((unsigned)((rows + GRAD_END_ROWS - 1) / GRAD_END_ROWS)), dim3(256), 0, s,
-                                                 bounds, part, p.dpad, d, scale, accumulate, (TT *)table_grad, rows, ld_table));
+    VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL(
+        (k_vec_grad_chunks<TG, TT, E>), dim3((unsigned)((p.chunks + 3) / 4), (unsigned)((d + 64 * E - 1) / (64 * E))), dim3(256), 0, s, (const TG *)grad,
+        d, ld_grad, ks, ps, n, rows, scale, accumulate, (TT *)table_grad, ld_table, bounds, part, p.dpad, p.chunks))));
+    const int64_t zeros = accumulate ? 0 : (rows + GRAD_END_ROWS - 1) / GRAD_END_ROWS;
+    VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL((k_vec_grad_end<TT, E>), dim3((unsigned)(p.chunks + zeros)), dim3(256), 0, s, ks, n,
+                                                                bounds, part, p.dpad, d, scale, accumulate, (TT *)table_grad, rows, ld_table, p.chunks)));
     QADC_LAUNCH_CHECK("vec_lookup_grad's kernels");
     return PQ_OK;
 }
