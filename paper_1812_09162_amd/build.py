@@ -25,7 +25,9 @@ FLAGS = [
 
 def _compile(src: str) -> str:
     obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-    subprocess.check_call([HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
+    # the products with F32 scales multiply what the matrix instructions give, which can stay in vector registers for that
+    more = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] if src.startswith("vec_matmul_") else []
+    subprocess.check_call([HIPCC, *FLAGS, *more, "-c", os.path.join(CSRC, src), "-o", obj])
     return obj
 
 

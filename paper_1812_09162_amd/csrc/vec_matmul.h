@@ -95,19 +95,27 @@ __device__ __forceinline__ void mat_store(const MatArgs &p, int64_t row, int64_t
 }
 
 // ------------------------------------------------------------------- tiles --
-// A block of WM x WN waves makes a tile of c; a wave 16 MI rows by 16 NI columns of it.  Blocks of k pass through two buffers
-// of LDS: while one is multiplied, the next is on its way to the other, from memory to LDS without registers (ASYNC: rows
-// that start at multiples of 16 bytes) or through them.  A row of a buffer is 128 bytes, its sixteen-byte pieces exchanged by
-// the row's low three bits, so that eight lanes that read the same piece of eight rows meet eight different banks.
-// A last block of fewer than 128 columns always comes through registers, with zeros behind.
-// Rows beyond the matrix are the last row again; what comes of them is not stored.
+// A block of WM x WN waves makes a tile of c; a wave 16 MI rows by 16 NI columns of it.  Blocks of k pass through two
+// buffers of LDS: while one is multiplied, the next is on its way, from memory to LDS without registers (ASYNC: rows that
+// start at multiples of 16 bytes) or through them.  (Three blocks ahead in four buffers was no faster: 2048 x 2048 x 2048 25.3 us with
+// two, 26.3 with four; what bounds a lone block is the chain of reading, widening and multiplying.)  A row of a buffer is 128 bytes, its sixteen-byte
+// pieces exchanged by the row's low three bits, so that eight lanes that read the same piece of eight rows meet eight
+// different banks.  ASYNC reads through a buffer that ends with the tile's last row, so that one offset per lane serves all rows, and
+// rows beyond the matrix and pieces beyond the last column are zeros; a piece that the last column divides comes through
+// registers, and its block of k last and by itself.  (There, rows beyond the matrix are the last row again; what comes of
+// them is not stored.)
+typedef __attribute__((address_space(3))) void *mat_to;
+#define MAT_BUFFER 0x00027000  // a raw buffer: offsets in bytes; what lies at or behind its length reads as zero
+
 template <int FA, int FB, bool P2, bool ASYNC, int WM, int WN, int MI, int NI>
 __global__ void __launch_bounds__(64 * WM * WN)
 k_vec_mat(const MatArgs p) {
-    constexpr int BM = WM * MI * 16, BN = WN * NI * 16, ROWS = BM + BN, WAVES = WM * WN, NT = 64 * WAVES;
-    constexpr int PER = ROWS / 8 / WAVES;  // wave instructions per step: eight rows each
-    constexpr int STAGE = ROWS * 132;      // bytes of a buffer: values and scales
-    static_assert(ROWS <= NT && (ROWS / 8) % WAVES == 0 && BM % (8 * PER) == 0, "a thread brings one scale; a wave's rows are of one factor");
+#if defined(__HIP_DEVICE_COMPILE__)  // (the host has no type for a buffer)
+    constexpr int BM = WM * MI * 16, BN = WN * NI * 16, ROWS = BM + BN, WAVES = WM * WN;
+    constexpr int PER = ROWS / 8 / WAVES, PER_A = BM / 8 / WAVES;  // wave instructions per step, eight rows each; a's are first
+    constexpr int STAGE = ROWS * 132;                              // bytes of a buffer: values and scales
+    static_assert(ROWS == 64 * WAVES &&  // (a thread brings one row's scale)
+                  BM % 64 == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "");
     extern __shared__ __align__(16) uint8_t lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
 
@@ -126,29 +134,36 @@ k_vec_mat(const MatArgs p) {
 
     const int steps = (int)((p.k + VEC_BLOCK - 1) / VEC_BLOCK);
     const int s0 = split * p.per, s1 = s0 + p.per < steps ? s0 + p.per : steps;
-    const int whole = (int)(p.k / VEC_BLOCK) < s1 ? (int)(p.k / VEC_BLOCK) : s1;  // steps before this one are of 128 columns
+    const int full = (int)(p.k / VEC_BLOCK);  // steps before this one have all their columns
+    const int last_step = ASYNC && p.k % 16 == 0 ? s1 : (full < s1 ? full : s1);  // ... those before this one go through the buffers in turn
 
-    // this wave's rows of the buffer: wave * 8 PER ..
-    const bool is_b = wave * 8 * PER >= BM;
-    const int64_t ld = is_b ? p.ld_b : p.ld_a;
-    const int64_t first = is_b ? n0 + wave * 8 * PER - BM : m0 + wave * 8 * PER, last = (is_b ? p.n : p.m) - 1;
-    const int64_t from = first < last ? first : last;
-    const uint8_t *mat = (is_b ? p.b : p.a) + from * ld;
-    const int most = (int)(last - from < ROWS ? last - from : ROWS);  // rows from there on
+    // where this wave's rows of a buffer come from: i-th instruction, rows 8 (i WAVES + wave) + lane / 8
+    const uint8_t *const mat_a = p.a + m0 * p.ld_a, *const mat_b = p.b + n0 * p.ld_b;
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // the columns that this lane's place in a row holds
-    auto delta = [&](int i) { return i * 8 + (lane >> 3) < most ? i * 8 + (lane >> 3) : most; };
-    uint32_t off[ASYNC ? PER : 1];  // (ASYNC: rows are less than 2^23 apart)
-    if constexpr (ASYNC)
-#pragma unroll
-        for (int i = 0; i < PER; ++i) off[i] = (uint32_t)delta(i) * (uint32_t)ld + piece;
-    // ... and the thread's scale
-    const bool sc = (int)threadIdx.x < ROWS, sc_b = (int)threadIdx.x >= BM;
-    const int64_t sr = sc_b ? n0 + threadIdx.x - BM : m0 + threadIdx.x, sl = (sc_b ? p.n : p.m) - 1;
-    const int64_t srow = (sr < sl ? sr : sl) * (sc_b ? p.ld_bs : p.ld_as);
-    const void *const sp = sc_b ? p.b_scales : p.a_scales;
-    // (E8M0: a lane needs its row's in tiles of sixteen rows, and those of four tiles lie side by side.  F32: b's are needed for four
-    // neighbouring rows, a's for one.)
-    const int t = threadIdx.x, st = ROWS * 128 + 4 * (P2 ? (t & ~63) + (t & 15) * 4 + (t >> 4 & 3) : t);
+    // (ASYNC: rows are less than 2^23 apart, their scales less than 2^21, so that a tile's offsets have 32 bits)
+    auto buffer = [](const uint8_t *at, int rows, int64_t ld, int64_t cols) {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, ASYNC ? (int)((uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)cols) : 0, MAT_BUFFER);
+    };
+    const int rows_a = (int)(p.m - m0 < BM ? p.m - m0 : BM), rows_b = (int)(p.n - n0 < BN ? p.n - n0 : BN);
+    auto delta = [&](int i) {
+        const int r = (i * WAVES + wave) * 8 + (lane >> 3) - (i < PER_A ? 0 : BM), most = (i < PER_A ? rows_a : rows_b) - 1;
+        return r < most ? r : most;
+    };
+    const auto buf_a = buffer(mat_a, rows_a, p.ld_a, p.k), buf_b = buffer(mat_b, rows_b, p.ld_b, p.k);
+    const uint32_t off_a = (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.ld_a + piece, off_b = (uint32_t)(wave * 8 + (lane >> 3)) * (uint32_t)p.ld_b + piece;
+    // ... and the scale of this thread's row.  E8M0: a lane multiplies rows 16 apart, so their scales lie side by side.
+    const int t = threadIdx.x, srow = P2 ? (t & ~63) + (t & 3) * 16 + (t >> 2 & 15) : t;
+    constexpr int SB = P2 ? 1 : 4;  // bytes of a scale
+    const bool sc_b = wave * 64 >= BM;
+    const uint8_t *const mat_s = (const uint8_t *)(sc_b ? p.b_scales : p.a_scales) + (sc_b ? n0 * p.ld_bs : m0 * p.ld_as) * SB;
+    const int64_t ld_s = (sc_b ? p.ld_bs : p.ld_as) * SB;
+    const int rows_s = sc_b ? rows_b : rows_a, srow_in = srow - (sc_b ? BM : 0);
+    const auto buf_s = buffer(mat_s, rows_s, ld_s, (int64_t)steps * SB);
+    const uint32_t off_s = (uint32_t)srow_in * (uint32_t)ld_s;
+    auto scale_at = [&](int s) {  // (through registers)
+        const uint8_t *q = mat_s + (srow_in < rows_s ? srow_in : rows_s - 1) * ld_s;
+        return P2 ? (uint32_t)q[s] : ((const uint32_t *)q)[s];
+    };
 
     vec_f4 acc[MI][NI];
 #pragma unroll
@@ -161,28 +176,31 @@ k_vec_mat(const MatArgs p) {
 
     uint32_t scale_next = 0;
     vec_i4 regs[ASYNC ? 1 : PER];
-    auto request_scale = [&](int s) {
-        if (sc) scale_next = mat_scale_bits(sp, srow + s, P2);
-    };
-    auto put_scale = [&](int buf) {
-        if (sc) *(uint32_t *)(lds + buf + st) = scale_next;
-    };
-    auto request = [&](int s, int buf) {  // a whole step
-        request_scale(s);
+    auto request = [&](int s, int buf) {
+        if constexpr (ASYNC) {
+            // (all of an address is in the lanes' offsets: a scalar offset would not count against the buffer's end)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_s, (mat_to)(lds + buf + ROWS * 128 + wave * 256), SB, off_s + (uint32_t)s * SB, 0, 0, 0);  // (a byte arrives as a word)
+            const bool none = s >= full && s * 128 + piece >= (int)p.k;  // beyond the last column: 2^31 is behind every tile
+            const uint32_t at_a = (none ? 0x80000000u : off_a) + (uint32_t)s * 128, at_b = (none ? 0x80000000u : off_b) + (uint32_t)s * 128;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if constexpr (ASYNC)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(mat + (int64_t)s * 128 + off[i]),
-                                                 (__attribute__((address_space(3))) void *)(lds + buf + (wave * PER + i) * 1024), 16, 0, 0);
-            else
-                regs[i] = mat_chunk(mat + delta(i) * ld, (int64_t)s * 128 + piece, p.k);
+            for (int i = 0; i < PER; ++i) {
+                const mat_to to = (mat_to)(lds + buf + (i * WAVES + wave) * 1024);
+                if (i < PER_A) __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_a, to, 16, at_a + (uint32_t)(i * WAVES * 8) * (uint32_t)p.ld_a, 0, 0, 0);
+                else __builtin_amdgcn_raw_ptr_buffer_load_lds(buf_b, to, 16, at_b + (uint32_t)((i - PER_A) * WAVES * 8) * (uint32_t)p.ld_b, 0, 0, 0);
+            }
+        } else {
+            scale_next = scale_at(s);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                regs[i] = mat_chunk((i < PER_A ? mat_a : mat_b) + delta(i) * (i < PER_A ? p.ld_a : p.ld_b), (int64_t)s * 128 + piece, p.k);
         }
     };
     auto put = [&](int buf) {
-        put_scale(buf);
-        if constexpr (!ASYNC)
+        if constexpr (!ASYNC) {
+            *(uint32_t *)(lds + buf + ROWS * 128 + t * 4) = scale_next;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) *(vec_i4 *)(lds + buf + (wave * PER + i) * 1024 + lane * 16) = regs[i];
+            for (int i = 0; i < PER; ++i) *(vec_i4 *)(lds + buf + (i * WAVES + wave) * 1024 + lane * 16) = regs[i];
+        }
     };
     auto multiply = [&](int buf) {
         const int fa = buf + wm * MI * 2048 + frag, fb = buf + BM * 128 + wn * NI * 2048 + frag;
@@ -190,22 +208,45 @@ k_vec_mat(const MatArgs p) {
         // (bit 4 tells a lane's two pieces apart, and no tile's offset has it)
         auto load = [&](int at, int half) { return *(const vec_i4 *)(lds + (half ? at ^ 16 : at)); };
         if constexpr (P2) {
+            // E8M0 as the float32 whose exponent it is (mat_widen looks at the exponent alone, so 0 is 2^-127)
             vec_f4 sa[MI / 4], sb[NI / 4];
 #pragma unroll
-            for (int i = 0; i < MI / 4; ++i) sa[i] = *(const vec_f4 *)(lds + sca + ((wm * MI / 4 + i) * 64 + (lane & 15) * 4) * 4);
+            for (int i = 0; i < MI / 4; ++i) sa[i] = __builtin_bit_cast(vec_f4, *(const vec_i4 *)(lds + sca + ((wm * MI / 4 + i) * 64 + (lane & 15) * 4) * 4) << 23);
 #pragma unroll
-            for (int j = 0; j < NI / 4; ++j) sb[j] = *(const vec_f4 *)(lds + scb + ((wn * NI / 4 + j) * 64 + (lane & 15) * 4) * 4);
+            for (int j = 0; j < NI / 4; ++j) sb[j] = __builtin_bit_cast(vec_f4, *(const vec_i4 *)(lds + scb + ((wn * NI / 4 + j) * 64 + (lane & 15) * 4) * 4) << 23);
+            // in turn the tile rows of one half, then of the other: while one is multiplied, the next is widened and the one behind it read; so
+            // are, during the first half, b's of the second, where registers allow it
+            constexpr int N = 2 * MI;
+            constexpr bool BOTH = MI <= NI;
+            auto read_a = [&](int t) { return load(fa + t % MI * 2048, t / MI); };
+            auto wide_a = [&](int t, vec_i4 x) { return mat_half<FA>(x, sa[t % MI / 4][t % MI % 4]); };
+            auto wide_b = [&](int j, vec_i4 x) { return mat_half<FB>(x, sb[j / 4][j % 4]); };
+            MatHalf b[BOTH ? 2 : 1][NI], a[2];
+            vec_i4 raw[2], rawb[NI];
+            raw[0] = read_a(0);
+            raw[1] = read_a(1);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                MatHalf b[NI];
+            for (int j = 0; j < NI; ++j) rawb[j] = load(fb + j * 2048, 0);
 #pragma unroll
-                for (int j = 0; j < NI; ++j) b[j] = mat_half<FB>(load(fb + j * 2048, half), sb[j / 4][j % 4]);
+            for (int j = 0; j < NI; ++j) b[0][j] = wide_b(j, rawb[j]);
+            a[0] = wide_a(0, raw[0]);
 #pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    const MatHalf a = mat_half<FA>(load(fa + i * 2048, half), sa[i / 4][i % 4]);
+            for (int t = 0; t < N; ++t) {
+                if (!BOTH && t == MI) {
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) acc[i][j] = mat_mul(b[j], a, acc[i][j]);
+                    for (int j = 0; j < NI; ++j) b[0][j] = wide_b(j, load(fb + j * 2048, 1));
                 }
+                if (t + 2 < N) raw[t & 1] = read_a(t + 2);
+                if (t + 1 < N) a[(t + 1) & 1] = wide_a(t + 1, raw[(t + 1) & 1]);
+                if (BOTH && t < MI) {
+#pragma unroll
+                    for (int j = t * NI / MI; j < (t + 1) * NI / MI; ++j) b[BOTH ? 1 : 0][j] = wide_b(j, load(fb + j * 2048, 1));
+                }
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[t % MI][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[BOTH ? t / MI : 0][j].v[v], a[t & 1].v[v], acc[t % MI][j], 0, 0, 0);
             }
         } else {
             MatHalf b[2][NI];
@@ -216,45 +257,62 @@ k_vec_mat(const MatArgs p) {
                 b[1][j] = mat_half<FB>(load(fb + j * 2048, 1), 1.0f);
                 sb[j] = *(const vec_f4 *)(lds + scb + ((wn * NI + j) * 16 + (lane >> 4) * 4) * 4);
             }
+            // a tile row's sums are scaled while the next one's products run
+            vec_f4 q[2][NI];
+            float sa[2];
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const MatHalf a0 = mat_half<FA>(load(fa + i * 2048, 0), 1.0f), a1 = mat_half<FA>(load(fa + i * 2048, 1), 1.0f);
-                const float sa = *(const float *)(lds + sca + ((wm * MI + i) * 16 + (lane & 15)) * 4);
+            for (int i = 0; i <= MI; ++i) {
+                if (i < MI) {
+                    const MatHalf a0 = mat_half<FA>(load(fa + i * 2048, 0), 1.0f), a1 = mat_half<FA>(load(fa + i * 2048, 1), 1.0f);
+                    sa[i & 1] = *(const float *)(lds + sca + ((wm * MI + i) * 16 + (lane & 15)) * 4);
 #pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    const vec_f4 q = mat_mul(b[1][j], a1, mat_mul(b[0][j], a0, (vec_f4)0.0f));
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][j][r] = __fmaf_rn(q[r], sa * sb[j][r], acc[i][j][r]);
+                    for (int j = 0; j < NI; ++j) q[i & 1][j] = mat_mul(b[1][j], a1, mat_mul(b[0][j], a0, (vec_f4)0.0f));
                 }
+                if (i > 0)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            acc[i - 1][j][r] = __fmaf_rn(q[(i - 1) & 1][j][r], sa[(i - 1) & 1] * sb[j][r], acc[i - 1][j][r]);
             }
         }
     };
-    auto landed = [&]() {  // the buffer on its way is whole, and nobody reads the other any more
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
 
-    int now = 0, other = STAGE;
-    if (s0 < whole) {
-        request(s0, now);
-        put(now);
-        for (int s = s0; s < whole; ++s) {
-            landed();
-            if (s + 1 < whole) request(s + 1, other);
+    if constexpr (ASYNC) {
+        int now = 0;
+        if (s0 < last_step) request(s0, 0);
+        for (int s = s0; s < last_step; ++s) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // this wave's part of the step has landed, and its reads of the last are done
+            __builtin_amdgcn_s_barrier();                                  // everybody's have
+            asm volatile("" ::: "memory");
+            if (s + 1 < last_step) request(s + 1, STAGE - now);
             multiply(now);
-            if (s + 1 < whole) put(other);
-            now = other;
-            other = STAGE - now;
+            now = STAGE - now;
+        }
+    } else {
+        int now = 0;
+        if (s0 < last_step) {
+            request(s0, 0);
+            put(0);
+            for (int s = s0; s < last_step; ++s) {
+                __syncthreads();
+                if (s + 1 < last_step) request(s + 1, 0);
+                multiply(now);
+                now = STAGE - now;
+                if (s + 1 < last_step) put(now);
+            }
         }
     }
-    if (whole < s1) {  // fewer than 128 columns are left
-        request_scale(whole);
-        put_scale(now);
-#pragma unroll 1
-        for (int i = 0; i < PER; ++i)
-            *(vec_i4 *)(lds + now + (wave * PER + i) * 1024 + lane * 16) = mat_chunk(mat + delta(i) * ld, (int64_t)whole * 128 + piece, p.k);
+    if (last_step < s1) {  // a piece that the last column divides
         __syncthreads();
-        multiply(now);
+        *(uint32_t *)(lds + ROWS * 128 + t * 4) = scale_at(last_step);
+#pragma unroll 1
+        for (int i = 0; i < PER; ++i) {
+            const uint8_t *const row = i < PER_A ? mat_a + delta(i) * p.ld_a : mat_b + delta(i) * p.ld_b;
+            *(vec_i4 *)(lds + (i * WAVES + wave) * 1024 + lane * 16) = mat_chunk(row, (int64_t)last_step * 128 + piece, p.k);
+        }
+        __syncthreads();
+        multiply(0);
     }
 
 #pragma unroll
@@ -276,6 +334,7 @@ k_vec_mat(const MatArgs p) {
             }
         }
     }
+#endif
 }
 
 // -------------------------------------------------------------- few rows of a --
@@ -355,10 +414,11 @@ k_vec_mat_few(const MatArgs p, int kshare) {
 }
 
 // The host's choice of a form.
+enum { MAT_128 = 0, MAT_256 = 1 };  // tiles of 128 x 128 or of 256 x 256
 struct MatPlan {
-    int few;       // 0: tiles; 1, 2, 4: sixteens of rows of a
+    int few;       // 0: tiles; 1, 2: sixteens of rows of a
     int kshare;    // few: waves that share a tile's k
-    bool big;      // tiles of 256 x 256 instead of 128 x 128
+    int tile;      // MAT_*
     int tm, tn, splits, per;
     size_t workspace;
 };

@@ -21,29 +21,38 @@ __global__ void __launch_bounds__(256) k_vec_mat_join(const MatArgs p) {
     mat_store(p, row, col, sum);
 }
 
-static MatPlan mat_plan(int64_t m, int64_t n, int64_t k) {
+// The form of a product, by what each was measured to take (us; E8M0 scales unless said otherwise).
+//   Tiles: 5, and for a step of 128 columns 1.15 (128 x 128, one tile on a CU; 0.92 per tile with more; F32 scales 1.45 and 1.25) or 3.1
+//   (256 x 256), so that large tiles win by a sixth where they fill the CUs; k is split into shares where tiles are too few
+//   for that, at the price of a launch and of partial results written and read (4.5 TB/s).
+//   Up to 32 rows of a, each wave sixteen rows of b: 2.5, and b at 4.6 TB/s for one row, 3.1 up to 16, 2.1 up to 32 (rows of a are read again by
+//   every wave): 16 x 4096 x 4096 9.3 against 13.4 in tiles, 32 11.5 / 14.0, but 16 x 65,536 x 4096 88 / 59 and 64 x 4096 x 4096 17.4 / 16.2.
+static MatPlan mat_plan(int64_t m, int64_t n, int64_t k, bool pow2) {
     MatPlan p = {};
     const int64_t steps = (k + VEC_BLOCK - 1) / VEC_BLOCK;
-    p.splits = 1;
-    p.per = (int)steps;
-    if (m <= 64) {
-        p.few = m <= 16 ? 1 : (m <= 32 ? 2 : 4);
-        const int64_t tiles = (n + 15) / 16;
-        p.kshare = 1;
-        while (p.kshare < MAT_FEW_WAVES && p.kshare * 2 <= steps && tiles * p.kshare < 4096) p.kshare *= 2;
-        return p;
+    double best = 1e300;
+    for (int tile = MAT_128; tile <= (pow2 ? MAT_256 : MAT_128); ++tile) {
+        const int side = tile == MAT_256 ? 256 : 128;
+        const int64_t tm = (m + side - 1) / side, tn = (n + side - 1) / side;
+        if (tm * tn > 0x7fffffffLL) continue;
+        for (int64_t s = 1; s <= 32 && (s == 1 || (s * 4 <= steps && tm * tn * s <= 512)); ++s) {
+            const int64_t per = (steps + s - 1) / s, rounds = (tm * tn * s + 255) / 256;
+            const double step = tile == MAT_256 ? 3.1 : (rounds == 1 ? (pow2 ? 1.15 : 1.45) : (pow2 ? 0.92 : 1.25));
+            const double us = 5.0 + (double)rounds * (double)per * step + (s > 1 ? 4.0 + (double)s * (double)m * (double)n * 8 / 4.5e6 : 0.0);
+            if (us >= best) continue;
+            best = us;
+            p.tile = tile;
+            p.tm = (int)tm;
+            p.tn = (int)tn;
+            p.per = (int)per;
+            p.splits = per > 0 ? (int)((steps + per - 1) / per) : 1;
+        }
     }
-    const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-    p.big = big >= 192;
-    const int side = p.big ? 256 : 128;
-    const int64_t tm = (m + side - 1) / side, tn = (n + side - 1) / side, tiles = tm * tn;
-    p.tm = (int)tm;
-    p.tn = (int)tn;
-    if (!p.big && tiles < 384 && steps >= 8) {
-        int64_t s = (512 + tiles - 1) / tiles;
-        if (s > steps / 4) s = steps / 4;
-        p.per = (int)((steps + s - 1) / s);
-        p.splits = (int)((steps + p.per - 1) / p.per);
+    if (m <= 32 && 2.5 + (double)n * (double)k / (m == 1 ? 4.6e6 : (m <= 16 ? 3.1e6 : 2.1e6)) < best) {
+        p.few = m <= 16 ? 1 : 2;
+        p.splits = 1;
+        p.kshare = 1;
+        while (p.kshare < MAT_FEW_WAVES && p.kshare * 2 <= steps && (n + 15) / 16 * p.kshare < 4096) p.kshare *= 2;
     }
     if (p.splits > 1) p.workspace = vec_up256((size_t)p.splits * (size_t)m * (size_t)n * 4);
     return p;
@@ -53,7 +62,9 @@ static bool mat_sizes(int64_t m, int64_t n, int64_t k) {
     return m >= 0 && n >= 0 && k >= 0 && m <= 0x7fffffffLL && n <= 0x7fffffffLL && k <= 0x7fffffffLL;
 }
 extern "C" size_t vec_matmul_blocks_workspace_bytes(int64_t m, int64_t n, int64_t k) {
-    return !mat_sizes(m, n, k) || m == 0 || n == 0 ? 0 : mat_plan(m, n, k).workspace;
+    if (!mat_sizes(m, n, k) || m == 0 || n == 0) return 0;
+    const size_t a = mat_plan(m, n, k, true).workspace, b = mat_plan(m, n, k, false).workspace;
+    return a > b ? a : b;
 }
 
 extern "C" int vec_matmul_blocks(const void *a, int64_t ld_a, int a_type, const void *a_scales, int64_t ld_a_scales, const void *b,
@@ -68,26 +79,25 @@ extern "C" int vec_matmul_blocks(const void *a, int64_t ld_a, int a_type, const 
     if (m == 0 || n == 0) return PQ_OK;
     VEC_REQUIRE(c && (k == 0 || (a && b && a_scales && b_scales)), "vec_matmul_blocks: null pointer");
     VEC_REQUIRE(vec_aligned(c, c_type) && vec_aligned(a_scales, scale_type) && vec_aligned(b_scales, scale_type), "vec_matmul_blocks: misaligned pointer");
-    MatPlan plan = mat_plan(m, n, k);
+    const bool pow2 = scale_type == VEC_E8M0;
+    const bool async = (((uintptr_t)a | (uintptr_t)b | (uintptr_t)ld_a | (uintptr_t)ld_b) & 15u) == 0 && ld_a < (1 << 23) && ld_b < (1 << 23) &&
+                       ld_a_scales < (1 << 21) && ld_b_scales < (1 << 21);
+    // (the large tile has no registers to spare for a detour, nor for sums of a block)
+    const MatPlan plan = mat_plan(m, n, k, pow2 && async);
     if (plan.workspace > 0) {
+        const size_t need = vec_matmul_blocks_workspace_bytes(m, n, k);
         VEC_REQUIRE(workspace && ((uintptr_t)workspace & 255u) == 0, "vec_matmul_blocks: workspace null or not 256-byte aligned");
-        if (workspace_bytes < plan.workspace) {
-            qadc_set_error("vec_matmul_blocks: workspace of %zu bytes, %zu needed", workspace_bytes, plan.workspace);
+        if (workspace_bytes < need) {
+            qadc_set_error("vec_matmul_blocks: workspace of %zu bytes, %zu needed", workspace_bytes, need);
             return PQ_ENOMEM;
         }
     }
-    const bool async = (((uintptr_t)a | (uintptr_t)b | (uintptr_t)ld_a | (uintptr_t)ld_b) & 15u) == 0 && ld_a < (1 << 23) && ld_b < (1 << 23);
-    if (plan.big && !(async && scale_type == VEC_E8M0)) {  // the large tile has no registers to spare for a detour, nor for sums of a block
-        plan.big = false;
-        plan.tm = (int)((m + 127) / 128);
-        plan.tn = (int)((n + 127) / 128);
-    }
-    VEC_REQUIRE(plan.few ? (n + 15) / 16 <= 0x7fffffffLL : (int64_t)plan.tm * plan.tn <= 0x7fffffffLL / plan.splits, "vec_matmul_blocks: m=%lld, n=%lld too large for one call",
+    VEC_REQUIRE(plan.few > 0 || plan.tm > 0, "vec_matmul_blocks: m=%lld, n=%lld too large for one call",
                 (long long)m, (long long)n);
     const MatArgs p = {(const uint8_t *)a, (const uint8_t *)b, a_scales, b_scales, ld_a, ld_b, ld_a_scales, ld_b_scales, m, n, k,
                        c, ld_c, c_type, (float *)workspace, plan.splits, plan.per, plan.tm, plan.tn};
     hipStream_t s = (hipStream_t)stream;
-    const bool pow2 = scale_type == VEC_E8M0, a5 = a_type == VEC_E5M2, b5 = b_type == VEC_E5M2;
+    const bool a5 = a_type == VEC_E5M2, b5 = b_type == VEC_E5M2;
     const int rc = a5 ? (b5 ? qadc_vec_mat_launch<1, 1>(p, plan, pow2, async, s) : qadc_vec_mat_launch<1, 0>(p, plan, pow2, async, s))
                       : (b5 ? qadc_vec_mat_launch<0, 1>(p, plan, pow2, async, s) : qadc_vec_mat_launch<0, 0>(p, plan, pow2, async, s));
     if (rc != PQ_OK || plan.splits == 1) return rc;

@@ -21,10 +21,10 @@ template <bool P2>
 static int go(const MatArgs &p, const MatPlan &plan, bool async, hipStream_t s) {
     if (plan.few == 1) return go_few<P2, 1>(p, plan, s);
     if (plan.few == 2) return go_few<P2, 2>(p, plan, s);
-    if (plan.few == 4) return go_few<P2, 4>(p, plan, s);
+    if (!async) return go_tiles<P2, false, 2, 2, 4, 4>(p, s);
     if constexpr (P2)
-        if (plan.big) return go_tiles<P2, true, 2, 4, 8, 4>(p, s);
-    return async ? go_tiles<P2, true, 2, 2, 4, 4>(p, s) : go_tiles<P2, false, 2, 2, 4, 4>(p, s);
+        if (plan.tile == MAT_256) return go_tiles<P2, true, 2, 4, 8, 4>(p, s);
+    return go_tiles<P2, true, 2, 2, 4, 4>(p, s);
 }
 template <>
 int qadc_vec_mat_launch<MAT_FA, MAT_FB>(const MatArgs &p, const MatPlan &plan, bool pow2, bool async, hipStream_t s) {
