@@ -50,7 +50,16 @@ __device__ __forceinline__ void vec_store(T *p, int64_t left, vec_f<E> f) {
     for (int i = 0; i < E - 1; ++i)
         if (i < left) p[i] = v[i];
 }
-// eight bytes
+// sixteen bytes, eight bytes
+__device__ __forceinline__ void vec_store_bytes(uint8_t *p, int64_t left, vec_i4 v) {
+    typedef int any128 __attribute__((ext_vector_type(4), aligned(1)));
+    if (left >= 16) {
+        *(any128 *)p = v;
+        return;
+    }
+    for (int i = 0; i < 15; ++i)
+        if (i < left) p[i] = (uint8_t)(v[i >> 2] >> (8 * (i & 3)));
+}
 __device__ __forceinline__ void vec_store_bytes(uint8_t *p, int64_t left, uint64_t v) {
     typedef uint64_t any64 __attribute__((aligned(1)));
     if (left >= 8) {
@@ -91,7 +100,8 @@ __device__ __forceinline__ float vec_top(vec_f8 f) {
 struct VecScale {
     float scale;     // F32
     uint32_t e8m0;   // E8M0: the byte
-    float inverse;   // ... and one over the power
+    float inverse;   // one over the scale
+    bool divide;     // F32: quotients of such scales take a division
 };
 __device__ __forceinline__ VecScale vec_scale(float top, bool e5m2, bool pow2) {
     VecScale s;
@@ -101,14 +111,34 @@ __device__ __forceinline__ VecScale vec_scale(float top, bool e5m2, bool pow2) {
     s.e8m0 = (uint32_t)e;
     s.inverse = __uint_as_float((uint32_t)(254 - e) << 23);
     s.scale = 1.0f;
-    if (!pow2 && top != 0.0f) s.scale = fmaxf(top / (e5m2 ? 57344.0f : 448.0f), 1.17549435e-38f);
+    s.divide = false;
+    if (!pow2) {
+        s.scale = top == 0.0f ? 1.0f : fmaxf(top / (e5m2 ? 57344.0f : 448.0f), 1.17549435e-38f);
+        s.inverse = 1.0f / s.scale;
+        s.divide = s.scale < 7.9e-31f || (__float_as_uint(s.scale) & 0x7fffffu) == 0x7fffffu;
+    }
     return s;
+}
+// f over the scale as a division rounds it, in three operations: with r = 1 / scale rounded to nearest, q = f r is within one step of the
+// quotient, f - q scale is exact, and q + r (f - q scale) rounds to the quotient's nearest (Markstein, 1990) unless scale's bits are
+// all ones or the remainder falls below the smallest numbers; those take the division.
+__device__ __forceinline__ float vec_quotient(float f, const VecScale &s) {
+    const float q = f * s.inverse;
+    return __fmaf_rn(__fmaf_rn(-q, s.scale, f), s.inverse, q);
 }
 // Eight values over the scale, to 8 bits each (an infinity is made NaN where the type has none).
 __device__ __forceinline__ uint64_t vec_to8(vec_f8 f, const VecScale &s, bool e5m2, bool pow2) {
     float v[8];
+    if (pow2) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = pow2 ? f[i] * s.inverse : f[i] / s.scale;
+        for (int i = 0; i < 8; ++i) v[i] = f[i] * s.inverse;
+    } else if (__builtin_expect(s.divide, 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = f[i] / s.scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fabsf(f[i]) < INFINITY ? vec_quotient(f[i], s) : f[i];
+    }
     int lo = 0, hi = 0;
     if (e5m2) {
         lo = __builtin_amdgcn_cvt_pk_bf8_f32(v[0], v[1], lo, false);

@@ -73,9 +73,11 @@ k_vec_quantize_t(const T *__restrict__ x, int64_t ld, int64_t n, int64_t d, int6
     }
     __syncthreads();
     const int64_t left = n - row0;
-    for (int e = threadIdx.x; e < VEC_BLOCK * 16; e += 256) {
-        const int c = e / 16, p = (e & 15) * 8;
-        if (col0 + c < d && p < left) vec_store_bytes(o.q + (col0 + c) * o.ld_q + row0 + p, left - p, *(uint64_t *)(tile + c * QT_LD + p));
+#pragma unroll
+    for (int u = 0; u < VEC_BLOCK * 8 / 256; ++u) {
+        const int e = u * 256 + threadIdx.x, c = e / 8, p = (e & 7) * 16;
+        typedef int at8 __attribute__((ext_vector_type(4), aligned(8)));
+        if (col0 + c < d && p < left) vec_store_bytes(o.q + (col0 + c) * o.ld_q + row0 + p, left - p, (vec_i4) * (at8 *)(tile + c * QT_LD + p));
     }
 }
 
