@@ -74,14 +74,18 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 // are read once per block, from the L2 cache.
 //
 // Many: the positions are sorted by id (a stable radix sort of up to 2^GRAD_BITS buckets a pass), then summed in pieces
-// of GRAD_CHUNK sorted positions, whatever ids they hold, so that a frequent id is no wave's alone; sums of ids that cross
-// a piece's ends are joined by the kernel that also writes the rows without an id.
+// of at most GRAD_CHUNK sorted positions, whatever ids they hold, so that a frequent id is no wave's alone; sums of ids that cross
+// a piece's ends are joined by a last kernel.  The sort's kernels wait for memory most of the time: blocks beside theirs clear the
+// table meanwhile, a share in each launch.
 //
 // A row is spread over the 64 lanes of a wave, E elements each (2, 4 or 8, the fewest that hold it, else 64 E columns at a time).
-#define GRAD_FEW 4096
+// us, one launch / sorted: 2,048 ids into 65,536 x 256 21 / 60, 4,096 25 / 57, 8,192 44 / 46; tables that one pass sorts: 883 into 623 x 2944 21 / 43,
+// 4,000 54 / 43, 4,000 into 623 x 128 20 / 22
+#define GRAD_POS 12  // bits of a position
+#define GRAD_FEW (1 << GRAD_POS)
 #define GRAD_BITS 10
-#define GRAD_TILE 1024   // keys a block of the sort takes: four per thread
-#define GRAD_CHUNK 64
+#define GRAD_TILE 4096   // keys that a block of 1024 threads of the sort takes
+#define GRAD_CHUNK 64    // at most: shorter pieces, more waves where there are few (16,384 ids into 65,536 x 256: 18 us with 64)
 
 #define GRAD_WIDTHS(d, ...)          \
     do {                             \
@@ -100,21 +104,23 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 struct GradPlan {
     bool few;
     int passes, bits;   // of the sort
-    int tiles, chunks;  // blocks of a pass; pieces of the sum
+    int tiles, chunks;  // blocks of a pass; pieces of the sum,
+    int len;            // so many positions each
     int dpad;           // floats of a partial row
-    size_t key0, key1, pos0, pos1, counts, totals, bounds, part, total;
+    size_t key0, key1, pos0, pos1, counts, begins, part, total;
 };
 
 static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
     GradPlan p = {};
-    p.few = n <= GRAD_FEW;
+    p.few = n <= (rows < (1 << GRAD_BITS) ? GRAD_FEW / 2 : GRAD_FEW);
     if (p.few) return p;
     int bits = 1;
     while (((int64_t)1 << bits) <= rows) ++bits;  // ids 0..rows, `rows` standing for those that take no part
     p.passes = (bits + GRAD_BITS - 1) / GRAD_BITS;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tiles = (int)((n + GRAD_TILE - 1) / GRAD_TILE);
-    p.chunks = (int)((n + GRAD_CHUNK - 1) / GRAD_CHUNK);
+    p.len = n <= 32768 ? GRAD_CHUNK / 4 : (n <= 131072 ? GRAD_CHUNK / 2 : GRAD_CHUNK);
+    p.chunks = (int)((n + p.len - 1) / p.len);
     p.dpad = (d + 7) & ~7;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
@@ -123,8 +129,7 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
     p.pos0 = take((size_t)n * 4);
     p.pos1 = take((size_t)n * 4);
     p.counts = take(((size_t)p.tiles << p.bits) * 4);
-    p.totals = take(((size_t)1 << p.bits) * 4);
-    p.bounds = take((size_t)rows * 8);
+    p.begins = take((size_t)rows * 4);
     p.part = take((size_t)p.chunks * 2 * p.dpad * 4);
     p.total = at;
     return p;
@@ -144,123 +149,147 @@ __device__ __forceinline__ void grad_write(TT *__restrict__ row, int64_t col, in
     vec_store<TT, E>(row + col, left, f);
 }
 
-// Zeros in those of `nrow` rows whose bit of `has` is not set; row(r): address of the r-th.
-template <class TT, class ROW>
-__device__ __forceinline__ void grad_zeros(int nrow, int d, const uint32_t *has, ROW row) {
-    const int pieces = (d + 7) / 8;
+// Zeros in the first `cols` columns of those of `nrow` rows whose bit of `has` is not set; row(r): where the r-th begins.
+template <class TT, int NT, class ROW>
+__device__ __forceinline__ void grad_zeros(int nrow, int cols, const uint32_t *has, ROW row) {
+    const int pieces = (cols + 7) / 8;
     int r = threadIdx.x / pieces, c = threadIdx.x - r * pieces;
-    const int dr = 256 / pieces, dc = 256 - dr * pieces;
+    const int dr = NT / pieces, dc = NT - dr * pieces;
     while (r < nrow) {
-        if (!(has[r >> 5] >> (r & 31) & 1)) vec_store<TT>(row(r) + c * 8, d - c * 8, (vec_f8)0.0f);
+        if (!(has[r >> 5] >> (r & 31) & 1)) vec_store<TT>(row(r) + c * 8, cols - c * 8, (vec_f8)0.0f);
         r += dr;
         c += dc;
         if (c >= pieces) c -= pieces, ++r;
     }
 }
 
-// Adds to acc the rows of grad at the positions (low 12 bits) of those of list[0 .. m - 1] that are of row r (the bits above), in order.
+// Adds to acc the rows of grad at the positions (low GRAD_POS bits) of those of list[0 .. m - 1] that are of row r (the bits above), in order.
 template <class TG, int E>
 __device__ __forceinline__ void grad_pick(const TG *__restrict__ grad, int64_t ld, int64_t col, int64_t left, const uint32_t *list, int m,
                                           uint32_t r, vec_f<E> &acc) {
     const int lane = threadIdx.x & 63;
     for (int i0 = 0; i0 < m; i0 += 64) {
         const uint32_t e = i0 + lane < m ? list[i0 + lane] : 0xffffffffu;
-        uint64_t hits = __ballot(e >> 12 == r);
+        uint64_t hits = __ballot(e >> GRAD_POS == r);
         while (hits) {
-            vec_pack<TG, E> v[8];
+            constexpr int B = sizeof(TG) * E <= 16 ? 16 : 8;  // rows on their way
+            vec_pack<TG, E> v[B];
             int k = 0;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < B; ++u) {
                 const int at = hits ? __builtin_ctzll(hits) : 0;
                 const bool more = hits != 0;
                 hits &= hits - 1;
-                const uint32_t pos = __builtin_amdgcn_readlane(e, at) & 4095u;
+                const uint32_t pos = __builtin_amdgcn_readlane(e, at) & (GRAD_FEW - 1);
                 k += more;
                 v[u] = vec_load<TG, E>(grad + (int64_t)pos * ld + col, more ? left : 0);
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < B; ++u)
                 if (u < k) acc += vec_wide<TG, E>(v[u]);
         }
     }
 }
 
-// The block's rows: groups of 2^group neighbouring rows are dealt out over 2^deal blocks.
+// The block's rows: groups of 2^group neighbouring rows are dealt out over 2^deal blocks.  Its columns: 64 E from blockIdx.y 64 E on.
 template <class TG, class TT, class ID, int E>
 __global__ void __launch_bounds__(256)
 k_vec_grad_few(const TG *__restrict__ grad, int n, int d, int64_t ld_grad, const ID *__restrict__ ids, float scale,
                int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int group, int deal, int rpb) {
+    constexpr int WAVES = 4;  // (sixteen: twice the time, 2,048 ids into 65,536 x 256 43 us)
     extern __shared__ __align__(16) unsigned char smem[];
     uint32_t *has = (uint32_t *)smem;           // [(rpb + 31) / 32]
-    uint32_t *list = has + (rpb + 31) / 32;     // [GRAD_FEW] row of the block << 12 | position
-    __shared__ int count[4];
-    __shared__ vec_f<E> quarter[4][64];
+    uint32_t *list = has + (rpb + 31) / 32;     // [n, up to the next 64 WAVES] row of the block << GRAD_POS | position
+    __shared__ int count[WAVES];
+    __shared__ vec_f<E> share[WAVES][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int col0 = (int)blockIdx.y * 64 * E, col = col0 + lane * E, cols = d - col0 < 64 * E ? d - col0 : 64 * E;
     // row r of the block is row of(r) of the table; its rows below `rows` come first
     auto of = [&](int r) { return ((((int64_t)(r >> group) << deal) + blockIdx.x) << group) + (r & ((1 << group) - 1)); };
     int nrow = rpb;
     while (nrow > 0 && of(nrow - 1) >= rows) --nrow;
-    for (int i = threadIdx.x; i < (rpb + 31) / 32; i += 256) has[i] = 0;
-    // each wave takes a quarter of the positions, all loads at once, and keeps the block's own, in order, in its quarter of the list
-    const int per = (n + 255) / 256 * 64, from = wave * per;
-    int64_t id[GRAD_FEW / 256];
-#pragma unroll
-    for (int u = 0; u < GRAD_FEW / 256; ++u) {
-        const int i = from + u * 64 + lane;
-        id[u] = u * 64 < per && i < n ? (int64_t)ids[i] : -1;
-    }
+    for (int i = threadIdx.x; i < (rpb + 31) / 32; i += 64 * WAVES) has[i] = 0;
     __syncthreads();
+    // each wave takes its share of the positions, sixteen loads at once, and keeps the block's own, in order, in its share of the list
+    const int per = (n + 64 * WAVES - 1) / (64 * WAVES) * 64, from = wave * per;
     int m = 0;
+    for (int i0 = from; i0 < from + per; i0 += 1024) {
+        int64_t id[16];
 #pragma unroll
-    for (int u = 0; u < GRAD_FEW / 256; ++u) {
-        const bool mine = id[u] >= 0 && id[u] < rows && ((id[u] >> group) & ((1 << deal) - 1)) == blockIdx.x;
-        const uint64_t b = __ballot(mine);
-        if (!b) continue;
-        if (mine) {
-            const int r = (int)(id[u] >> (group + deal) << group) + (int)(id[u] & ((1 << group) - 1));
-            list[from + m + __popcll(b & ((1ull << lane) - 1))] = (uint32_t)r << 12 | (uint32_t)(from + u * 64 + lane);
-            atomicOr(&has[r >> 5], 1u << (r & 31));
+        for (int u = 0; u < 16; ++u) {
+            const int i = i0 + u * 64 + lane;
+            id[u] = i < from + per && i < n ? (int64_t)ids[i] : -1;
         }
-        m += __popcll(b);
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            const bool mine = id[u] >= 0 && id[u] < rows && ((id[u] >> group) & ((1 << deal) - 1)) == blockIdx.x;
+            const uint64_t b = __ballot(mine);
+            if (!b) continue;
+            if (mine) {
+                const int r = (int)(id[u] >> (group + deal) << group) + (int)(id[u] & ((1 << group) - 1));
+                list[from + m + __popcll(b & ((1ull << lane) - 1))] = (uint32_t)r << GRAD_POS | (uint32_t)(i0 + u * 64 + lane);
+                atomicOr(&has[r >> 5], 1u << (r & 31));
+            }
+            m += __popcll(b);
+        }
     }
     if (lane == 0) count[wave] = m;
     __syncthreads();
-    if (!accumulate) grad_zeros<TT>(nrow, d, has, [&](int r) { return table + of(r) * ld_table; });
-    const int all = count[0] + count[1] + count[2] + count[3];
+    if (!accumulate) grad_zeros<TT, 64 * WAVES>(nrow, cols, has, [&](int r) { return table + of(r) * ld_table + col0; });
+    int all = 0;
+#pragma unroll
+    for (int q = 0; q < WAVES; ++q) all += count[q];
     if (all == 0) return;
     int turn = 0;
     for (int w = 0; w < (nrow + 31) / 32; ++w) {
         for (uint32_t bits = has[w]; bits; bits &= bits - 1) {
             const int r = w * 32 + __builtin_ctz(bits);
             TT *row = table + of(r) * ld_table;
+            vec_f<E> acc = (vec_f<E>)0.0f;
             if (all <= 64) {  // a wave per row
-                if ((turn++ & 3) != wave) continue;
-                for (int col0 = 0; col0 < d; col0 += 64 * E) {
-                    const int col = col0 + lane * E;
-                    vec_f<E> acc = (vec_f<E>)0.0f;
-                    for (int q = 0; q < 4; ++q) grad_pick<TG, E>(grad, ld_grad, col, d - col, list + q * per, count[q], r, acc);
+                if ((turn++ & (WAVES - 1)) != wave) continue;
+                for (int q = 0; q < WAVES; ++q) grad_pick<TG, E>(grad, ld_grad, col, d - col, list + q * per, count[q], r, acc);
+                grad_write<TT, E>(row, col, d - col, acc, scale, accumulate);
+            } else {  // frequent ids: each wave its share of the positions
+                grad_pick<TG, E>(grad, ld_grad, col, d - col, list + from, m, r, acc);
+                share[wave][lane] = acc;
+                __syncthreads();
+                if (wave == 0) {
+#pragma unroll
+                    for (int q = 1; q < WAVES; ++q) acc += share[q][lane];
                     grad_write<TT, E>(row, col, d - col, acc, scale, accumulate);
                 }
-            } else {  // frequent ids: each wave its quarter of the positions
-                for (int col0 = 0; col0 < d; col0 += 64 * E) {
-                    const int col = col0 + lane * E;
-                    vec_f<E> acc = (vec_f<E>)0.0f;
-                    grad_pick<TG, E>(grad, ld_grad, col, d - col, list + from, m, r, acc);
-                    quarter[wave][lane] = acc;
-                    __syncthreads();
-                    if (wave == 0) {
-#pragma unroll
-                        for (int q = 1; q < 4; ++q) acc += quarter[q][lane];
-                        grad_write<TT, E>(row, col, d - col, acc, scale, accumulate);
-                    }
-                    __syncthreads();
-                }
+                __syncthreads();
             }
         }
     }
 }
 
-// --- the sort.  counts[bucket][tile] -> where a tile's keys of a bucket go within it; totals[bucket] -> where a bucket begins
+// --- the sort.  counts[tile][bucket]
+
+// Clears rows: the blocks of a launch from `after` on take `each` rows, from `lo` on.
+struct GradClear {
+    void *table;
+    int64_t lo, hi, ld;
+    int d, each, after;
+};
+template <class TT>
+__device__ __forceinline__ bool grad_clear(const GradClear &z) {
+    if ((int)blockIdx.x < z.after) return false;
+    const int64_t lo = z.lo + (int64_t)((int)blockIdx.x - z.after) * z.each, hi = lo + z.each < z.hi ? lo + z.each : z.hi;
+    const int pieces = (z.d + 7) / 8;
+    TT *row = (TT *)z.table + lo * z.ld;
+    int r = threadIdx.x / pieces, c = threadIdx.x - r * pieces;
+    const int dr = 1024 / pieces, dc = 1024 - dr * pieces;
+    while (r < hi - lo) {
+        vec_store<TT>(row + r * z.ld + c * 8, z.d - c * 8, (vec_f8)0.0f);
+        r += dr;
+        c += dc;
+        if (c >= pieces) c -= pieces, ++r;
+    }
+    return true;
+}
+
 template <class ID>
 __device__ __forceinline__ uint32_t grad_key(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, int64_t i, int64_t rows) {
     if (keys) return keys[i];
@@ -268,76 +297,64 @@ __device__ __forceinline__ uint32_t grad_key(const ID *__restrict__ ids, const u
     return id >= 0 && id < rows ? (uint32_t)id : (uint32_t)rows;
 }
 
-template <class ID>
-__global__ void __launch_bounds__(256)
+#define GRAD_PER (GRAD_TILE / 1024)
+template <class ID, class TT>
+__global__ void __launch_bounds__(1024)
 k_vec_grad_count(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, int64_t n, int64_t rows, int shift, int bits,
-                 uint32_t *__restrict__ counts, int tiles, uint2 *__restrict__ bounds) {
+                 uint32_t *__restrict__ counts, GradClear z) {
+    if (grad_clear<TT>(z)) return;
     __shared__ uint32_t h[1 << GRAD_BITS];
     const int nb = 1 << bits;
-    for (int i = threadIdx.x; i < nb; i += 256) h[i] = 0;
-    __syncthreads();
-    for (int u = 0; u < GRAD_TILE / 256; ++u) {
-        const int64_t i = (int64_t)blockIdx.x * GRAD_TILE + u * 256 + threadIdx.x;
-        if (i < n) atomicAdd(&h[grad_key(ids, keys, i, rows) >> shift & (nb - 1)], 1u);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < nb; i += 256) counts[(size_t)i * tiles + blockIdx.x] = h[i];
-    if (bounds)  // (first pass: no row has an id yet)
-        for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v < rows; v += (int64_t)gridDim.x * 256) bounds[v] = make_uint2(0, 0);
-}
-
-// a wave per bucket: running sums over the tiles
-__global__ void __launch_bounds__(256)
-k_vec_grad_scan(uint32_t *__restrict__ counts, int tiles, int nb, uint32_t *__restrict__ totals) {
-    const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (b >= nb) return;
-    uint32_t *c = counts + (size_t)b * tiles, sum = 0;
-    for (int t0 = 0; t0 < tiles; t0 += 64) {
-        const uint32_t v = t0 + lane < tiles ? c[t0 + lane] : 0;
-        uint32_t s = v;
+    const int64_t first = (int64_t)blockIdx.x * GRAD_TILE + threadIdx.x;
+    uint32_t key[GRAD_PER];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t x = __shfl_up(s, o);
-            if (lane >= o) s += x;
-        }
-        if (t0 + lane < tiles) c[t0 + lane] = sum + s - v;
-        sum += __shfl(s, 63);
-    }
-    if (lane == 0) totals[b] = sum;
+    for (int u = 0; u < GRAD_PER; ++u) key[u] = first + u * 1024 < n ? grad_key(ids, keys, first + u * 1024, rows) : 0;
+    if ((int)threadIdx.x < nb) h[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < GRAD_PER; ++u)
+        if (first + u * 1024 < n) atomicAdd(&h[key[u] >> shift & (nb - 1)], 1u);
+    __syncthreads();
+    if ((int)threadIdx.x < nb) counts[((size_t)blockIdx.x << bits) + threadIdx.x] = h[threadIdx.x];
 }
 
-// A tile's keys to their places: those of one bucket keep their order.  Wave w holds the tile's w-th quarter, 64 keys at a
-// time; a key's rank among them is the number of lower lanes with the same bucket, found bit by bit with ballots.
-template <class ID>
-__global__ void __launch_bounds__(256)
+// A tile's keys to their places: those of one bucket keep their order.  Thread b adds up the sizes of bucket b over the tiles, of those
+// before this one and of all; running sums over the buckets then say where the tile's keys go.  (A kernel of its own for these sums
+// took 5 us, the loads here about 2.)  Wave w holds the tile's w-th sixteenth, 64 keys at a time; a key's rank among them is
+// the number of lower lanes with the same bucket, found bit by bit with ballots.
+template <class ID, class TT>
+__global__ void __launch_bounds__(1024)
 k_vec_grad_place(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos, int64_t n,
                  int64_t rows, int shift, int bits, const uint32_t *__restrict__ counts, int tiles,
-                 const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out) {
-    __shared__ uint32_t next[4][1 << GRAD_BITS];  // per wave: where its next key of a bucket goes
-    __shared__ uint32_t part[4];
+                 uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out, GradClear z) {
+    if (grad_clear<TT>(z)) return;
+    extern __shared__ uint32_t next[];  // [16 waves][buckets]: a wave's keys of a bucket, then where its next one goes
+    __shared__ uint32_t part[16];
     const int nb = 1 << bits, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int i = threadIdx.x; i < 4 * nb; i += 256) next[i >> bits][i & (nb - 1)] = 0;
-    __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * GRAD_TILE + wave * (GRAD_TILE / 4);
-    uint32_t key[GRAD_TILE / 256], bucket[GRAD_TILE / 256];
+    const int64_t first = (int64_t)blockIdx.x * GRAD_TILE + wave * (GRAD_TILE / 16) + lane;
+    uint32_t key[GRAD_PER], from[GRAD_PER];
 #pragma unroll
-    for (int u = 0; u < GRAD_TILE / 256; ++u) {
-        const int64_t i = first + u * 64 + lane;
+    for (int u = 0; u < GRAD_PER; ++u) {
+        const int64_t i = first + u * 64;
         key[u] = i < n ? grad_key(ids, keys, i, rows) : 0;
-        bucket[u] = key[u] >> shift & (nb - 1);
-        if (i < n) atomicAdd(&next[wave][bucket[u]], 1u);
+        from[u] = i < n && pos ? pos[i] : (uint32_t)i;
     }
+    uint32_t before_tile = 0, total = 0;
+    if ((int)threadIdx.x < nb) {
+        const uint32_t *c = counts + threadIdx.x;
+#pragma unroll 16
+        for (int t = 0; t < tiles; ++t) {
+            const uint32_t v = c[(size_t)t << bits];
+            total += v;
+            before_tile += t < (int)blockIdx.x ? v : 0;
+        }
+    }
+    for (int i = threadIdx.x; i < 16 * nb; i += 1024) next[i] = 0;
     __syncthreads();
-    // where each bucket begins: running sums over the totals, four buckets per thread at most
-    const int per = (nb + 255) / 256;
-    uint32_t mine[(1 << GRAD_BITS) / 256], sum = 0;
 #pragma unroll
-    for (int j = 0; j < (1 << GRAD_BITS) / 256; ++j) {
-        const int b = threadIdx.x * per + j;
-        mine[j] = j < per && b < nb ? totals[b] : 0;
-        sum += mine[j];
-    }
-    uint32_t s = sum;
+    for (int u = 0; u < GRAD_PER; ++u)
+        if (first + u * 64 < n) atomicAdd(&next[(wave << bits) + (key[u] >> shift & (nb - 1))], 1u);
+    uint32_t s = total;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t x = __shfl_up(s, o);
@@ -345,65 +362,57 @@ k_vec_grad_place(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, 
     }
     if (lane == 63) part[wave] = s;
     __syncthreads();
-    uint32_t before = s - sum;
-    for (int w = 0; w < wave; ++w) before += part[w];
+    if ((int)threadIdx.x < nb) {
+        uint32_t at = s - total + before_tile;
+        for (int w = 0; w < wave; ++w) at += part[w];
 #pragma unroll
-    for (int j = 0; j < (1 << GRAD_BITS) / 256; ++j) {
-        const int b = threadIdx.x * per + j;
-        if (j < per && b < nb) {
-            uint32_t at = before + counts[(size_t)b * tiles + blockIdx.x];
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t c = next[w][b];
-                next[w][b] = at;
-                at += c;
-            }
+        for (int w = 0; w < 16; ++w) {
+            const uint32_t c = next[(w << bits) + threadIdx.x];
+            next[(w << bits) + threadIdx.x] = at;
+            at += c;
         }
-        before += mine[j];
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < GRAD_TILE / 256; ++u) {
-        const int64_t i = first + u * 64 + lane;
-        const bool in = i < n;
+    for (int u = 0; u < GRAD_PER; ++u) {
+        const bool in = first + u * 64 < n;
+        const uint32_t bucket = key[u] >> shift & (nb - 1);
+        uint32_t *mine = &next[(wave << bits) + bucket];
         uint64_t same = __ballot(in);
         for (int b = 0; b < bits; ++b) {
-            const uint64_t x = __ballot(bucket[u] >> b & 1);
-            same &= bucket[u] >> b & 1 ? x : ~x;
+            const uint64_t x = __ballot(bucket >> b & 1);
+            same &= bucket >> b & 1 ? x : ~x;
         }
         if (in) {
-            const int rank = __popcll(same & ((1ull << lane) - 1));
-            const uint32_t at = next[wave][bucket[u]] + rank;
+            const uint32_t at = *mine + __popcll(same & ((1ull << lane) - 1));
             keys_out[at] = key[u];
-            pos_out[at] = pos ? pos[i] : (uint32_t)i;
+            pos_out[at] = from[u];
         }
         __builtin_amdgcn_wave_barrier();  // the reads above come before the wave's own update
-        if (in && (same >> lane) == 1) next[wave][bucket[u]] += __popcll(same);  // the bucket's last lane
+        if (in && (same >> lane) == 1) *mine += __popcll(same);  // the bucket's last lane
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-// --- the sums.  A wave per piece of GRAD_CHUNK sorted positions and 64 E columns: ids that lie within the piece are written to
-// the table; the sum of one that began before goes to part[chunk][0], that of one that begins here and goes on to part[chunk][1].  bounds[v]: first and last + 1 sorted position of id v.
+// --- the sums.  A wave per piece of `len` sorted positions and 64 E columns: ids that lie within the piece are written to
+// the table; the sum of one that began before goes to part[chunk][0], that of one that begins here and goes on to part[chunk][1].  begins[v]: first sorted position of id v.
 // Rows are requested eight at a time, whatever ids they are of, eight ahead of those that are added.
 template <class TG, class TT, int E>
 __global__ void __launch_bounds__(256)
 k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uint32_t *__restrict__ keys,
                   const uint32_t *__restrict__ pos, int64_t n, int64_t rows, float scale, int accumulate,
-                  TT *__restrict__ table, int64_t ld_table, uint2 *__restrict__ bounds, float *__restrict__ part, int dpad, int chunks) {
+                  TT *__restrict__ table, int64_t ld_table, uint32_t *__restrict__ begins, float *__restrict__ part, int dpad, int chunks, int len) {
     const int chunk = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (chunk >= chunks) return;
-    const int64_t first = (int64_t)chunk * GRAD_CHUNK;
-    int m = (int)(n - first < GRAD_CHUNK ? n - first : GRAD_CHUNK);
+    const int64_t first = (int64_t)chunk * len;
+    int m = (int)(n - first < len ? n - first : len);
     const uint32_t none = 0xffffffffu;
     const uint32_t key = lane < m ? keys[first + lane] : none, p = lane < m ? pos[first + lane] : 0;
     const uint32_t prev = lane < m && first + lane > 0 ? keys[first + lane - 1] : none;
     const uint32_t next = lane < m && first + lane + 1 < n ? keys[first + lane + 1] : none;
-    const bool begins = lane < m && key != prev, ends = lane < m && key != next;
-    if (blockIdx.y == 0 && key < (uint64_t)rows) {
-        if (begins) bounds[key].x = (uint32_t)(first + lane);
-        if (ends) bounds[key].y = (uint32_t)(first + lane) + 1;
-    }
-    const uint64_t heads = __ballot(begins), tails = __ballot(ends);
+    const bool head = lane < m && key != prev, tail = lane < m && key != next;
+    if (blockIdx.y == 0 && head && key < (uint64_t)rows) begins[key] = (uint32_t)(first + lane);
+    const uint64_t heads = __ballot(head), tails = __ballot(tail);
     m = __popcll(__ballot(key < (uint64_t)rows));  // (ids that take no part come last)
     const int col = (int)blockIdx.y * 64 * E + lane * E, left = d - col;
     const TG *g = grad + col;
@@ -437,54 +446,52 @@ k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uin
         *(vec_f<E> *)(part + ((int64_t)chunk * 2 + (whole ? 1 : 0)) * dpad + col) = acc;
 }
 
-// The first `chunks` blocks of a row of the grid: the run that ends in the piece and began before it, its partial sums added in order, a
-// quarter of them per wave if they are many.  The other blocks: the rows without an id, GRAD_END_ROWS each.
-#define GRAD_END_ROWS 64
+// The run that ends in a piece and began before it: its partial sums added in order, by a wave, or by the block, a quarter of them per
+// wave, if they are many.  64 E columns from blockIdx.y 64 E on.
+#define GRAD_JOIN_ALONE 16
 template <class TT, int E>
 __global__ void __launch_bounds__(256)
-k_vec_grad_end(const uint32_t *__restrict__ keys, int64_t n, const uint2 *__restrict__ bounds, const float *__restrict__ part, int dpad,
-               int d, float scale, int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int chunks) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if ((int64_t)blockIdx.x >= chunks) {
-        __shared__ uint32_t has[GRAD_END_ROWS / 32];
-        const int64_t lo = ((int64_t)blockIdx.x - chunks) * GRAD_END_ROWS;
-        const int nrow = (int)(rows - lo < GRAD_END_ROWS ? rows - lo : GRAD_END_ROWS);
-        if (threadIdx.x < 64) {
-            const uint2 b = lane < nrow ? bounds[lo + lane] : make_uint2(0, 0);
-            const uint64_t h = __ballot(b.y > b.x);
-            if (lane < 2) has[lane] = (uint32_t)(h >> (32 * lane));
-        }
-        __syncthreads();
-        grad_zeros<TT>(nrow, d, has, [&](int r) { return table + (lo + r) * ld_table; });
-        return;
-    }
+k_vec_grad_join(const uint32_t *__restrict__ keys, int64_t n, const uint32_t *__restrict__ begins, const float *__restrict__ part, int dpad,
+                int d, float scale, int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int chunks, int len) {
     __shared__ vec_f<E> quarter[4][64];
-    const int chunk = blockIdx.x;
-    const int64_t first = (int64_t)chunk * GRAD_CHUNK;
-    const uint32_t key = keys[first];
-    if (chunk == 0 || key >= (uint64_t)rows || keys[first - 1] != key) return;
-    const uint2 b = bounds[key];
-    if ((b.y - 1) / GRAD_CHUNK != (uint32_t)chunk) return;  // (a later block's)
-    const int c0 = (int)(b.x / GRAD_CHUNK);
-    const int cnt = chunk - c0 + 1, each = cnt <= 8 ? cnt : (cnt + 3) / 4;
-    if (cnt <= 8 && wave > 0) return;
-    const int from = c0 + wave * each, to = from + each < chunk + 1 ? from + each : chunk + 1;
-    for (int col0 = 0; col0 < d; col0 += 64 * E) {
-        const int col = col0 + lane * E;
+    __shared__ int many[4];  // a wave's run, if the block is to take it: its first piece
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first_chunk = blockIdx.x * 4 + 1, chunk = first_chunk + wave;
+    const int col = (int)blockIdx.y * 64 * E + lane * E;
+    auto sum = [&](int c0, int from, int to) {
         vec_f<E> acc = (vec_f<E>)0.0f;
         if (col < d) {
 #pragma unroll 8
             for (int c = from; c < to; ++c) acc += *(const vec_f<E> *)(part + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * dpad + col);
         }
-        if (cnt > 8) {
-            quarter[wave][lane] = acc;
-            __syncthreads();
-            if (wave == 0)
+        return acc;
+    };
+    auto write = [&](int c, vec_f<E> acc) {
+        grad_write<TT, E>(table + (int64_t)keys[(int64_t)c * len] * ld_table, col, d - col, acc, scale, accumulate);
+    };
+    int c0 = -1;
+    if (chunk < chunks) {
+        const int64_t first = (int64_t)chunk * len, behind = first + len;
+        const uint32_t key = keys[first], prev = keys[first - 1], last = behind < n ? keys[behind - 1] : 0, next = behind < n ? keys[behind] : 1;
+        // (a run that goes on is a later piece's)
+        if (key < (uint64_t)rows && prev == key && !(last == key && next == key)) c0 = (int)(begins[key] / (uint32_t)len);
+    }
+    const bool all = c0 >= 0 && chunk - c0 >= GRAD_JOIN_ALONE;
+    if (lane == 0) many[wave] = all ? c0 : -1;
+    if (c0 >= 0 && !all) write(chunk, sum(c0, c0, chunk + 1));
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) {
+        const int at = many[w], c1 = first_chunk + w + 1;
+        if (at < 0) continue;
+        const int each = (c1 - at + 3) / 4, from = at + wave * each;
+        vec_f<E> acc = sum(at, from, from + each < c1 ? from + each : c1);
+        quarter[wave][lane] = acc;
+        __syncthreads();
+        if (wave == 0) {
 #pragma unroll
-                for (int w = 1; w < 4; ++w) acc += quarter[w][lane];
+            for (int q = 1; q < 4; ++q) acc += quarter[q][lane];
+            write(c1 - 1, acc);
         }
-        if (wave == 0) grad_write<TT, E>(table + (int64_t)key * ld_table, col, d - col, acc, scale, accumulate);
-        if (cnt > 8) __syncthreads();
+        __syncthreads();
     }
 }
 
@@ -510,16 +517,17 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     }
     hipStream_t s = (hipStream_t)stream;
     if (p.few) {
-        // 512 bytes of neighbouring rows together; about 1024 blocks (at most 2^16 rows each: a row of a block shares a word with a position)
+        // 512 bytes of neighbouring rows together; at least about 1024 blocks (at most 2^15 rows each, a group more: a row of a block shares a word with a position)
         int group = 0, deal = 0;
         while (group < 5 && ((int64_t)vec_bytes(table_type) * d << group) < 512) ++group;
-        while (deal < 10 && ((int64_t)4 << group << deal) < rows) ++deal;
+        const int tiles = (d + 511) / 512;  // (of 64 E columns: d > 256 has E = 8)
+        while (((int64_t)tiles << deal) < 1024 && ((int64_t)4 << group << deal) < rows) ++deal;
         while ((rows >> (deal + 15)) > 0) ++deal;
         const int64_t groups = (rows + ((int64_t)1 << group) - 1) >> group, each = (groups + ((int64_t)1 << deal) - 1) >> deal;
         const int rpb = (int)(each << group);
-        const size_t lds = (size_t)((rpb + 31) / 32) * 4 + GRAD_FEW * 4;
+        const size_t lds = (size_t)((rpb + 31) / 32) * 4 + (size_t)(n + 255) / 256 * 256 * 4;
 #define GO(TG, TT, ID, E)                                                                                                  \
-    hipLaunchKernelGGL((k_vec_grad_few<TG, TT, ID, E>), dim3(1u << deal), dim3(256), lds, s, (const TG *)grad, (int)n, d,  \
+    hipLaunchKernelGGL((k_vec_grad_few<TG, TT, ID, E>), dim3(1u << deal, (unsigned)tiles), dim3(256), lds, s, (const TG *)grad, (int)n, d, \
                        ld_grad, (const ID *)ids, scale, accumulate, (TT *)table_grad, rows, ld_table, group, deal, rpb)
         VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, if (id_bytes == 4) GO(TG, TT, int32_t, E); else GO(TG, TT, int64_t, E))));
 #undef GO
@@ -528,32 +536,46 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     }
     char *ws = (char *)workspace;
     uint32_t *key[2] = {(uint32_t *)(ws + p.key0), (uint32_t *)(ws + p.key1)}, *pos[2] = {(uint32_t *)(ws + p.pos0), (uint32_t *)(ws + p.pos1)};
-    uint32_t *counts = (uint32_t *)(ws + p.counts), *totals = (uint32_t *)(ws + p.totals);
-    uint2 *bounds = (uint2 *)(ws + p.bounds);
+    uint32_t *counts = (uint32_t *)(ws + p.counts);
+    uint32_t *begins = (uint32_t *)(ws + p.begins);
     float *part = (float *)(ws + p.part);
-    const int nb = 1 << p.bits;
+    const int launches = 2 * p.passes;
+    int launch = 0;
+    // a launch's share of the rows to clear, 32 KB and more a block
+    const size_t row_bytes = vec_bytes(table_type) * (size_t)d;
+    GradClear z = {table_grad, 0, 0, ld_table, d, (int)(row_bytes >= 32768 ? 1 : 32768 / row_bytes), 0};
+    auto share = [&](unsigned own) {
+        z.after = (int)own;
+        z.lo = z.hi;
+        z.hi = accumulate ? 0 : rows / launches * ++launch + (launch == launches ? rows % launches : 0);
+        int64_t blocks = (z.hi - z.lo + z.each - 1) / z.each;
+        while (blocks > (1 << 20)) {
+            z.each *= 2;
+            blocks = (z.hi - z.lo + z.each - 1) / z.each;
+        }
+        return dim3(own + (unsigned)blocks);
+    };
     for (int pass = 0; pass < p.passes; ++pass) {
         const uint32_t *ki = pass ? key[(pass - 1) & 1] : nullptr, *pi = pass ? pos[(pass - 1) & 1] : nullptr;
         const int shift = pass * p.bits;
-#define GO(ID)                                                                                                             \
-    do {                                                                                                                   \
-        hipLaunchKernelGGL(k_vec_grad_count<ID>, dim3(p.tiles), dim3(256), 0, s, (const ID *)ids, ki, n, rows, shift, p.bits, counts, \
-                           p.tiles, pass ? (uint2 *)nullptr : bounds);                                                     \
-        hipLaunchKernelGGL(k_vec_grad_scan, dim3((nb + 3) / 4), dim3(256), 0, s, counts, p.tiles, nb, totals);             \
-        hipLaunchKernelGGL(k_vec_grad_place<ID>, dim3(p.tiles), dim3(256), 0, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
-                           counts, p.tiles, totals, key[pass & 1], pos[pass & 1]);                                         \
+        dim3 grid;
+#define GO(ID, TT)                                                                                                          \
+    do {                                                                                                                    \
+        grid = share((unsigned)p.tiles);                                                                                    \
+        hipLaunchKernelGGL((k_vec_grad_count<ID, TT>), grid, dim3(1024), 0, s, (const ID *)ids, ki, n, rows, shift, p.bits, counts, z); \
+        grid = share((unsigned)p.tiles);                                                                                    \
+        hipLaunchKernelGGL((k_vec_grad_place<ID, TT>), grid, dim3(1024), (size_t)64 << p.bits, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
+                           counts, p.tiles, key[pass & 1], pos[pass & 1], z);                                               \
     } while (0)
-        if (id_bytes == 4) GO(int32_t);
-        else GO(int64_t);
+        VEC_TYPED(table_type, TT, if (id_bytes == 4) GO(int32_t, TT); else GO(int64_t, TT));
 #undef GO
     }
     const uint32_t *ks = key[(p.passes - 1) & 1], *ps = pos[(p.passes - 1) & 1];
     VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL(
         (k_vec_grad_chunks<TG, TT, E>), dim3((unsigned)((p.chunks + 3) / 4), (unsigned)((d + 64 * E - 1) / (64 * E))), dim3(256), 0, s, (const TG *)grad,
-        d, ld_grad, ks, ps, n, rows, scale, accumulate, (TT *)table_grad, ld_table, bounds, part, p.dpad, p.chunks))));
-    const int64_t zeros = accumulate ? 0 : (rows + GRAD_END_ROWS - 1) / GRAD_END_ROWS;
-    VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL((k_vec_grad_end<TT, E>), dim3((unsigned)(p.chunks + zeros)), dim3(256), 0, s, ks, n,
-                                                                bounds, part, p.dpad, d, scale, accumulate, (TT *)table_grad, rows, ld_table, p.chunks)));
+        d, ld_grad, ks, ps, n, rows, scale, accumulate, (TT *)table_grad, ld_table, begins, part, p.dpad, p.chunks, p.len))));
+    VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL((k_vec_grad_join<TT, E>), dim3((unsigned)(p.chunks + 2) / 4, (unsigned)((d + 64 * E - 1) / (64 * E))),
+                                                                dim3(256), 0, s, ks, n, begins, part, p.dpad, d, scale, accumulate, (TT *)table_grad, rows, ld_table, p.chunks, p.len)));
     QADC_LAUNCH_CHECK("vec_lookup_grad's kernels");
     return PQ_OK;
 }
