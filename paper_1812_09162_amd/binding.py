@@ -497,11 +497,11 @@ class _Call:
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.index)  # (entered around allocations and the launch)
             self.raw = self.stream.cuda_stream
 
-    def empty(self, shape, dtype) -> torch.Tensor:
+    def empty(self, dtype, *shape) -> torch.Tensor:
         if self.stream is not None:
             with torch.cuda.stream(self.stream):
-                return torch.empty(shape, dtype=dtype, device=self.device)
-        return torch.empty(shape, dtype=dtype, device=self.device)
+                return torch.empty(*shape, dtype=dtype, device=self.device)
+        return torch.empty(*shape, dtype=dtype, device=self.device)
 
     def rows(self, what: str, t: torch.Tensor, n: int, d: int, dtype):
         """Address of a matrix [n, d] and the distance of its rows, checked."""
@@ -534,7 +534,7 @@ class _Call:
         if t is None:
             if nbytes == 0:
                 return None, 0, None
-            t = self.empty(nbytes, torch.uint8)
+            t = self.empty(torch.uint8, nbytes)
             return t.data_ptr(), nbytes, t
         return self.vector("workspace", t), t.numel() * t.element_size(), t
 
@@ -576,7 +576,7 @@ def vec_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype
     n = ids.numel()
     to = call.out_type(out, dtype, table.dtype)
     if out is None:
-        out = call.empty((*ids.shape, d), to)
+        out = call.empty(to, *ids.shape, d)
         optr, old = out.data_ptr(), d
     else:
         optr, old = call.rows("out", out, n, d, to)
@@ -606,7 +606,7 @@ def vec_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: flo
         _refuse(call.name, "accumulate needs an out to add to")
     to = call.out_type(out, dtype, grad.dtype)
     if out is None:
-        out = call.empty((rows, d), to)
+        out = call.empty(to, rows, d)
         optr, old = out.data_ptr(), d
     else:
         optr, old = call.rows("out", out, rows, d, to)
@@ -628,7 +628,7 @@ def _blocks_out(call: _Call, n: int, d: int, quant, scale_dtype, out):
         q, scales = out
         return (q, scales, *call.rows("q", q, n, d, quant), *call.rows("scales", scales, n, nb, scale_dtype))
     ld = -(-d // 16) * 16
-    q, scales = call.empty((n, ld), quant), call.empty((n, nb), scale_dtype)
+    q, scales = call.empty(quant, n, ld), call.empty(scale_dtype, n, nb)
     return (q if ld == d else q[:, :d]), scales, q.data_ptr(), ld or 1, scales.data_ptr(), nb or 1
 
 
@@ -649,10 +649,10 @@ def vec_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
     y = h = q = scales = None
     if out is None:
         if want_y:
-            y = call.empty((n, d), t)
+            y = call.empty(t, n, d)
             yp, ldy = y.data_ptr(), d
         if residual is not None:
-            h = call.empty((n, d), t)
+            h = call.empty(t, n, d)
             hp, ldh = h.data_ptr(), d
         if quant is not None:
             q, scales, qp, ldq, sp, lds = _blocks_out(call, n, d, quant, scale_dtype, None)
@@ -685,7 +685,7 @@ def vec_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, dh: O
     ep, lde = call.rows("dh", dh, n, d, t) if dh is not None else (None, 0)
     wp = call.vector("weight", weight, d)
     if out is None:
-        dx, dweight = call.empty((n, d), t), call.empty((d,), torch.float32)
+        dx, dweight = call.empty(t, n, d), call.empty(torch.float32, d)
         xp, ldx, dwp = dx.data_ptr(), d, dweight.data_ptr()
     else:
         dx, dweight = out
@@ -725,7 +725,7 @@ def vec_matmul_blocks(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, 
     bsp, ldbs = call.rows("b_scales", b_scales, n, nb, st)
     to = call.out_type(out, dtype, torch.bfloat16)
     if out is None:
-        out = call.empty((m, n), to)
+        out = call.empty(to, m, n)
         cp, ldc = out.data_ptr(), n or 1
     else:
         cp, ldc = call.rows("out", out, m, n, to)

@@ -24,11 +24,34 @@ using vec_pack = typename VecPack<T, E>::type;
 template <int E>
 using vec_f = typename VecPack<float, E>::wide;
 
-// left: elements of the row from p on (those beyond it read as zero and are not touched)
+// The vector's elements from the N-th on, zeros behind.
+template <int N, int E, class V>
+__device__ __forceinline__ V vec_down(V v) {
+    V r = v;
+#pragma unroll
+    for (int i = 0; i < E; ++i) r[i] = i + N < E ? v[i + N] : 0;
+    return r;
+}
+
+// left: elements of the row from p on (those beyond it read as zero and are not touched); before: elements of the row before p.  At the
+// end of a row the last E elements are read and moved into place: one load, where one for each element of odd widths cost half the time of
+// a row of 257.
 template <class T, int E = 8>
-__device__ __forceinline__ vec_pack<T, E> vec_load(const T *p, int64_t left) {
-    if (left >= E) return *(const vec_pack<T, E> *)p;
-    vec_pack<T, E> v = (vec_pack<T, E>)(T)0.0f;
+__device__ __forceinline__ vec_pack<T, E> vec_load(const T *p, int64_t left, int64_t before) {
+    typedef vec_pack<T, E> pack;
+    if (left >= E) return *(const pack *)p;
+    pack v = (pack)(T)0.0f;
+    if (left <= 0) return v;
+    if (before + left >= E) {
+        const int k = E - (int)left;
+        v = *(const pack *)(p - k);
+        if constexpr (E > 4)
+            if (k & 4) v = vec_down<4, E>(v);
+        if constexpr (E > 2)
+            if (k & 2) v = vec_down<2, E>(v);
+        if (k & 1) v = vec_down<1, E>(v);
+        return v;
+    }
 #pragma unroll
     for (int i = 0; i < E - 1; ++i)
         if (i < left) v[i] = p[i];
@@ -38,50 +61,84 @@ template <class T, int E = 8>
 __device__ __forceinline__ vec_f<E> vec_wide(vec_pack<T, E> v) {
     return __builtin_convertvector(v, vec_f<E>);
 }
+// (the end of a row: four, two and one of its elements)
 template <class T, int E = 8>
 __device__ __forceinline__ void vec_store(T *p, int64_t left, vec_f<E> f) {
     typedef vec_pack<T, E> pack;
-    const pack v = __builtin_convertvector(f, pack);
+    pack v = __builtin_convertvector(f, pack);
     if (left >= E) {
         *(pack *)p = v;
         return;
     }
+    if (left <= 0) return;
+    if constexpr (E > 4)
+        if (left & 4) {
+            vec_pack<T, 4> w;
 #pragma unroll
-    for (int i = 0; i < E - 1; ++i)
-        if (i < left) p[i] = v[i];
+            for (int i = 0; i < 4; ++i) w[i] = v[i];
+            *(vec_pack<T, 4> *)p = w;
+            p += 4;
+            v = vec_down<4, E>(v);
+        }
+    if constexpr (E > 2)
+        if (left & 2) {
+            vec_pack<T, 2> w;
+            w[0] = v[0], w[1] = v[1];
+            *(vec_pack<T, 2> *)p = w;
+            p += 2;
+            v = vec_down<2, E>(v);
+        }
+    if (left & 1) *p = v[0];
 }
-// sixteen bytes, eight bytes
+// eight bytes, sixteen bytes
+__device__ __forceinline__ void vec_store_bytes(uint8_t *p, int64_t left, uint64_t v) {
+    typedef uint64_t any64 __attribute__((aligned(1)));
+    typedef uint32_t any32 __attribute__((aligned(1)));
+    typedef uint16_t any16 __attribute__((aligned(1)));
+    if (left >= 8) {
+        *(any64 *)p = v;
+        return;
+    }
+    if (left <= 0) return;
+    if (left & 4) *(any32 *)p = (uint32_t)v, p += 4, v >>= 32;
+    if (left & 2) *(any16 *)p = (uint16_t)v, p += 2, v >>= 16;
+    if (left & 1) *p = (uint8_t)v;
+}
 __device__ __forceinline__ void vec_store_bytes(uint8_t *p, int64_t left, vec_i4 v) {
     typedef int any128 __attribute__((ext_vector_type(4), aligned(1)));
     if (left >= 16) {
         *(any128 *)p = v;
         return;
     }
-    for (int i = 0; i < 15; ++i)
-        if (i < left) p[i] = (uint8_t)(v[i >> 2] >> (8 * (i & 3)));
-}
-__device__ __forceinline__ void vec_store_bytes(uint8_t *p, int64_t left, uint64_t v) {
-    typedef uint64_t any64 __attribute__((aligned(1)));
-    if (left >= 8) {
-        *(any64 *)p = v;
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < left) p[i] = (uint8_t)(v >> (8 * i));
+    vec_store_bytes(p, left, (uint64_t)(uint32_t)v[1] << 32 | (uint32_t)v[0]);
+    vec_store_bytes(p + 8, left - 8, (uint64_t)(uint32_t)v[3] << 32 | (uint32_t)v[2]);
 }
 
-// Sum, or largest, over the LANES (16, 32 or 64) neighbouring lanes of a row; every one of them has the result.
+// Sum, or largest, over the LANES (16, 32 or 64) neighbouring lanes of a row; every one of them has the result.  Sixteen lanes by
+// rotations in the vector unit (both partners of a step add the same two values, so all agree); their sums meet in scalar registers.
+template <int N>
+__device__ __forceinline__ float vec_rotate(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, true));
+}
 template <int LANES>
 __device__ __forceinline__ float vec_sum(float v) {
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) v += __shfl_xor(v, o);
+    v += vec_rotate<8>(v);
+    v += vec_rotate<4>(v);
+    v += vec_rotate<2>(v);
+    v += vec_rotate<1>(v);
+    if constexpr (LANES > 16) {
+        const int u = __float_as_int(v);
+        const float a = __int_as_float(__builtin_amdgcn_readlane(u, 0)) + __int_as_float(__builtin_amdgcn_readlane(u, 16));
+        const float b = __int_as_float(__builtin_amdgcn_readlane(u, 32)) + __int_as_float(__builtin_amdgcn_readlane(u, 48));
+        v = LANES == 64 ? a + b : ((threadIdx.x & 63) < 32 ? a : b);
+    }
     return v;
 }
 __device__ __forceinline__ float vec_max16(float v) {
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    v = fmaxf(v, vec_rotate<8>(v));
+    v = fmaxf(v, vec_rotate<4>(v));
+    v = fmaxf(v, vec_rotate<2>(v));
+    return fmaxf(v, vec_rotate<1>(v));
 }
 
 // The largest finite magnitude of eight values.

@@ -26,7 +26,7 @@ k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table
             const bool known = id >= 0 && id < rows;
             left[u] = d - col;
             to[u] = (row0 + r) * ld_out + col;
-            v[u] = vec_load(table + (known ? id * ld_table + col : 0), known ? left[u] : 0);
+            v[u] = vec_load(table + (known ? id * ld_table + col : 0), known ? left[u] : 0, col);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
@@ -145,7 +145,7 @@ __device__ __forceinline__ void grad_write(TT *__restrict__ row, int64_t col, in
     vec_f<E> f;
 #pragma unroll
     for (int i = 0; i < E; ++i) f[i] = acc[i] * scale;
-    if (accumulate) f += vec_wide<TT, E>(vec_load<TT, E>(row + col, left));
+    if (accumulate) f += vec_wide<TT, E>(vec_load<TT, E>(row + col, left, col));
     vec_store<TT, E>(row + col, left, f);
 }
 
@@ -182,7 +182,7 @@ __device__ __forceinline__ void grad_pick(const TG *__restrict__ grad, int64_t l
                 hits &= hits - 1;
                 const uint32_t pos = __builtin_amdgcn_readlane(e, at) & (GRAD_FEW - 1);
                 k += more;
-                v[u] = vec_load<TG, E>(grad + (int64_t)pos * ld + col, more ? left : 0);
+                v[u] = vec_load<TG, E>(grad + (int64_t)pos * ld + col, more ? left : 0, col);
             }
 #pragma unroll
             for (int u = 0; u < B; ++u)
@@ -420,7 +420,7 @@ k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uin
     auto request = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            ahead[u] = vec_load<TG, E>(g + (int64_t)__builtin_amdgcn_readlane(p, (i0 + u) & 63) * ld_grad, i0 + u < m ? left : 0);
+            ahead[u] = vec_load<TG, E>(g + (int64_t)__builtin_amdgcn_readlane(p, (i0 + u) & 63) * ld_grad, i0 + u < m ? left : 0, col);
     };
     vec_f<E> acc = (vec_f<E>)0.0f;
     bool whole = heads & 1;  // the run that is being added has begun here

@@ -1,22 +1,29 @@
 // vec_norm and vec_norm_grad: root-mean-square norm of rows, with the residual's addition and an 8-bit result.
 //
 // LANES lanes hold a row, eight elements in each of CH pieces: piece c of lane l starts at column 8 (c LANES + l), so that
-// sixteen neighbouring lanes hold the 128 values of a block's scale.  A wave holds 64 / LANES rows (LANES <= 64), or the
-// block of 256 threads one row (LANES = 256).  Everything is read once and stays in registers; bound by memory.  (Outputs that
+// sixteen neighbouring lanes hold the 128 values of a block's scale.  A wave holds 64 / LANES rows (LANES <= 64, four waves a
+// block), or a block of 256 or 512 threads one row.  Everything is read once and stays in registers; bound by memory.  (Outputs that
 // may be inputs in place are not __restrict__: a row is read whole before it is written.)
 #include "vec_device.h"
 
 #define NORM_BLOCKS 2048
 
-// Sum over a row's lanes; LANES = 256: over the block, through LDS (two calls in a row need two buffers).
+// Sum over a row's lanes; over the block, through LDS (two calls in a row need two buffers), where it has more than a wave.
 template <int LANES>
 __device__ __forceinline__ float norm_sum(float v, float *buf) {
-    if constexpr (LANES <= 64) return vec_sum<LANES>(v);
-    v = vec_sum<64>(v);
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (buf[0] + buf[1]) + (buf[2] + buf[3]);
+    if constexpr (LANES <= 64) {
+        return vec_sum<LANES>(v);
+    } else {
+        v = vec_sum<64>(v);
+        if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = (buf[0] + buf[1]) + (buf[2] + buf[3]);
+        if constexpr (LANES == 512) v += (buf[4] + buf[5]) + (buf[6] + buf[7]);
+        return v;
+    }
 }
+template <int LANES>
+constexpr int norm_threads = LANES > 256 ? LANES : 256;
 
 struct NormOut {
     void *h, *y;
@@ -27,15 +34,15 @@ struct NormOut {
 };
 
 template <class T, class W, int LANES, int CH>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(norm_threads<LANES>)
 k_vec_norm(const T *x, int64_t ld_x, const T *residual, int64_t ld_r, const W *__restrict__ weight,
            int64_t n, int d, float eps, NormOut o) {
-    __shared__ float buf[2][4];
-    constexpr int ROWS = 256 / LANES;
+    __shared__ float buf[2][8];
+    constexpr int ROWS = norm_threads<LANES> / LANES;
     const int lane = threadIdx.x % LANES;
     vec_pack<W> w[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) w[c] = vec_load(weight + 8 * (c * LANES + lane), d - 8 * (c * LANES + lane));
+    for (int c = 0; c < CH; ++c) w[c] = vec_load(weight + 8 * (c * LANES + lane), d - 8 * (c * LANES + lane), 8 * (c * LANES + lane));
     int turn = 0;
     for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < n; row0 += (int64_t)gridDim.x * ROWS, turn ^= 1) {
         const int64_t row = row0 + threadIdx.x / LANES;
@@ -46,8 +53,8 @@ k_vec_norm(const T *x, int64_t ld_x, const T *residual, int64_t ld_r, const W *_
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = 8 * (c * LANES + lane);
-                a[c] = vec_load(x + (in ? row * ld_x + col : 0), in ? d - col : 0);
-                if (residual) b[c] = vec_load(residual + (in ? row * ld_r + col : 0), in ? d - col : 0);
+                a[c] = vec_load(x + (in ? row * ld_x + col : 0), in ? d - col : 0, col);
+                if (residual) b[c] = vec_load(residual + (in ? row * ld_r + col : 0), in ? d - col : 0, col);
             }
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -95,7 +102,7 @@ k_vec_norm(const T *x, int64_t ld_x, const T *residual, int64_t ld_r, const W *_
         else if ((d) <= 2048) GO(64, 4); \
         else if ((d) <= 4096) GO(256, 2); \
         else if ((d) <= 8192) GO(256, 4); \
-        else GO(256, 8);                 \
+        else GO(512, 4);                 \
     } while (0)
 
 extern "C" int vec_norm(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, int type, const void *weight,
@@ -117,13 +124,14 @@ extern "C" int vec_norm(const void *x, int64_t ld_x, const void *residual, int64
     hipStream_t s = (hipStream_t)stream;
 #define GO(LANES, CH)                                                                                                     \
     do {                                                                                                                  \
-        const int64_t need = (n + 256 / LANES - 1) / (256 / LANES);                                                       \
+        constexpr int rows = norm_threads<LANES> / LANES;                                                                 \
+        const int64_t need = (n + rows - 1) / rows;                                                                       \
         const unsigned blocks = (unsigned)(need < NORM_BLOCKS ? need : NORM_BLOCKS);                                      \
         if (weight_type == type)                                                                                          \
-            hipLaunchKernelGGL((k_vec_norm<T, T, LANES, CH>), dim3(blocks), dim3(256), 0, s, (const T *)x, ld_x,          \
+            hipLaunchKernelGGL((k_vec_norm<T, T, LANES, CH>), dim3(blocks), dim3(norm_threads<LANES>), 0, s, (const T *)x, ld_x,          \
                                (const T *)residual, ld_residual, (const T *)weight, n, d, eps, o);                        \
         else                                                                                                              \
-            hipLaunchKernelGGL((k_vec_norm<T, float, LANES, CH>), dim3(blocks), dim3(256), 0, s, (const T *)x, ld_x,      \
+            hipLaunchKernelGGL((k_vec_norm<T, float, LANES, CH>), dim3(blocks), dim3(norm_threads<LANES>), 0, s, (const T *)x, ld_x,      \
                                (const T *)residual, ld_residual, (const float *)weight, n, d, eps, o);                    \
     } while (0)
     VEC_TYPED(type, T, NORM_FORMS(d, GO));
@@ -135,30 +143,32 @@ extern "C" int vec_norm(const void *x, int64_t ld_x, const void *residual, int64
 // ----------------------------------------------------------------- gradient --
 // The same layout.  Every lane sums its columns of dweight over the rows that it meets (a fixed set), the block joins its rows
 // through LDS and writes a row of partial sums, which k_vec_norm_join adds up in order.
-#define NORM_GRAD_BLOCKS 512
-
+//
+// More blocks hide the latency of a row, but each writes a row of partial sums.  us with 256 / 512 / 1024 blocks: 32,768 x 128 bf16
+// 12.5 / 12.3 / 12.5; 32,768 x 257 66.8 / 39.4 / 28.2; 10,000 x 1001 fp16 31.1 / 22.9 / 21.9; 16,384 x 2048 bf16 56.2 / 51.4 / 55.3; 8192 x 4096
+// 63.6 / 51.9 / 55.3; 1000 x 16,384 41.7 / 51.5 / 70.4.
 static int norm_grad_blocks(int64_t n, int d) {
-    const int lanes = d <= 128 ? 16 : (d <= 256 ? 32 : (d <= 2048 ? 64 : 256));
-    const int64_t need = (n + 256 / lanes - 1) / (256 / lanes);
-    return (int)(need < NORM_GRAD_BLOCKS ? need : NORM_GRAD_BLOCKS);
+    const int rows = d <= 128 ? 16 : (d <= 256 ? 8 : (d <= 2048 ? 4 : 1));  // a block holds at once
+    const int64_t need = (n + rows - 1) / rows, most = rows == 4 && d <= 1024 ? 1024 : (rows == 1 && n < 2048 ? 256 : 512);
+    return (int)(need < most ? need : most);
 }
 extern "C" size_t vec_norm_grad_workspace_bytes(int64_t n, int d) {
     return n <= 0 || d <= 0 ? 0 : vec_up256((size_t)norm_grad_blocks(n, d) * ((d + 7) & ~7) * 4);
 }
 
 template <class T, class W, int LANES, int CH>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(norm_threads<LANES>)
 k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *dh, int64_t ld_dh,
                 const W *__restrict__ weight, int64_t n, int d, float eps, T *dx, int64_t ld_dx,
                 float *__restrict__ part, int dpad) {
-    __shared__ float buf[4][4];
-    constexpr int ROWS = 256 / LANES;
+    __shared__ float buf[4][8];
+    constexpr int ROWS = norm_threads<LANES> / LANES;
     const int lane = threadIdx.x % LANES;
     vec_pack<W> w[CH];
     vec_f8 dw[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        w[c] = vec_load(weight + 8 * (c * LANES + lane), d - 8 * (c * LANES + lane));
+        w[c] = vec_load(weight + 8 * (c * LANES + lane), d - 8 * (c * LANES + lane), 8 * (c * LANES + lane));
         dw[c] = (vec_f8)0.0f;
     }
     int turn = 0;
@@ -170,9 +180,9 @@ k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *
         for (int c = 0; c < CH; ++c) {
             const int col = 8 * (c * LANES + lane);
             const int64_t left = in ? d - col : 0;
-            a[c] = vec_load(dy + (in ? row * ld_dy + col : 0), left);
-            b[c] = vec_load(hs + (in ? row * ld_h + col : 0), left);
-            if (dh) e[c] = vec_load(dh + (in ? row * ld_dh + col : 0), left);
+            a[c] = vec_load(dy + (in ? row * ld_dy + col : 0), left, col);
+            b[c] = vec_load(hs + (in ? row * ld_h + col : 0), left, col);
+            if (dh) e[c] = vec_load(dh + (in ? row * ld_dh + col : 0), left, col);
         }
         float sq = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -203,7 +213,7 @@ k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *
         }
     }
     float *mine = part + (int64_t)blockIdx.x * dpad;
-    if constexpr (LANES == 256) {
+    if constexpr (LANES >= 256) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
             if (8 * (c * LANES + lane) < dpad) *(vec_f8 *)(mine + 8 * (c * LANES + lane)) = dw[c];
@@ -263,11 +273,11 @@ extern "C" int vec_norm_grad(const void *dy, int64_t ld_dy, const void *h, int64
 #define GO(LANES, CH)                                                                                                     \
     do {                                                                                                                  \
         if (weight_type == type)                                                                                          \
-            hipLaunchKernelGGL((k_vec_norm_grad<T, T, LANES, CH>), dim3(blocks), dim3(256), 0, s, (const T *)dy, ld_dy,   \
+            hipLaunchKernelGGL((k_vec_norm_grad<T, T, LANES, CH>), dim3(blocks), dim3(norm_threads<LANES>), 0, s, (const T *)dy, ld_dy,   \
                                (const T *)h, ld_h, (const T *)dh, ld_dh, (const T *)weight, n, d, eps, (T *)dx, ld_dx,    \
                                (float *)workspace, dpad);                                                                 \
         else                                                                                                              \
-            hipLaunchKernelGGL((k_vec_norm_grad<T, float, LANES, CH>), dim3(blocks), dim3(256), 0, s, (const T *)dy,      \
+            hipLaunchKernelGGL((k_vec_norm_grad<T, float, LANES, CH>), dim3(blocks), dim3(norm_threads<LANES>), 0, s, (const T *)dy,      \
                                ld_dy, (const T *)h, ld_h, (const T *)dh, ld_dh, (const float *)weight, n, d, eps, (T *)dx, \
                                ld_dx, (float *)workspace, dpad);                                                          \
     } while (0)

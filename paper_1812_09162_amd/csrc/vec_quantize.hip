@@ -16,7 +16,7 @@ k_vec_quantize(const T *__restrict__ x, int64_t ld, int64_t n, int64_t d, int64_
     const int64_t b = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;  // block of the matrix
     const int64_t row = b / nb, col = (b - row * nb) * VEC_BLOCK + (threadIdx.x & 15) * 8;
     const bool in = row < n;
-    const vec_f8 f = vec_wide<T>(vec_load(x + (in ? row * ld + col : 0), in ? d - col : 0));
+    const vec_f8 f = vec_wide<T>(vec_load(x + (in ? row * ld + col : 0), in ? d - col : 0, col));
     const VecScale s = vec_scale(vec_max16(vec_top(f)), o.e5m2, o.pow2);
     if (!in) return;
     if (col < d) vec_store_bytes(o.q + row * o.ld_q + col, d - col, vec_to8(f, s, o.e5m2, o.pow2));
@@ -38,7 +38,7 @@ k_vec_quantize_t(const T *__restrict__ x, int64_t ld, int64_t n, int64_t d, int6
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t row = row0 + tr * 8 + i, col = col0 + tc * 8;
-        v[i] = vec_load(x + (row < n ? row * ld + col : 0), row < n ? d - col : 0);
+        v[i] = vec_load(x + (row < n ? row * ld + col : 0), row < n ? d - col : 0, col);
     }
     vec_f8 m = (vec_f8)0.0f;
 #pragma unroll
