@@ -60,15 +60,27 @@ __device__ __forceinline__ uint32_t mat_scale_bits(const void *scales, int64_t a
     return pow2 ? (uint32_t)((const uint8_t *)scales)[at] << 23 : ((const uint32_t *)scales)[at];
 }
 
-// Sixteen bytes of a row from column k on, at any address; zeros beyond column `end`.
+// Sixteen bytes of a row from column k on, at any address; zeros beyond column `end`.  (The end of a row: its last sixteen, moved into place.)
 __device__ __forceinline__ vec_i4 mat_chunk(const uint8_t *row, int64_t k, int64_t end) {
     typedef int any128 __attribute__((ext_vector_type(4), aligned(1)));
+    typedef uint64_t any64x2 __attribute__((ext_vector_type(2), aligned(1)));
     if (k + 16 <= end) return *(const any128 *)(row + k);
-    vec_i4 v = {0, 0, 0, 0};
-    for (int i = 0; i < 16 && k + i < end; ++i) v[i >> 2] |= (int)row[k + i] << (8 * (i & 3));
-    return v;
+    uint64_t lo = 0, hi = 0;
+    if (k < end && end >= 16) {
+        const any64x2 x = *(const any64x2 *)(row + end - 16);
+        const int bits = (int)(k + 16 - end) * 8;  // 8..120
+        lo = bits >= 64 ? x[1] >> (bits - 64) : x[0] >> bits | x[1] << (64 - bits);
+        hi = bits >= 64 ? 0 : x[1] >> bits;
+    } else if (k < end) {  // (a row of fewer than sixteen: k is 0)
+#pragma unroll 1
+        for (int i = 0; i < (int)end; ++i) {
+            const uint64_t x = (uint64_t)row[i] << (8 * (i & 7));
+            if (i < 8) lo |= x;
+            else hi |= x;
+        }
+    }
+    return vec_i4{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
 }
-
 __device__ __forceinline__ vec_i4 mat_chunk(const uint8_t *p) {
     typedef int any128 __attribute__((ext_vector_type(4), aligned(1)));
     return *(const any128 *)p;
@@ -306,7 +318,7 @@ k_vec_mat(const MatArgs p) {
     if (last_step < s1) {  // a piece that the last column divides
         __syncthreads();
         *(uint32_t *)(lds + ROWS * 128 + t * 4) = scale_at(last_step);
-#pragma unroll 1
+#pragma unroll MI <= 4 ? 4 : 1
         for (int i = 0; i < PER; ++i) {
             const uint8_t *const row = i < PER_A ? mat_a + delta(i) * p.ld_a : mat_b + delta(i) * p.ld_b;
             *(vec_i4 *)(lds + (i * WAVES + wave) * 1024 + lane * 16) = mat_chunk(row, (int64_t)last_step * 128 + piece, p.k);
