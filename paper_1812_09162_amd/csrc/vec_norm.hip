@@ -196,8 +196,8 @@ k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *
         }
         sq = norm_sum<LANES>(sq, buf[turn]);
         dot = norm_sum<LANES>(dot, buf[turn + 1]);
-        const float r = rsqrtf(sq / (float)d + eps);
-        const float k = r * r * r * (dot / (float)d);
+        const float r = in ? rsqrtf(sq / (float)d + eps) : 0.0f;  // (a row behind the last would bring 0 / 0 into dweight where eps is 0)
+        const float k = r * (r * (dot / (float)d));  // (h r and r h are near one, so that nothing here leaves float32's range early: r^3 did, for h of 1e13 and of 1e-13)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = 8 * (c * LANES + lane);
@@ -205,8 +205,9 @@ k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *
             vec_f8 f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                f[i] = __fmaf_rn(-h[i], k, r * (y[i] * g[i]));
-                dw[c][i] = __fmaf_rn(y[i] * h[i], r, dw[c][i]);
+                const float hr = h[i] * r;
+                f[i] = __fmaf_rn(-hr, k, r * (y[i] * g[i]));
+                dw[c][i] = __fmaf_rn(y[i], hr, dw[c][i]);
             }
             if (dh) f += vec_wide<T>(e[c]);
             if (in) vec_store(dx + row * ld_dx + col, d - col, f);

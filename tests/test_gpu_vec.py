@@ -365,6 +365,21 @@ def test_norm_grad_against_differences(qb):
             assert abs(float(got.view(-1)[at]) - float(diff)) <= 1e-7 + 300 * U * float(dy.abs().max() * w.abs().max() * 4)
 
 
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("size", [1e15, 1e-15])
+def test_norm_grad_far_from_one(qb, t, size):
+    """Rows whose inverse root, to the third power, is outside float32."""
+    n, d = 5, 300
+    h, dy, w = rnd((n, d), 1, t, size), rnd((n, d), 2, t), 1 + 0.3 * rnd((d,), 3)
+    hd, u = h.double(), dy.double() * w.double()
+    r = 1 / torch.sqrt((hd * hd).mean(1, keepdim=True))
+    want = r * u - hd * r ** 3 * (u * hd).mean(1, keepdim=True)
+    mag = (r * u).abs() + hd.abs() * r ** 3 * (u * hd).abs().mean(1, keepdim=True)
+    dx, dw = qb.vec_norm_grad(dy, h, w, eps=0.0)
+    close(dx, want, (3 * NORM_U + 80 * U) * mag + half_step(want, t))
+    close(dw, (dy.double() * hd * r).sum(0), (NORM_U + (n + 3) * U) * (dy.double() * hd * r).abs().sum(0))
+
+
 def test_norm_grad_of_nothing(qb):
     dx, dw = qb.vec_norm_grad(torch.empty((0, 40), device=dev()), torch.empty((0, 40), device=dev()), torch.ones(40, device=dev()))
     assert dx.shape == (0, 40) and bool((dw == 0).all())
