@@ -1,10 +1,12 @@
 // vec_matmul_blocks: the kernels.  c = a b^T over 8-bit factors whose rows carry a scale for each 128 values.
 //
 // The matrix cores' own 8-bit products add eight terms at a time after aligning them to the largest and dropping what lies
-// below 2^-13 of it (measured, e4m3 and e5m2, with and without scales): a sum is then 1.5e-5 of its size off, not the 1e-7 of
-// float32, and a result in float32 shows it.  So the factors are read and kept as bytes and become bfloat16 in registers, which holds
-// every one of them exactly (with its power of two, if scales are E8M0), and v_mfma_f32_16x16x32_bf16 adds their products
-// in float32.  F32 scales multiply each block's sum.  b's rows are the instruction's first factor, so that a lane holds
+// below 2^-13 of it (measured, e4m3 and e5m2, with and without scales): of a sum, about 2e-5 of the result, which float32 and float16 results
+// show and long sums in bfloat16 do not (mat_native).  For these v_mfma_scale_f32_16x16x128_f8f6f4 takes the bytes as they are
+// (k_vec_mat8; 16,384 x 4096 x 4096 with E8M0 scales 237 us = 2.3 PFLOP/s; half of the cycles have a product, the rest wait for the step's
+// rows and the block's other waves).  For the others the factors are read and kept as bytes and become bfloat16 in registers, which holds every one of
+// them exactly (with its power of two, if scales are E8M0), and v_mfma_f32_16x16x32_bf16 adds their products in float32 (k_vec_mat, 418 us;
+// vector instructions that widen and products take turns).  F32 scales multiply each block's sum.  b's rows are the instruction's first factor, so that a lane holds
 // four neighbouring columns of c.  Lane l holds 32 of the 128 values of row l % 16; which 32 is the same for both factors, so that
 // their order does not matter.
 #pragma once
@@ -111,17 +113,20 @@ __device__ __forceinline__ void mat_store(const MatArgs &p, int64_t row, int64_t
 // buffers of LDS: while one is multiplied, the next is on its way, from memory to LDS without registers (ASYNC: rows that
 // start at multiples of 16 bytes) or through them.  (Three blocks ahead in four buffers was no faster: 2048 x 2048 x 2048 25.3 us with
 // two, 26.3 with four; what bounds a lone block is the chain of reading, widening and multiplying.)  A row of a buffer is 128 bytes, its sixteen-byte
-// pieces exchanged by the row's low three bits, so that eight lanes that read the same piece of eight rows meet eight
+// pieces exchanged by what mat_turn says, so that the sixteen lanes that an LDS read of sixteen bytes serves at once meet 64
 // different banks.  ASYNC reads through a buffer that ends with the tile's last row, so that one offset per lane serves all rows, and
 // rows beyond the matrix and pieces beyond the last column are zeros; a piece that the last column divides comes through
 // registers, and its block of k last and by itself.  (There, rows beyond the matrix are the last row again; what comes of
 // them is not stored.)
 typedef __attribute__((address_space(3))) void *mat_to;
+// The piece c of row r lies at place c ^ mat_turn(r).  Lanes 0..3, 12..15 and 20..27 of a read are served together (the others alike): rows 0..3 and
+// 12..15 of one piece, rows 4..11 of the piece two further on; a row's parity is half of its banks.  (Exchanged by the row's low three bits, every
+// read met four cycles of conflicts.)
+__device__ __forceinline__ int mat_turn(int row) { return ((row >> 1) + 2) & 7; }
 #define MAT_BUFFER 0x00027000  // a raw buffer: offsets in bytes; what lies at or behind its length reads as zero
 
-template <int FA, int FB, bool P2, bool ASYNC, int WM, int WN, int MI, int NI>
-__global__ void __launch_bounds__(64 * WM * WN)
-k_vec_mat(const MatArgs p) {
+template <int FA, int FB, bool P2, bool ASYNC, int WM, int WN, int MI, int NI, bool NATIVE>
+__device__ __forceinline__ void mat_tiles(const MatArgs &p) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host has no type for a buffer)
     constexpr int BM = WM * MI * 16, BN = WN * NI * 16, ROWS = BM + BN, WAVES = WM * WN;
     constexpr int PER = ROWS / 8 / WAVES, PER_A = BM / 8 / WAVES;  // wave instructions per step, eight rows each; a's are first
@@ -151,7 +156,7 @@ k_vec_mat(const MatArgs p) {
 
     // where this wave's rows of a buffer come from: i-th instruction, rows 8 (i WAVES + wave) + lane / 8
     const uint8_t *const mat_a = p.a + m0 * p.ld_a, *const mat_b = p.b + n0 * p.ld_b;
-    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;  // the columns that this lane's place in a row holds
+    const int piece = ((lane & 7) ^ mat_turn(lane >> 3 | (wave & 1) << 3)) * 16;  // the columns that this lane's place in a row holds (WAVES is even)
     // (ASYNC: rows are less than 2^23 apart, their scales less than 2^21, so that a tile's offsets have 32 bits)
     auto buffer = [](const uint8_t *at, int rows, int64_t ld, int64_t cols) {
         return __builtin_amdgcn_make_buffer_rsrc((void *)at, 0, ASYNC ? (int)((uint32_t)(rows - 1) * (uint32_t)ld + (uint32_t)cols) : 0, MAT_BUFFER);
@@ -184,7 +189,7 @@ k_vec_mat(const MatArgs p) {
         for (int j = 0; j < NI; ++j) acc[i][j] = (vec_f4)0.0f;
 
     const int wm = wave / WN, wn = wave % WN;
-    const int frag = (lane & 15) * 128 + (((lane >> 4) * 2) ^ (lane & 7)) * 16;  // its first sixteen bytes of sixteen rows; the second: ^ 16
+    const int frag = (lane & 15) * 128 + (((lane >> 4) * 2) ^ mat_turn(lane & 15)) * 16;  // its first sixteen bytes of sixteen rows; the second: ^ 16
 
     uint32_t scale_next = 0;
     vec_i4 regs[ASYNC ? 1 : PER];
@@ -214,12 +219,60 @@ k_vec_mat(const MatArgs p) {
             for (int i = 0; i < PER; ++i) *(vec_i4 *)(lds + buf + (i * WAVES + wave) * 1024 + lane * 16) = regs[i];
         }
     };
-    auto multiply = [&](int buf) {
+    auto multiply = [&](int buf, auto &&meanwhile) {
         const int fa = buf + wm * MI * 2048 + frag, fb = buf + BM * 128 + wn * NI * 2048 + frag;
         const int sca = buf + ROWS * 128, scb = sca + BM * 4;
         // (bit 4 tells a lane's two pieces apart, and no tile's offset has it)
         auto load = [&](int at, int half) { return *(const vec_i4 *)(lds + (half ? at ^ 16 : at)); };
-        if constexpr (P2) {
+        if constexpr (NATIVE) {
+            // a lane's 32 bytes of a row as they are; while one tile row is multiplied, the next is read.  What is to be requested meanwhile goes behind
+            // the first reads, and the products before the other waves' (16,384 x 4096 x 4096: 258 -> 244 -> 241 us; the requests
+            // dealt out over the tile rows 252, the rows brought to the cache two steps ahead 258)
+            auto read = [&](int at) { return __builtin_shufflevector(load(at, 0), load(at, 1), 0, 1, 2, 3, 4, 5, 6, 7); };
+            vec_i8 b[NI], a[2];
+            a[0] = read(fa);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) b[j] = read(fb + j * 2048);
+            meanwhile();
+            __builtin_amdgcn_s_setprio(1);
+            if constexpr (P2) {
+                vec_i4 sa[MI / 4], sb[NI / 4];
+#pragma unroll
+                for (int i = 0; i < MI / 4; ++i) sa[i] = *(const vec_i4 *)(lds + sca + ((wm * MI / 4 + i) * 64 + (lane & 15) * 4) * 4);
+#pragma unroll
+                for (int j = 0; j < NI / 4; ++j) sb[j] = *(const vec_i4 *)(lds + scb + ((wn * NI / 4 + j) * 64 + (lane & 15) * 4) * 4);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    if (i + 1 < MI) a[(i + 1) & 1] = read(fa + (i + 1) * 2048);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i & 1], acc[i][j], FB, FA, 0, sb[j / 4][j % 4], 0, sa[i / 4][i % 4]);
+                }
+            } else {
+                vec_f4 sb[NI], q[2][NI];
+                float sa[2];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) sb[j] = *(const vec_f4 *)(lds + scb + ((wn * NI + j) * 16 + (lane >> 4) * 4) * 4);
+                // a tile row's sums are scaled while the next one's products run
+#pragma unroll
+                for (int i = 0; i <= MI; ++i) {
+                    if (i + 1 < MI) a[(i + 1) & 1] = read(fa + (i + 1) * 2048);
+                    if (i < MI) {
+                        sa[i & 1] = *(const float *)(lds + sca + ((wm * MI + i) * 16 + (lane & 15)) * 4);
+#pragma unroll
+                        for (int j = 0; j < NI; ++j)
+                            q[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i & 1], (vec_f4)0.0f, FB, FA, 0, 127, 0, 127);
+                    }
+                    if (i > 0)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                acc[i - 1][j][r] = __fmaf_rn(q[(i - 1) & 1][j][r], sa[(i - 1) & 1] * sb[j][r], acc[i - 1][j][r]);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+        } else if constexpr (P2) {
             // E8M0 as the float32 whose exponent it is (mat_widen looks at the exponent alone, so 0 is 2^-127)
             vec_f4 sa[MI / 4], sb[NI / 4];
 #pragma unroll
@@ -297,8 +350,11 @@ k_vec_mat(const MatArgs p) {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // this wave's part of the step has landed, and its reads of the last are done
             __builtin_amdgcn_s_barrier();                                  // everybody's have
             asm volatile("" ::: "memory");
-            if (s + 1 < last_step) request(s + 1, STAGE - now);
-            multiply(now);
+            auto next = [&] {
+                if (s + 1 < last_step) request(s + 1, STAGE - now);
+            };
+            if (!NATIVE) next();
+            multiply(now, next);
             now = STAGE - now;
         }
     } else {
@@ -309,7 +365,7 @@ k_vec_mat(const MatArgs p) {
             for (int s = s0; s < last_step; ++s) {
                 __syncthreads();
                 if (s + 1 < last_step) request(s + 1, 0);
-                multiply(now);
+                multiply(now, [] {});
                 now = STAGE - now;
                 if (s + 1 < last_step) put(now);
             }
@@ -324,7 +380,7 @@ k_vec_mat(const MatArgs p) {
             *(vec_i4 *)(lds + (i * WAVES + wave) * 1024 + lane * 16) = mat_chunk(row, (int64_t)last_step * 128 + piece, p.k);
         }
         __syncthreads();
-        multiply(0);
+        multiply(0, [] {});
     }
 
 #pragma unroll
@@ -347,6 +403,14 @@ k_vec_mat(const MatArgs p) {
         }
     }
 #endif
+}
+template <int FA, int FB, bool P2, bool ASYNC, int WM, int WN, int MI, int NI>
+__global__ void __launch_bounds__(64 * WM * WN) k_vec_mat(const MatArgs p) {
+    mat_tiles<FA, FB, P2, ASYNC, WM, WN, MI, NI, false>(p);
+}
+template <int FA, int FB, bool P2, bool ASYNC, int WM, int WN, int MI, int NI>
+__global__ void __launch_bounds__(64 * WM * WN) k_vec_mat8(const MatArgs p) {
+    mat_tiles<FA, FB, P2, ASYNC, WM, WN, MI, NI, true>(p);
 }
 
 // -------------------------------------------------------------- few rows of a --
@@ -431,6 +495,7 @@ struct MatPlan {
     int few;       // 0: tiles; 1, 2: sixteens of rows of a
     int kshare;    // few: waves that share a tile's k
     int tile;      // MAT_*
+    int native;    // tiles: 8-bit products
     int tm, tn, splits, per;
     size_t workspace;
 };

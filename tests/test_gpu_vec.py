@@ -474,6 +474,44 @@ def test_matmul_scales_at_the_ends(qb):
         assert torch.equal(got.isnan(), bad)
 
 
+@pytest.mark.parametrize("st", [E8M0, F32])
+@pytest.mark.parametrize("ta,tb", [(E4M3, E4M3), (E4M3, E5M2), (E5M2, E4M3), (E5M2, E5M2)])
+@pytest.mark.parametrize("m,n,k,aligned", [(70, 90, 512, True), (300, 130, 640, True), (129, 257, 520, False), (500, 70, 1000, True), (2100, 3900, 1024, True),
+                                           (256, 512, 8192, True), (260, 300, 700, False)])
+def test_matmul_long_sums(qb, m, n, k, aligned, ta, tb, st):
+    """bfloat16 results from k = 512 on: small whole numbers exactly, and values of very unequal size within 7 x 2^-13 of the largest of each eight
+    products (at most all magnitudes), beside the float32 additions and the last rounding."""
+    (a, sa), (b, sb) = factor(m, k, 1, ta, st, True), factor(n, k, 2, tb, st, True)
+    if not aligned:
+        a, _ = framed(a, 3, 4)
+    want, _ = product64(a, sa, b, sb)
+    assert torch.equal(qb.vec_matmul_blocks(a, sa, b, sb), want.to(F32).to(BF16))
+    g = torch.Generator().manual_seed(m)
+    a, b = (torch.exp2(torch.randint(-6, 8, (r, k), generator=g).float() * torch.randint(0, 2, (r, k), generator=g)).to(t).to(dev()) for r, t in ((m, ta), (n, tb)))
+    want, size = product64(a, sa, b, sb)  # no sign: every loss adds up
+    got = qb.vec_matmul_blocks(a, sa, b, sb)
+    close(got, want, (7 * 2.0 ** -13 + (2 * k + 8) * U) * size + half_step(want, BF16))
+    assert torch.equal(got, qb.vec_matmul_blocks(a, sa, b, sb))
+
+
+@pytest.mark.parametrize("m", [70, 600])
+def test_matmul_long_sums_scales_at_the_ends(qb, m):
+    """The same of test_matmul_scales_at_the_ends for the 8-bit products, and columns behind a row's last that are NaN."""
+    n, k = 1500, 640
+    a, b = torch.ones((m, k), device=dev()).to(E4M3), torch.ones((n, k), device=dev()).to(E4M3)
+    a, _ = framed(a, 16, 16)
+    sa, sb = torch.full((m, 5), 2.0 ** -120, device=dev()).to(E8M0), torch.full((n, 5), 2.0 ** 100, device=dev()).to(E8M0)
+    assert bool((qb.vec_matmul_blocks(a, sa, b, sb) == 640 * 2.0 ** -20).all())
+    a.view(torch.uint8)[3, 200] = 0x7F
+    sb.view(torch.uint8)[8, 1] = 255
+    bad = torch.zeros((m, n), dtype=torch.bool, device=dev())
+    bad[3], bad[:, 8] = True, True
+    assert torch.equal(qb.vec_matmul_blocks(a, sa, b, sb).isnan(), bad)
+    sa, sb = sa.float(), torch.full((n, 5), 2.0 ** 100, device=dev())
+    sb[8, 1] = math.nan
+    assert torch.equal(qb.vec_matmul_blocks(a, sa, b, sb).isnan(), bad)
+
+
 def test_matmul_beyond_32_bits(qb):
     """Bytes past 2^32 of a factor, elements past 2^31 of the result."""
     n, k = 4_300_000, 1024
