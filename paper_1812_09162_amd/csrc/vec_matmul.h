@@ -130,6 +130,7 @@ __device__ __forceinline__ void mat_tiles(const MatArgs &p) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (the host has no type for a buffer)
     constexpr int BM = WM * MI * 16, BN = WN * NI * 16, ROWS = BM + BN, WAVES = WM * WN;
     constexpr int PER = ROWS / 8 / WAVES, PER_A = BM / 8 / WAVES;  // wave instructions per step, eight rows each; a's are first
+    constexpr bool TURNS = NATIVE && P2 && ASYNC && WAVES == 8;  // (see there)
     constexpr int STAGE = ROWS * 132;                              // bytes of a buffer: values and scales
     static_assert(ROWS == 64 * WAVES &&  // (a thread brings one row's scale)
                   BM % 64 == 0 && BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "");
@@ -343,7 +344,69 @@ __device__ __forceinline__ void mat_tiles(const MatArgs &p) {
         }
     };
 
-    if constexpr (ASYNC) {
+    if constexpr (TURNS) {
+        // The large tile: two groups of four waves, one wave of each on a SIMD, take turns.  While one multiplies a step, the other reads all of its
+        // fragments from LDS.  Turn 2s: the first group reads step s, the second multiplies s - 1; turn 2s + 1: the first multiplies s, the second
+        // reads it.  So a buffer has been read when turn 2s + 1 ends, and both groups request step s + 2 into it in turn 2s + 2 and have
+        // waited for it when turn 2s + 3 ends.  (16,384 x 4096 x 4096 252 -> 243 us against all waves in step, on one card, 4096 x 4096 x 8192 122 -> 117, but 8192 x 2048 x 512 20 -> 21; requests dealt out among the products cost the gain.)
+        auto read = [&](int at) { return __builtin_shufflevector(*(const vec_i4 *)(lds + at), *(const vec_i4 *)(lds + (at ^ 16)), 0, 1, 2, 3, 4, 5, 6, 7); };
+        const bool second = wave >= WAVES / 2;
+        auto turn = [] {
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" ::: "memory");
+        };
+        if (s0 < last_step) {
+            request(s0, 0);
+            if (s0 + 1 < last_step) {
+                static_assert(PER == 8 || !TURNS, "");
+                request(s0 + 1, STAGE);
+                asm volatile("s_waitcnt vmcnt(9)" ::: "memory");  // (its eight rows and the scale may still be on their way)
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            turn();
+            if (second) turn();
+            int now = 0;
+            for (int s = s0; s < last_step; ++s) {
+                vec_i8 a[MI], b[NI];
+                vec_i4 sa[MI / 4], sb[NI / 4];
+                const int fa = now + wm * MI * 2048 + frag, fb = now + BM * 128 + wn * NI * 2048 + frag;
+                const int sca = now + ROWS * 128, scb = sca + BM * 4;
+#pragma unroll
+                for (int j = 0; j < NI; ++j) b[j] = read(fb + j * 2048);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) a[i] = read(fa + i * 2048);
+#pragma unroll
+                for (int i = 0; i < MI / 4; ++i) sa[i] = *(const vec_i4 *)(lds + sca + ((wm * MI / 4 + i) * 64 + (lane & 15) * 4) * 4);
+#pragma unroll
+                for (int j = 0; j < NI / 4; ++j) sb[j] = *(const vec_i4 *)(lds + scb + ((wn * NI / 4 + j) * 64 + (lane & 15) * 4) * 4);
+                if (!second && s > s0 && s + 1 < last_step) request(s + 1, STAGE - now);
+                if (second) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                turn();
+                __builtin_amdgcn_s_setprio(1);
+                if (second && s + 2 < last_step) request(s + 2, now);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], FB, FA, 0, sb[j / 4][j % 4], 0, sa[i / 4][i % 4]);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {  // (here, and not behind the turn)
+                    static_assert(NI == 4 || !TURNS, "");
+                    asm volatile("" : "+v"(acc[i][0]), "+v"(acc[i][1]), "+v"(acc[i][2]), "+v"(acc[i][3]));
+                }
+                __builtin_amdgcn_s_setprio(0);
+                if (!second) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                turn();
+                now = STAGE - now;
+            }
+            if (!second) turn();
+        }
+    } else if constexpr (ASYNC) {
         int now = 0;
         if (s0 < last_step) request(s0, 0);
         for (int s = s0; s < last_step; ++s) {
