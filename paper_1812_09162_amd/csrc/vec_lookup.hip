@@ -235,11 +235,9 @@ k_vec_grad_few(const TG *__restrict__ grad, int n, int d, int64_t ld_grad, const
     }
     if (lane == 0) count[wave] = m;
     __syncthreads();
-    if (!accumulate) grad_zeros<TT, 64 * WAVES>(nrow, cols, has, [&](int r) { return table + of(r) * ld_table + col0; });
     int all = 0;
 #pragma unroll
     for (int q = 0; q < WAVES; ++q) all += count[q];
-    if (all == 0) return;
     int turn = 0;
     for (int w = 0; w < (nrow + 31) / 32; ++w) {
         for (uint32_t bits = has[w]; bits; bits &= bits - 1) {
@@ -263,6 +261,8 @@ k_vec_grad_few(const TG *__restrict__ grad, int n, int d, int64_t ld_grad, const
             }
         }
     }
+    // (behind the sums, whose reads would wait for these stores)
+    if (!accumulate) grad_zeros<TT, 64 * WAVES>(nrow, cols, has, [&](int r) { return table + of(r) * ld_table + col0; });
 }
 
 // --- the sort.  counts[tile][bucket]
