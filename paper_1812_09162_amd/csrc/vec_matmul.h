@@ -293,6 +293,7 @@ __device__ __forceinline__ void mat_tiles(const MatArgs &p) {
             raw[1] = read_a(1);
 #pragma unroll
             for (int j = 0; j < NI; ++j) rawb[j] = load(fb + j * 2048, 0);
+            meanwhile();
 #pragma unroll
             for (int j = 0; j < NI; ++j) b[0][j] = wide_b(j, rawb[j]);
             a[0] = wide_a(0, raw[0]);
@@ -315,24 +316,45 @@ __device__ __forceinline__ void mat_tiles(const MatArgs &p) {
                         acc[t % MI][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[BOTH ? t / MI : 0][j].v[v], a[t & 1].v[v], acc[t % MI][j], 0, 0, 0);
             }
         } else {
-            MatHalf b[2][NI];
-            vec_f4 sb[NI];
+            // in turn the tile rows: while one is multiplied, the next is widened, the one behind it read and the sums of the one before it scaled
+            MatHalf b[2][NI], a[2][2];
+            vec_i4 raw[2][2], rawb[2][NI];
+            vec_f4 sb[NI], q[2][NI];
+            float sa[2];
+            auto read_a = [&](int i) {
+                raw[i & 1][0] = load(fa + i * 2048, 0);
+                raw[i & 1][1] = load(fa + i * 2048, 1);
+            };
+            auto wide_a = [&](int i) {
+                a[i & 1][0] = mat_half<FA>(raw[i & 1][0], 1.0f);
+                a[i & 1][1] = mat_half<FA>(raw[i & 1][1], 1.0f);
+            };
+            read_a(0);
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                b[0][j] = mat_half<FB>(load(fb + j * 2048, 0), 1.0f);
-                b[1][j] = mat_half<FB>(load(fb + j * 2048, 1), 1.0f);
+                rawb[0][j] = load(fb + j * 2048, 0);
+                rawb[1][j] = load(fb + j * 2048, 1);
                 sb[j] = *(const vec_f4 *)(lds + scb + ((wn * NI + j) * 16 + (lane >> 4) * 4) * 4);
             }
-            // a tile row's sums are scaled while the next one's products run
-            vec_f4 q[2][NI];
-            float sa[2];
+            read_a(1);
+            meanwhile();
+            wide_a(0);
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                b[0][j] = mat_half<FB>(rawb[0][j], 1.0f);
+                b[1][j] = mat_half<FB>(rawb[1][j], 1.0f);
+            }
 #pragma unroll
             for (int i = 0; i <= MI; ++i) {
                 if (i < MI) {
-                    const MatHalf a0 = mat_half<FA>(load(fa + i * 2048, 0), 1.0f), a1 = mat_half<FA>(load(fa + i * 2048, 1), 1.0f);
+                    if (i + 2 < MI) read_a(i + 2);
                     sa[i & 1] = *(const float *)(lds + sca + ((wm * MI + i) * 16 + (lane & 15)) * 4);
+                    if (i + 1 < MI) wide_a(i + 1);
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) q[i & 1][j] = mat_mul(b[1][j], a1, mat_mul(b[0][j], a0, (vec_f4)0.0f));
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j)
+                            q[i & 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[v >> 1][j].v[v & 1], a[i & 1][v >> 1].v[v & 1], v ? q[i & 1][j] : (vec_f4)0.0f, 0, 0, 0);
                 }
                 if (i > 0)
 #pragma unroll
@@ -416,7 +438,6 @@ __device__ __forceinline__ void mat_tiles(const MatArgs &p) {
             auto next = [&] {
                 if (s + 1 < last_step) request(s + 1, STAGE - now);
             };
-            if (!NATIVE) next();
             multiply(now, next);
             now = STAGE - now;
         }
