@@ -30,10 +30,11 @@ enum { VEC_F32 = 0, VEC_BF16 = 1, VEC_F16 = 2, VEC_E4M3 = 3, VEC_E5M2 = 4, VEC_E
 
 #define VEC_BLOCK 128         /* consecutive values that share a scale */
 #define VEC_MAX_NORM_DIM 16384 /* columns of vec_norm and vec_norm_grad */
+#define VEC_MAX_ROW_DIM (1 << 24) /* columns of vec_lookup and vec_lookup_grad */
 
 /*
  * out[i] = scale * table[ids[i]].  An id outside 0..rows-1 (a search pads its results with -1) gives a row of zeros.
- *   table [dev][rows][d], table_type F32, BF16 or F16; rows >= 0, d >= 1
+ *   table [dev][rows][d], table_type F32, BF16 or F16; rows >= 0, 1 <= d <= VEC_MAX_ROW_DIM
  *   ids   [dev][n], int32 (id_bytes 4) or int64 (8); n >= 0
  *   out   [dev][n][d], out_type F32, BF16 or F16
  */
@@ -44,7 +45,7 @@ int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_table, int tab
  * The gradient of vec_lookup for its table:
  *   table_grad[v] = (accumulate ? table_grad[v] : 0) + scale * sum over the i with ids[i] == v of grad[i]
  * Every row is written, those without an id with zeros (accumulate: these are left alone).  Ids outside 0..rows-1 take no part.
- *   grad       [dev][n][d], grad_type F32, BF16 or F16; n < 2^31
+ *   grad       [dev][n][d], grad_type F32, BF16 or F16; n < 2^31, 1 <= d <= VEC_MAX_ROW_DIM
  *   table_grad [dev][rows][d], table_type F32, BF16 or F16; rows < 2^31
  *   workspace  >= vec_lookup_grad_workspace_bytes(n, rows, d), 256-byte aligned, any content
  */

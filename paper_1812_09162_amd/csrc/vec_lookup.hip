@@ -3,7 +3,8 @@
 
 // ------------------------------------------------------------------ look-up --
 // out[i] = scale * table[ids[i]].  A block copies `rpb` neighbouring rows of the result as pieces of eight elements; bound by
-// memory: every piece is one wide load behind a load of the row's id, eight of them in flight per thread.
+// memory: every piece is one wide load behind a load of the row's id, four of them in flight per thread.  65,536 rows of 65,536 x 1024 bf16 (some
+// rows again and again): 32 us for the 134 MB written, 44 us a call among calls (its neighbours' stores drain); 100 rows 3.6 us, all latency.
 template <class TI, class TO, class ID>
 __global__ void __launch_bounds__(256)
 k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table, const ID *__restrict__ ids, int64_t n,
@@ -41,7 +42,7 @@ k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table
 
 extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_table, int table_type, const void *ids,
                           int id_bytes, int64_t n, float scale, void *out, int64_t ld_out, int out_type, void *stream) {
-    VEC_REQUIRE(n >= 0 && rows >= 0 && d >= 1, "vec_lookup: n=%lld, rows=%lld, d=%d", (long long)n, (long long)rows, d);
+    VEC_REQUIRE(n >= 0 && rows >= 0 && d >= 1 && d <= VEC_MAX_ROW_DIM, "vec_lookup: n=%lld, rows=%lld, d=%d", (long long)n, (long long)rows, d);
     VEC_REQUIRE(vec_is_wide(table_type) && vec_is_wide(out_type), "vec_lookup: types %d and %d are not F32, BF16 or F16", table_type, out_type);
     VEC_REQUIRE(id_bytes == 4 || id_bytes == 8, "vec_lookup: ids of %d bytes", id_bytes);
     VEC_REQUIRE(ld_table >= d && ld_out >= d, "vec_lookup: rows of %lld and %lld elements hold no %d", (long long)ld_table, (long long)ld_out, d);
@@ -71,12 +72,13 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 //
 // Few ids (n <= GRAD_FEW): one launch.  Every block owns some rows of the table, dealt out in turn since frequent ids are often
 // neighbours; it goes through all ids, keeps the positions of its own in order, and writes its rows, zeros or sums.  The ids
-// are read once per block, from the L2 cache.
+// are read once per block, from the L2 cache.  2,048 ids into 65,536 x 256 float32: 20 us, of which the 67 MB of zeros are 14 at the rate of a large copy.
 //
 // Many: the positions are sorted by id (a stable radix sort of up to 2^GRAD_BITS buckets a pass), then summed in pieces
 // of at most GRAD_CHUNK sorted positions, whatever ids they hold, so that a frequent id is no wave's alone; sums of ids that cross
 // a piece's ends are joined by a last kernel.  The sort's kernels wait for memory most of the time: blocks beside theirs clear the
-// table meanwhile, a share in each launch.
+// table meanwhile, a share in each launch.  262,144 ids into 100,003 x 512 (bf16, 373 MB, log-uniform): two passes of 8 + 15 us, in which the 102 MB are
+// cleared, sums 74 (268 MB read at 3.6 TB/s: a wave's rows come in the order of the ids), joins 11: 135 us a call.
 //
 // A row is spread over the 64 lanes of a wave, E elements each (2, 4 or 8, the fewest that hold it, else 64 E columns at a time).
 // us, one launch / sorted: 2,048 ids into 65,536 x 256 21 / 60, 4,096 25 / 57, 8,192 44 / 46; tables that one pass sorts: 883 into 623 x 2944 21 / 43,
@@ -498,7 +500,7 @@ k_vec_grad_join(const uint32_t *__restrict__ keys, int64_t n, const uint32_t *__
 extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_grad, int grad_type, const void *ids, int id_bytes,
                                float scale, int accumulate, void *table_grad, int64_t rows, int64_t ld_table, int table_type,
                                void *workspace, size_t workspace_bytes, void *stream) {
-    VEC_REQUIRE(n >= 0 && rows >= 0 && d >= 1 && n <= 0x7fffffffLL && rows <= 0x7ffffffeLL, "vec_lookup_grad: n=%lld, rows=%lld, d=%d",
+    VEC_REQUIRE(n >= 0 && rows >= 0 && d >= 1 && d <= VEC_MAX_ROW_DIM && n <= 0x7fffffffLL && rows <= 0x7ffffffeLL, "vec_lookup_grad: n=%lld, rows=%lld, d=%d",
                 (long long)n, (long long)rows, d);
     VEC_REQUIRE(vec_is_wide(grad_type) && vec_is_wide(table_type), "vec_lookup_grad: types %d and %d are not F32, BF16 or F16", grad_type, table_type);
     VEC_REQUIRE(id_bytes == 4 || id_bytes == 8, "vec_lookup_grad: ids of %d bytes", id_bytes);

@@ -3,9 +3,9 @@
 // The matrix cores' own 8-bit products add eight terms at a time after aligning them to the largest and dropping what lies
 // below 2^-13 of it (measured, e4m3 and e5m2, with and without scales): of a sum, about 2e-5 of the result, which float32 and float16 results
 // show and long sums in bfloat16 do not (mat_native).  For these v_mfma_scale_f32_16x16x128_f8f6f4 takes the bytes as they are
-// (k_vec_mat8; 16,384 x 4096 x 4096 with E8M0 scales 237 us = 2.3 PFLOP/s; half of the cycles have a product, the rest wait for the step's
-// rows and the block's other waves).  For the others the factors are read and kept as bytes and become bfloat16 in registers, which holds every one of
-// them exactly (with its power of two, if scales are E8M0), and v_mfma_f32_16x16x32_bf16 adds their products in float32 (k_vec_mat, 418 us;
+// (k_vec_mat8; 16,384 x 4096 x 4096 with E8M0 scales 233 to 243 us on three cards = 2.3 PFLOP/s, F32 scales 340; products run in 58 % of the cycles, at 2.0 GHz; what
+// is left are waits for a step's rows, 64 KB for each of 2048 cycles of products).  For the others the factors are read and kept as bytes and become bfloat16 in registers, which holds every one of
+// them exactly (with its power of two, if scales are E8M0), and v_mfma_f32_16x16x32_bf16 adds their products in float32 (k_vec_mat, 420 us;
 // vector instructions that widen and products take turns).  F32 scales multiply each block's sum.  b's rows are the instruction's first factor, so that a lane holds
 // four neighbouring columns of c.  Lane l holds 32 of the 128 values of row l % 16; which 32 is the same for both factors, so that
 // their order does not matter.
@@ -499,7 +499,8 @@ __global__ void __launch_bounds__(64 * WM * WN) k_vec_mat8(const MatArgs p) {
 
 // -------------------------------------------------------------- few rows of a --
 // Up to 16 MF rows of a: b is read once, straight from memory to the registers of the lanes that multiply it; a wave takes
-// sixteen rows of b and a share of k, and the shares of a block's waves are joined in LDS.  Bound by reading b.
+// sixteen rows of b and a share of k, and the shares of a block's waves are joined in LDS.  Bound by reading b: 1 x 4096 x 2048 4.7 us, of which the
+// 8.4 MB are 1.8 (the rest is launch and latency), 1 x 65,536 x 4096 60.
 #define MAT_FEW_WAVES 8
 template <int FA, int FB, bool P2, int MF>
 __global__ void __launch_bounds__(64 * MAT_FEW_WAVES)

@@ -2,7 +2,8 @@
 //
 // LANES lanes hold a row, eight elements in each of CH pieces: piece c of lane l starts at column 8 (c LANES + l), so that
 // sixteen neighbouring lanes hold the 128 values of a block's scale.  A wave holds 64 / LANES rows (LANES <= 64, four waves a
-// block), or a block of 256 or 512 threads one row.  Everything is read once and stays in registers; bound by memory.  (Outputs that
+// block), or a block of 256 or 512 threads one row.  Everything is read once and stays in registers; bound by memory.  16,384 x 2048 bf16 with residual and
+// 8-bit result: 42 us for 235 MB (5.6 TB/s; 48 a call among calls, the rate of a large copy); one row 5 us, all latency.  (Outputs that
 // may be inputs in place are not __restrict__: a row is read whole before it is written.)
 #include "vec_device.h"
 
@@ -142,7 +143,8 @@ extern "C" int vec_norm(const void *x, int64_t ld_x, const void *residual, int64
 
 // ----------------------------------------------------------------- gradient --
 // The same layout.  Every lane sums its columns of dweight over the rows that it meets (a fixed set), the block joins its rows
-// through LDS and writes a row of partial sums, which k_vec_norm_join adds up in order.
+// through LDS and writes a row of partial sums, which k_vec_norm_join adds up in order.  Bound by memory: 16,384 x 2048 bf16 44 us for 268 MB (6.1 TB/s), the join 5,
+// 55 a call among calls; 10,000 x 1001 fp16 15 and 5 us.
 //
 // More blocks hide the latency of a row, but each writes a row of partial sums.  us with 256 / 512 / 1024 blocks: 32,768 x 128 bf16
 // 12.5 / 12.3 / 12.5; 32,768 x 257 66.8 / 39.4 / 28.2; 10,000 x 1001 fp16 31.1 / 22.9 / 21.9; 16,384 x 2048 bf16 56.2 / 51.4 / 55.3; 8192 x 4096

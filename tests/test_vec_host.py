@@ -147,3 +147,11 @@ def test_binding_refuses_host_tensors():
         with pytest.raises(qb.QadcError) as e:
             call()
         assert e.value.code == qb.PQ_EINVAL and "GPU" in str(e.value)
+
+
+def test_rows_of_too_many_columns_are_refused():
+    """Counts of columns near 2^31 would overflow."""
+    lib = qb.load()
+    for d in ((1 << 24) + 1, (1 << 31) - 1):
+        refused(lib.vec_lookup(P, 5, d, d, BF16, P, 8, 3, 1.0, P, d, BF16, None), f"d={d}")
+        refused(lib.vec_lookup_grad(P, 3, d, d, BF16, P, 8, 1.0, 0, P, 5, d, BF16, P, 1 << 40, None), f"d={d}")
