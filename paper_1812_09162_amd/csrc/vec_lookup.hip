@@ -76,8 +76,8 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 //
 // Many: the positions are sorted by id (a stable radix sort of up to 2^GRAD_BITS buckets a pass), then summed in pieces
 // of at most GRAD_CHUNK sorted positions, whatever ids they hold, so that a frequent id is no wave's alone; sums of ids that cross
-// a piece's ends are joined by a last kernel.  The sort's kernels wait for memory most of the time: blocks beside theirs clear the
-// table meanwhile, a share in each launch.  262,144 ids into 100,003 x 512 (bf16, 373 MB, log-uniform): two passes of 8 + 15 us, in which the 102 MB are
+// a piece's ends are joined by a last kernel.  k_vec_grad_place waits for memory most of the time: blocks beside its own clear the
+// table meanwhile, a share in each pass (in k_vec_grad_count too: 262,144 ids into 900,000 x 100 85 us, 79 without).  262,144 ids into 100,003 x 512 (bf16, 373 MB, log-uniform): two passes of 8 + 15 us, in which the 102 MB are
 // cleared, sums 74 (268 MB read at 3.6 TB/s: a wave's rows come in the order of the ids), joins 11: 135 us a call.
 //
 // A row is spread over the 64 lanes of a wave, E elements each (2, 4 or 8, the fewest that hold it, else 64 E columns at a time).
@@ -300,11 +300,10 @@ __device__ __forceinline__ uint32_t grad_key(const ID *__restrict__ ids, const u
 }
 
 #define GRAD_PER (GRAD_TILE / 1024)
-template <class ID, class TT>
+template <class ID>
 __global__ void __launch_bounds__(1024)
 k_vec_grad_count(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, int64_t n, int64_t rows, int shift, int bits,
-                 uint32_t *__restrict__ counts, GradClear z) {
-    if (grad_clear<TT>(z)) return;
+                 uint32_t *__restrict__ counts) {
     __shared__ uint32_t h[1 << GRAD_BITS];
     const int nb = 1 << bits;
     const int64_t first = (int64_t)blockIdx.x * GRAD_TILE + threadIdx.x;
@@ -448,16 +447,17 @@ k_vec_grad_chunks(const TG *__restrict__ grad, int d, int64_t ld_grad, const uin
         *(vec_f<E> *)(part + ((int64_t)chunk * 2 + (whole ? 1 : 0)) * dpad + col) = acc;
 }
 
-// The run that ends in a piece and began before it: its partial sums added in order, by a wave, or by the block, a quarter of them per
+// The run that ends in a piece and began before it: its partial sums added in order, by a wave, or by the block, a share of them per
 // wave, if they are many.  64 E columns from blockIdx.y 64 E on.
 #define GRAD_JOIN_ALONE 16
+#define GRAD_JOIN_WAVES 8  // (us with 4 / 8 / 16: 262,144 ids into 500 x 64 42.3 / 39.7 / 40.6, 5,000 into 65,536 x 256 43.0 / 43.7 / 45.1)
 template <class TT, int E>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(64 * GRAD_JOIN_WAVES)
 k_vec_grad_join(const uint32_t *__restrict__ keys, int64_t n, const uint32_t *__restrict__ begins, const float *__restrict__ part, int dpad,
                 int d, float scale, int accumulate, TT *__restrict__ table, int64_t rows, int64_t ld_table, int chunks, int len) {
-    __shared__ vec_f<E> quarter[4][64];
-    __shared__ int many[4];  // a wave's run, if the block is to take it: its first piece
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first_chunk = blockIdx.x * 4 + 1, chunk = first_chunk + wave;
+    __shared__ vec_f<E> share[GRAD_JOIN_WAVES][64];
+    __shared__ int many[GRAD_JOIN_WAVES];  // a wave's run, if the block is to take it: its first piece
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first_chunk = blockIdx.x * GRAD_JOIN_WAVES + 1, chunk = first_chunk + wave;
     const int col = (int)blockIdx.y * 64 * E + lane * E;
     auto sum = [&](int c0, int from, int to) {
         vec_f<E> acc = (vec_f<E>)0.0f;
@@ -481,16 +481,16 @@ k_vec_grad_join(const uint32_t *__restrict__ keys, int64_t n, const uint32_t *__
     if (lane == 0) many[wave] = all ? c0 : -1;
     if (c0 >= 0 && !all) write(chunk, sum(c0, c0, chunk + 1));
     __syncthreads();
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < GRAD_JOIN_WAVES; ++w) {
         const int at = many[w], c1 = first_chunk + w + 1;
         if (at < 0) continue;
-        const int each = (c1 - at + 3) / 4, from = at + wave * each;
-        vec_f<E> acc = sum(at, from, from + each < c1 ? from + each : c1);
-        quarter[wave][lane] = acc;
+        const int each = (c1 - at + GRAD_JOIN_WAVES - 1) / GRAD_JOIN_WAVES, from = at + wave * each;
+        vec_f<E> acc = sum(at, from < c1 ? from : c1, from + each < c1 ? from + each : c1);
+        share[wave][lane] = acc;
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
-            for (int q = 1; q < 4; ++q) acc += quarter[q][lane];
+            for (int q = 1; q < GRAD_JOIN_WAVES; ++q) acc += share[q][lane];
             write(c1 - 1, acc);
         }
         __syncthreads();
@@ -541,15 +541,13 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     uint32_t *counts = (uint32_t *)(ws + p.counts);
     uint32_t *begins = (uint32_t *)(ws + p.begins);
     float *part = (float *)(ws + p.part);
-    const int launches = 2 * p.passes;
-    int launch = 0;
-    // a launch's share of the rows to clear, 32 KB and more a block
+    // a pass's share of the rows to clear, 32 KB and more a block
     const size_t row_bytes = vec_bytes(table_type) * (size_t)d;
     GradClear z = {table_grad, 0, 0, ld_table, d, (int)(row_bytes >= 32768 ? 1 : 32768 / row_bytes), 0};
-    auto share = [&](unsigned own) {
+    auto share = [&](int pass, unsigned own) {
         z.after = (int)own;
         z.lo = z.hi;
-        z.hi = accumulate ? 0 : rows / launches * ++launch + (launch == launches ? rows % launches : 0);
+        z.hi = accumulate ? 0 : rows * (pass + 1) / p.passes;
         int64_t blocks = (z.hi - z.lo + z.each - 1) / z.each;
         while (blocks > (1 << 20)) {
             z.each *= 2;
@@ -560,15 +558,14 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     for (int pass = 0; pass < p.passes; ++pass) {
         const uint32_t *ki = pass ? key[(pass - 1) & 1] : nullptr, *pi = pass ? pos[(pass - 1) & 1] : nullptr;
         const int shift = pass * p.bits;
-        dim3 grid;
-#define GO(ID, TT)                                                                                                          \
-    do {                                                                                                                    \
-        grid = share((unsigned)p.tiles);                                                                                    \
-        hipLaunchKernelGGL((k_vec_grad_count<ID, TT>), grid, dim3(1024), 0, s, (const ID *)ids, ki, n, rows, shift, p.bits, counts, z); \
-        grid = share((unsigned)p.tiles);                                                                                    \
-        hipLaunchKernelGGL((k_vec_grad_place<ID, TT>), grid, dim3(1024), (size_t)64 << p.bits, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
-                           counts, p.tiles, key[pass & 1], pos[pass & 1], z);                                               \
-    } while (0)
+        if (id_bytes == 4)
+            hipLaunchKernelGGL((k_vec_grad_count<int32_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int32_t *)ids, ki, n, rows, shift, p.bits, counts);
+        else
+            hipLaunchKernelGGL((k_vec_grad_count<int64_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int64_t *)ids, ki, n, rows, shift, p.bits, counts);
+        const dim3 grid = share(pass, (unsigned)p.tiles);
+#define GO(ID, TT)                                                                                                         \
+    hipLaunchKernelGGL((k_vec_grad_place<ID, TT>), grid, dim3(1024), (size_t)64 << p.bits, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
+                       counts, p.tiles, key[pass & 1], pos[pass & 1], z)
         VEC_TYPED(table_type, TT, if (id_bytes == 4) GO(int32_t, TT); else GO(int64_t, TT));
 #undef GO
     }
@@ -576,8 +573,8 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL(
         (k_vec_grad_chunks<TG, TT, E>), dim3((unsigned)((p.chunks + 3) / 4), (unsigned)((d + 64 * E - 1) / (64 * E))), dim3(256), 0, s, (const TG *)grad,
         d, ld_grad, ks, ps, n, rows, scale, accumulate, (TT *)table_grad, ld_table, begins, part, p.dpad, p.chunks, p.len))));
-    VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL((k_vec_grad_join<TT, E>), dim3((unsigned)(p.chunks + 2) / 4, (unsigned)((d + 64 * E - 1) / (64 * E))),
-                                                                dim3(256), 0, s, ks, n, begins, part, p.dpad, d, scale, accumulate, (TT *)table_grad, rows, ld_table, p.chunks, p.len)));
+    VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL((k_vec_grad_join<TT, E>), dim3((unsigned)((p.chunks + GRAD_JOIN_WAVES - 2) / GRAD_JOIN_WAVES), (unsigned)((d + 64 * E - 1) / (64 * E))),
+                                                                dim3(64 * GRAD_JOIN_WAVES), 0, s, ks, n, begins, part, p.dpad, d, scale, accumulate, (TT *)table_grad, rows, ld_table, p.chunks, p.len)));
     QADC_LAUNCH_CHECK("vec_lookup_grad's kernels");
     return PQ_OK;
 }
