@@ -9,6 +9,7 @@ raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -480,6 +481,12 @@ def _refuse(name: str, msg: str):
     raise QadcError(PQ_EINVAL, f"{name}: {msg}")
 
 
+@functools.lru_cache(maxsize=1024)
+def _vec_bytes(name: str, *sizes) -> int:
+    """A workspace's bytes, which sizes alone decide."""
+    return getattr(load(), name)(*sizes)
+
+
 class _Call:
     """The device and the stream of a call, for its checks, allocations and launch.  (A call of a few microseconds on the GPU waits
     for what is done here, so messages are only put together for a refusal, and outputs made here are not looked over.)"""
@@ -493,7 +500,7 @@ class _Call:
             _refuse(name, f"a stream of {stream.device} for tensors of {first.device}")
         self.raw = torch._C._cuda_getCurrentRawStream(self.index)
         self.device = first.device
-        if (stream is not None and stream.cuda_stream != self.raw) or torch.cuda.current_device() != self.index:
+        if (stream is not None and stream.cuda_stream != self.raw) or torch._C._cuda_getDevice() != self.index:
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.index)  # (entered around allocations and the launch)
             self.raw = self.stream.cuda_stream
 
@@ -611,7 +618,7 @@ def vec_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: flo
     else:
         optr, old = call.rows("out", out, rows, d, to)
     lib = _lib or load()
-    wptr, wbytes, keep = call.workspace(workspace, lib.vec_lookup_grad_workspace_bytes(n, rows, d))
+    wptr, wbytes, keep = call.workspace(workspace, _vec_bytes("vec_lookup_grad_workspace_bytes", n, rows, d))
     call.launch(lib.vec_lookup_grad, ptr, n, d, ld, call.type("grad", grad.dtype), idp, id_bytes, scale, int(accumulate), optr, rows,
                 old, call.type("out", to), wptr, wbytes)
     return out
@@ -692,7 +699,7 @@ def vec_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, dh: O
         xp, ldx = call.rows("dx", dx, n, d, t)
         dwp = call.vector("dweight", dweight, d, torch.float32)
     lib = _lib or load()
-    wsp, wbytes, keep = call.workspace(workspace, lib.vec_norm_grad_workspace_bytes(n, d))
+    wsp, wbytes, keep = call.workspace(workspace, _vec_bytes("vec_norm_grad_workspace_bytes", n, d))
     call.launch(lib.vec_norm_grad, yp, ldy, hp, ldh, ep, lde, call.type("dy", t), wp, call.type("weight", weight.dtype), n, d, eps, xp, ldx,
                 dwp, wsp, wbytes)
     return dx, dweight
@@ -730,7 +737,7 @@ def vec_matmul_blocks(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, 
     else:
         cp, ldc = call.rows("out", out, m, n, to)
     lib = _lib or load()
-    wptr, wbytes, keep = call.workspace(workspace, lib.vec_matmul_blocks_workspace_bytes(m, n, k))
+    wptr, wbytes, keep = call.workspace(workspace, _vec_bytes("vec_matmul_blocks_workspace_bytes", m, n, k))
     call.launch(lib.vec_matmul_blocks, ap, lda, call.type("a", a.dtype), asp, ldas, bp, ldb, call.type("b", b.dtype), bsp, ldbs,
                 call.type("scales", st), m, n, k, cp, ldc, call.type("out", to), wptr, wbytes)
     return out

@@ -494,6 +494,13 @@ def test_matmul_long_sums(qb, m, n, k, aligned, ta, tb, st):
     assert torch.equal(got, qb.vec_matmul_blocks(a, sa, b, sb))
 
 
+@pytest.mark.parametrize("st", [E8M0, F32])
+@pytest.mark.parametrize("k", [512, 640, 1000, 1160, 1290])
+def test_matmul_long_sums_in_large_tiles(qb, k, st):
+    """Even and odd numbers of blocks, and a last column within a piece of sixteen; the last tiles are not full."""
+    check_product(qb, 3600, 3700, k, E4M3, E5M2, st, BF16, frame=k == 640)
+
+
 @pytest.mark.parametrize("m", [70, 600])
 def test_matmul_long_sums_scales_at_the_ends(qb, m):
     """The same of test_matmul_scales_at_the_ends for the 8-bit products, and columns behind a row's last that are NaN."""
