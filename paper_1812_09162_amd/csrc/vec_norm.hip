@@ -148,11 +148,13 @@ extern "C" int vec_norm(const void *x, int64_t ld_x, const void *residual, int64
 //
 // More blocks hide the latency of a row, but each writes a row of partial sums.  us with 256 / 512 / 1024 blocks: 32,768 x 128 bf16
 // 12.5 / 12.3 / 12.5; 32,768 x 257 66.8 / 39.4 / 28.2; 10,000 x 1001 fp16 31.1 / 22.9 / 21.9; 16,384 x 2048 bf16 56.2 / 51.4 / 55.3; 8192 x 4096
-// 63.6 / 51.9 / 55.3; 1000 x 16,384 41.7 / 51.5 / 70.4.
+// 63.6 / 51.9 / 55.3; 1000 x 16,384 41.7 / 51.5 / 70.4.  What one block does in two rounds (four of narrow rows)
+// it does alone, writing dweight itself, without the join: 8 x 2048 13.6 -> 11.5 a call, which waits for the host's launches, and 6.3 -> 5.7 in a graph; 16 x 2048
+// in four rounds 8.5 there, so not more.
 static int norm_grad_blocks(int64_t n, int d) {
     const int rows = d <= 128 ? 16 : (d <= 256 ? 8 : (d <= 2048 ? 4 : 1));  // a block holds at once
     const int64_t need = (n + rows - 1) / rows, most = rows == 4 && d <= 1024 ? 1024 : (rows == 1 && n < 2048 ? 256 : 512);
-    return (int)(need < most ? need : most);
+    return (int)(need <= (d <= 256 ? 4 : 2) ? 1 : (need < most ? need : most));
 }
 extern "C" size_t vec_norm_grad_workspace_bytes(int64_t n, int d) {
     return n <= 0 || d <= 0 ? 0 : vec_up256((size_t)norm_grad_blocks(n, d) * ((d + 7) & ~7) * 4);
@@ -162,7 +164,7 @@ template <class T, class W, int LANES, int CH>
 __global__ void __launch_bounds__(norm_threads<LANES>)
 k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *dh, int64_t ld_dh,
                 const W *__restrict__ weight, int64_t n, int d, float eps, T *dx, int64_t ld_dx,
-                float *__restrict__ part, int dpad) {
+                float *__restrict__ part, int dpad) {  // part: a row of dpad sums a block
     __shared__ float buf[4][8];
     constexpr int ROWS = norm_threads<LANES> / LANES;
     const int lane = threadIdx.x % LANES;
@@ -219,7 +221,7 @@ k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *
     if constexpr (LANES >= 256) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
-            if (8 * (c * LANES + lane) < dpad) *(vec_f8 *)(mine + 8 * (c * LANES + lane)) = dw[c];
+            vec_store(mine + 8 * (c * LANES + lane), dpad - 8 * (c * LANES + lane), dw[c]);
     } else {
         __shared__ vec_f8 all[ROWS][LANES];
 #pragma unroll
@@ -227,10 +229,10 @@ k_vec_norm_grad(const T *dy, int64_t ld_dy, const T *hs, int64_t ld_h, const T *
             __syncthreads();
             all[threadIdx.x / LANES][lane] = dw[c];
             __syncthreads();
-            if (threadIdx.x < LANES && 8 * (c * LANES + lane) < dpad) {
+            if (threadIdx.x < LANES) {
                 vec_f8 sum = all[0][lane];
                 for (int r = 1; r < ROWS; ++r) sum += all[r][lane];
-                *(vec_f8 *)(mine + 8 * (c * LANES + lane)) = sum;
+                vec_store(mine + 8 * (c * LANES + lane), dpad - 8 * (c * LANES + lane), sum);
             }
         }
     }
@@ -263,8 +265,9 @@ extern "C" int vec_norm_grad(const void *dy, int64_t ld_dy, const void *h, int64
     VEC_REQUIRE(vec_aligned(dy, type) && vec_aligned(h, type) && vec_aligned(dh, type) && vec_aligned(dx, type) && vec_aligned(weight, weight_type) &&
                     vec_aligned(dweight, VEC_F32), "vec_norm_grad: misaligned pointer");
     hipStream_t s = (hipStream_t)stream;
-    const int dpad = (d + 7) & ~7;
+    int dpad = (d + 7) & ~7;
     unsigned blocks = 0;
+    float *part = (float *)workspace;
     if (n > 0) {
         const size_t need = vec_norm_grad_workspace_bytes(n, d);
         VEC_REQUIRE(workspace && ((uintptr_t)workspace & 255u) == 0, "vec_norm_grad: workspace null or not 256-byte aligned");
@@ -273,21 +276,23 @@ extern "C" int vec_norm_grad(const void *dy, int64_t ld_dy, const void *h, int64
             return PQ_ENOMEM;
         }
         blocks = (unsigned)norm_grad_blocks(n, d);
+        if (blocks == 1) part = dweight, dpad = d;
 #define GO(LANES, CH)                                                                                                     \
     do {                                                                                                                  \
         if (weight_type == type)                                                                                          \
             hipLaunchKernelGGL((k_vec_norm_grad<T, T, LANES, CH>), dim3(blocks), dim3(norm_threads<LANES>), 0, s, (const T *)dy, ld_dy,   \
                                (const T *)h, ld_h, (const T *)dh, ld_dh, (const T *)weight, n, d, eps, (T *)dx, ld_dx,    \
-                               (float *)workspace, dpad);                                                                 \
+                               part, dpad);                                                                               \
         else                                                                                                              \
             hipLaunchKernelGGL((k_vec_norm_grad<T, float, LANES, CH>), dim3(blocks), dim3(norm_threads<LANES>), 0, s, (const T *)dy,      \
                                ld_dy, (const T *)h, ld_h, (const T *)dh, ld_dh, (const float *)weight, n, d, eps, (T *)dx, \
-                               ld_dx, (float *)workspace, dpad);                                                          \
+                               ld_dx, part, dpad);                                                                        \
     } while (0)
         VEC_TYPED(type, T, NORM_FORMS(d, GO));
 #undef GO
     }
-    hipLaunchKernelGGL(k_vec_norm_join, dim3((unsigned)((d + 15) / 16)), dim3(256), 0, s, (const float *)workspace, dpad, (int)blocks, d, dweight);
+    if (blocks != 1)
+        hipLaunchKernelGGL(k_vec_norm_join, dim3((unsigned)((d + 15) / 16)), dim3(256), 0, s, part, dpad, (int)blocks, d, dweight);
     QADC_LAUNCH_CHECK("vec_norm_grad's kernels");
     return PQ_OK;
 }

@@ -380,6 +380,22 @@ def test_norm_grad_far_from_one(qb, t, size):
     close(dw, (dy.double() * hd * r).sum(0), (NORM_U + (n + 3) * U) * (dy.double() * hd * r).abs().sum(0))
 
 
+@pytest.mark.parametrize("n,d", [(16, 100), (17, 128), (64, 127), (65, 127), (32, 250), (33, 256), (13, 301), (16, 2041), (17, 2048), (4, 2049), (5, 2049), (2, 9001), (4, 16_383)])
+def test_norm_grad_of_few_rows(qb, n, d):
+    """Around the rows that one block takes alone; dweight written within its columns."""
+    h, dy, w = rnd((n, d), 1, BF16), rnd((n, d), 2, BF16), 1 + 0.3 * rnd((d,), 3)
+    hd, yd = h.double(), dy.double()
+    r = 1 / torch.sqrt((hd * hd).mean(1, keepdim=True) + 1e-6)
+    store = torch.full((d + 8,), 7.0, device=dev())
+    dx, dw = qb.vec_norm_grad(dy, h, w, eps=1e-6, out=(torch.empty_like(dy), store[3:3 + d]))
+    u = yd * w.double()
+    mag = (r * u).abs() + hd.abs() * r ** 3 * (u * hd).abs().mean(1, keepdim=True)
+    want = r * u - hd * r ** 3 * (u * hd).mean(1, keepdim=True)
+    close(dx, want, (3 * NORM_U + 80 * U) * mag + half_step(want, BF16))
+    close(dw, (yd * hd * r).sum(0), (NORM_U + (n + 3) * U) * (yd * hd * r).abs().sum(0))
+    assert bool((store[:3] == 7).all()) and bool((store[3 + d:] == 7).all())
+
+
 def test_norm_grad_of_nothing(qb):
     dx, dw = qb.vec_norm_grad(torch.empty((0, 40), device=dev()), torch.empty((0, 40), device=dev()), torch.ones(40, device=dev()))
     assert dx.shape == (0, 40) and bool((dw == 0).all())
