@@ -77,8 +77,8 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 // Many: the positions are sorted by id (a stable radix sort of up to 2^GRAD_BITS buckets a pass), then summed in pieces
 // of at most GRAD_CHUNK sorted positions, whatever ids they hold, so that a frequent id is no wave's alone; sums of ids that cross
 // a piece's ends are joined by a last kernel.  k_vec_grad_place waits for memory most of the time: blocks beside its own clear the
-// table meanwhile, a share in each pass (in k_vec_grad_count too: 262,144 ids into 900,000 x 100 85 us, 79 without).  262,144 ids into 100,003 x 512 (bf16, 373 MB, log-uniform): two passes of 8 + 15 us, in which the 102 MB are
-// cleared, sums 74 (268 MB read at 3.6 TB/s: a wave's rows come in the order of the ids), joins 11: 135 us a call.
+// table meanwhile, a share in each pass (in k_vec_grad_count too: 262,144 ids into 900,000 x 100 85 us, 79 without).  262,144 ids into 100,003 x 512 (bf16, 373 MB, log-uniform): two passes of 5 + 15 us, in which the 102 MB are
+// cleared, sums 74 (271 MB read and 56 written, 4.4 TB/s), joins 9: 131 us a call.
 //
 // A row is spread over the 64 lanes of a wave, E elements each (2, 4 or 8, the fewest that hold it, else 64 E columns at a time).
 // us, one launch / sorted: 2,048 ids into 65,536 x 256 21 / 60, 4,096 25 / 57, 8,192 44 / 46; tables that one pass sorts: 883 into 623 x 2944 21 / 43,
