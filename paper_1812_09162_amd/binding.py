@@ -525,9 +525,12 @@ class _Call:
         _refuse(self.name, f"{what} of shape {tuple(shape)}, not {(n, d)}")
 
     def first_rows(self, what: str, t: torch.Tensor):
-        if t.dim() != 2:
-            _refuse(self.name, f"{what} of shape {tuple(t.shape)}, not a matrix")
-        n, d = t.shape
+        shape = t.shape
+        if len(shape) != 2:
+            _refuse(self.name, f"{what} of shape {tuple(shape)}, not a matrix")
+        n, d = shape
+        if t.is_contiguous():
+            return n, d, t.data_ptr(), d or 1
         return (n, d, *self.rows(what, t, n, d, t.dtype))
 
     def vector(self, what: str, t: torch.Tensor, n: Optional[int] = None, dtype=None) -> int:
@@ -552,9 +555,12 @@ class _Call:
         return t
 
     def ids(self, t: torch.Tensor):
-        if t.dtype != torch.int64 and t.dtype != torch.int32:
+        size = 8 if t.dtype == torch.int64 else 4
+        if size == 4 and t.dtype != torch.int32:
             _refuse(self.name, f"ids are int32 or int64, got {t.dtype}")
-        return self.vector("ids", t), t.element_size()
+        if t.get_device() != self.index or not t.is_contiguous():
+            self.vector("ids", t)  # (refuses)
+        return t.data_ptr(), size
 
     def out_type(self, out: Optional[torch.Tensor], dtype, default):
         """The type of a result that may be given, named, or left to the default."""
