@@ -10,7 +10,6 @@
 typedef float vec_f4 __attribute__((ext_vector_type(4)));
 typedef float vec_f8 __attribute__((ext_vector_type(8)));
 typedef int vec_i4 __attribute__((ext_vector_type(4)));
-typedef int vec_i8 __attribute__((ext_vector_type(8)));
 
 // E elements (eight, unless said otherwise) as they lie in memory.  Global loads and stores work at any byte address here; the
 // types only promise the alignment of one element.

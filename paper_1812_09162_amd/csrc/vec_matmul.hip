@@ -21,36 +21,26 @@ __global__ void __launch_bounds__(256) k_vec_mat_join(const MatArgs p) {
     mat_store(p, row, col, sum);
 }
 
-// Whether tiles take the matrix cores' 8-bit products as they are, twice as fast.  What these drop is at most 7 x 2^-13 of the largest of
-// eight products, so that a sum is at most 2^-10.2 of its terms' magnitudes off, less than half a step of bfloat16 (2^-9); measured
-// 2.0e-5 and 2.0e-6 (rms) of the magnitudes at k = 512, where a float32 sum in any order promises 512 x 2^-24 = 3.1e-5, and 2.5e-5 of the result (rms) at every k,
-// beside 1.6e-3 of the rounding.  float16 results (half a step 2^-11) and float32 ones show it, and short sums have no more terms than that to hide it.
-static bool mat_native(int c_type, int64_t k) { return c_type == VEC_BF16 && k >= 512; }
-
 // The form of a product, by what each was measured to take (us; E8M0 scales unless said otherwise).
 //   Tiles: 5, and for a step of 128 columns 1.15 (128 x 128, one tile on a CU; 0.92 per tile with more; F32 scales 1.45 and 1.25) or 3.1
 //   (256 x 256), so that large tiles win by a sixth where they fill the CUs; k is split into shares where tiles are too few
-//   for that, at the price of a launch and of partial results written and read (4.5 TB/s).  8-bit products: 0.56 (0.51; F32 scales 0.8 and
-//   0.7) or 1.63 (2.4), and 1.7 or 6 for a tile's beginning and end.
+//   for that, at the price of a launch and of partial results written and read (4.5 TB/s).
 //   Up to 32 rows of a, each wave sixteen rows of b: 2.5, and b at 4.6 TB/s for one row, 3.1 up to 16, 2.1 (F32 scales 1.75) up to 32 (rows of a are read again by
 //   every wave): 16 x 4096 x 4096 9.3 against 13.4 in tiles, 32 11.5 / 14.0, but 16 x 65,536 x 4096 88 / 59 and 64 x 4096 x 4096 17.4 / 16.2.
-static MatPlan mat_plan(int64_t m, int64_t n, int64_t k, bool pow2, bool async, bool native) {
+static MatPlan mat_plan(int64_t m, int64_t n, int64_t k, bool pow2, bool async) {
     MatPlan p = {};
-    p.native = native;
     const int64_t steps = (k + VEC_BLOCK - 1) / VEC_BLOCK;
     double best = 1e300;
-    // (the large tile has no registers to spare for a detour through them, nor, widened, for sums of a block)
-    for (int tile = MAT_128; tile <= (async && (pow2 || native) ? MAT_256 : MAT_128); ++tile) {
+    // (the large tile has no registers to spare for a detour through them, nor for sums of a block)
+    for (int tile = MAT_128; tile <= (async && pow2 ? MAT_256 : MAT_128); ++tile) {
         const int side = tile == MAT_256 ? 256 : 128;
         const int64_t tm = (m + side - 1) / side, tn = (n + side - 1) / side;
         if (tm * tn > 0x7fffffffLL) continue;
         for (int64_t s = 1; s <= 32 && (s == 1 || (s * 4 <= steps && tm * tn * s <= 512)); ++s) {
             const int64_t per = (steps + s - 1) / s, rounds = (tm * tn * s + 255) / 256;
             const bool one = rounds == 1;
-            const double step = native ? (tile == MAT_256 ? (pow2 ? 1.63 : 2.4) : (pow2 ? (one ? 0.56 : 0.51) : (one ? 0.8 : 0.7)))
-                                       : (tile == MAT_256 ? 3.1 : (pow2 ? (one ? 1.15 : 0.92) : (one ? 1.45 : 1.25)));
-            const double ends = native ? (tile == MAT_256 ? 6.0 : 1.7) : 0.0;
-            const double us = 5.0 + (double)rounds * ((double)per * step + ends) + (s > 1 ? 4.0 + (double)s * (double)m * (double)n * 8 / 4.5e6 : 0.0);
+            const double step = tile == MAT_256 ? 3.1 : (pow2 ? (one ? 1.15 : 0.92) : (one ? 1.45 : 1.25));
+            const double us = 5.0 + (double)(rounds * per) * step + (s > 1 ? 4.0 + (double)s * (double)m * (double)n * 8 / 4.5e6 : 0.0);
             if (us >= best) continue;
             best = us;
             p.tile = tile;
@@ -76,10 +66,8 @@ static bool mat_sizes(int64_t m, int64_t n, int64_t k) {
 extern "C" size_t vec_matmul_blocks_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (!mat_sizes(m, n, k) || m == 0 || n == 0) return 0;
     size_t most = 0;  // of all types and alignments
-    for (int form = 0; form < 8; ++form) {
-        const bool native = form & 4;
-        if (native && !mat_native(VEC_BF16, k)) break;
-        const size_t need = mat_plan(m, n, k, form & 1, form & 2, native).workspace;
+    for (int form = 0; form < 4; ++form) {
+        const size_t need = mat_plan(m, n, k, form & 1, form & 2).workspace;
         most = need > most ? need : most;
     }
     return most;
@@ -100,7 +88,7 @@ extern "C" int vec_matmul_blocks(const void *a, int64_t ld_a, int a_type, const 
     const bool pow2 = scale_type == VEC_E8M0;
     const bool async = (((uintptr_t)a | (uintptr_t)b | (uintptr_t)ld_a | (uintptr_t)ld_b) & 15u) == 0 && ld_a < (1 << 23) && ld_b < (1 << 23) &&
                        ld_a_scales < (1 << 21) && ld_b_scales < (1 << 21);
-    const MatPlan plan = mat_plan(m, n, k, pow2, async, mat_native(c_type, k));
+    const MatPlan plan = mat_plan(m, n, k, pow2, async);
     if (plan.workspace > 0) {
         const size_t need = vec_matmul_blocks_workspace_bytes(m, n, k);
         VEC_REQUIRE(workspace && ((uintptr_t)workspace & 255u) == 0, "vec_matmul_blocks: workspace null or not 256-byte aligned");

@@ -1,12 +1,10 @@
 // One translation unit per pair of factor types: MAT_FA and MAT_FB are 1 for E5M2.
 #include "vec_matmul.h"
 
-template <bool P2, bool ASYNC, int WM, int WN, int MI, int NI, bool NATIVE = false>
+template <bool P2, bool ASYNC, int WM, int WN, int MI, int NI>
 static int go_tiles(const MatArgs &p, hipStream_t s) {
     constexpr int rows = WM * MI * 16 + WN * NI * 16, lds = 2 * rows * 132;
-    void (*k)(MatArgs);
-    if constexpr (NATIVE) k = &k_vec_mat8<MAT_FA, MAT_FB, P2, ASYNC, WM, WN, MI, NI>;
-    else k = &k_vec_mat<MAT_FA, MAT_FB, P2, ASYNC, WM, WN, MI, NI>;
+    void (*const k)(MatArgs) = &k_vec_mat<MAT_FA, MAT_FB, P2, ASYNC, WM, WN, MI, NI>;
     QADC_HIP_TRY(hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     hipLaunchKernelGGL(k, dim3((unsigned)p.tm * (unsigned)p.tn * (unsigned)p.splits), dim3(64 * WM * WN), lds, s, p);
     QADC_LAUNCH_CHECK("k_vec_mat");
@@ -23,10 +21,6 @@ template <bool P2>
 static int go(const MatArgs &p, const MatPlan &plan, bool async, hipStream_t s) {
     if (plan.few == 1) return go_few<P2, 1>(p, plan, s);
     if (plan.few == 2) return go_few<P2, 2>(p, plan, s);
-    if (plan.native) {
-        if (!async) return go_tiles<P2, false, 2, 2, 4, 4, true>(p, s);
-        return plan.tile == MAT_256 ? go_tiles<P2, true, 2, 4, 8, 4, true>(p, s) : go_tiles<P2, true, 2, 2, 4, 4, true>(p, s);
-    }
     if (!async) return go_tiles<P2, false, 2, 2, 4, 4>(p, s);
     if constexpr (P2)
         if (plan.tile == MAT_256) return go_tiles<P2, true, 2, 4, 8, 4>(p, s);
