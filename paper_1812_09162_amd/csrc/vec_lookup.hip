@@ -87,6 +87,7 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
 #define GRAD_FEW (1 << GRAD_POS)
 #define GRAD_BITS 10
 #define GRAD_TILE 4096   // keys that a block of 1024 threads of the sort takes
+#define GRAD_TILES_ALONE 128  // tiles of the sort whose counts every block adds up itself
 #define GRAD_CHUNK 64    // at most: shorter pieces, more waves where there are few (16,384 ids into 65,536 x 256: 18 us with 64)
 
 #define GRAD_WIDTHS(d, ...)          \
@@ -108,8 +109,9 @@ struct GradPlan {
     int passes, bits;   // of the sort
     int tiles, chunks;  // blocks of a pass; pieces of the sum,
     int len;            // so many positions each
+    int seg, segs;      // tiles of a segment, and segments, where the counts become running sums first; else 0
     int dpad;           // floats of a partial row
-    size_t key0, key1, pos0, pos1, counts, begins, part, total;
+    size_t key0, key1, pos0, pos1, counts, sums, begins, part, total;
 };
 
 static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
@@ -123,6 +125,11 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
     p.tiles = (int)((n + GRAD_TILE - 1) / GRAD_TILE);
     p.len = n <= 32768 ? GRAD_CHUNK / 4 : (n <= 131072 ? GRAD_CHUNK / 2 : GRAD_CHUNK);
     p.chunks = (int)((n + p.len - 1) / p.len);
+    if (p.tiles > GRAD_TILES_ALONE) {
+        p.seg = 1;
+        while ((int64_t)p.seg * p.seg < p.tiles) p.seg *= 2;
+        p.segs = (p.tiles + p.seg - 1) / p.seg;
+    }
     p.dpad = (d + 7) & ~7;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
@@ -131,6 +138,7 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
     p.pos0 = take((size_t)n * 4);
     p.pos1 = take((size_t)n * 4);
     p.counts = take(((size_t)p.tiles << p.bits) * 4);
+    p.sums = p.segs > 0 ? take(((size_t)(p.segs + 1) << p.bits) * 4) : 0;
     p.begins = take((size_t)rows * 4);
     p.part = take((size_t)p.chunks * 2 * p.dpad * 4);
     p.total = at;
@@ -319,15 +327,38 @@ k_vec_grad_count(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, 
     if ((int)threadIdx.x < nb) counts[((size_t)blockIdx.x << bits) + threadIdx.x] = h[threadIdx.x];
 }
 
+// Running sums of the counts over many tiles, in place: a block takes a segment of them, thread b bucket b; sums[segment][bucket] becomes the segment's.
+// Sixteen counts are read before any is written.
+__global__ void __launch_bounds__(1024)
+k_vec_grad_running(uint32_t *counts, int tiles, int seg, int bits, uint32_t *__restrict__ sums) {
+    if (threadIdx.x >> bits) return;
+    const int t0 = blockIdx.x * seg, t1 = t0 + seg < tiles ? t0 + seg : tiles;
+    uint32_t *const c = counts + threadIdx.x;
+    uint32_t sum = 0;
+    for (int t = t0; t < t1; t += 16) {
+        uint32_t v[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) v[u] = t + u < t1 ? c[(size_t)(t + u) << bits] : 0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            if (t + u < t1) c[(size_t)(t + u) << bits] = sum;
+            sum += v[u];
+        }
+    }
+    sums[((size_t)blockIdx.x << bits) + threadIdx.x] = sum;
+}
+
 // A tile's keys to their places: those of one bucket keep their order.  Thread b adds up the sizes of bucket b over the tiles, of those
 // before this one and of all; running sums over the buckets then say where the tile's keys go.  (A kernel of its own for these sums
-// took 5 us, the loads here about 2.)  Wave w holds the tile's w-th sixteenth, 64 keys at a time; a key's rank among them is
+// took 5 us, the loads here about 2 with 64 tiles.  They grow with the square of the tiles, so that more than GRAD_TILES_ALONE have k_vec_grad_running make them, over the tiles
+// of a segment and then over the segments.  us, by the blocks / by k_vec_grad_running: into 900,000 x 8, 64 tiles 70 / 74, 128 98 / 95, 256 168 / 152,
+// 1024 760 / 442; into 500 x 64 37 / 39, 52 / 52, 88 / 84, 382 / 303.)  Wave w holds the tile's w-th sixteenth, 64 keys at a time; a key's rank among them is
 // the number of lower lanes with the same bucket, found bit by bit with ballots.
 template <class ID, class TT>
 __global__ void __launch_bounds__(1024)
 k_vec_grad_place(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ pos, int64_t n,
-                 int64_t rows, int shift, int bits, const uint32_t *__restrict__ counts, int tiles,
-                 uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out, GradClear z) {
+                 int64_t rows, int shift, int bits, const uint32_t *__restrict__ counts, int tiles, int seg, const uint32_t *__restrict__ sums,
+                 const uint32_t *__restrict__ totals, uint32_t *__restrict__ keys_out, uint32_t *__restrict__ pos_out, GradClear z) {
     if (grad_clear<TT>(z)) return;
     extern __shared__ uint32_t next[];  // [16 waves][buckets]: a wave's keys of a bucket, then where its next one goes
     __shared__ uint32_t part[16];
@@ -341,7 +372,12 @@ k_vec_grad_place(const ID *__restrict__ ids, const uint32_t *__restrict__ keys, 
         from[u] = i < n && pos ? pos[i] : (uint32_t)i;
     }
     uint32_t before_tile = 0, total = 0;
-    if ((int)threadIdx.x < nb) {
+    if (seg > 0) {
+        if ((int)threadIdx.x < nb) {
+            before_tile = counts[((size_t)blockIdx.x << bits) + threadIdx.x] + sums[((size_t)(blockIdx.x / seg) << bits) + threadIdx.x];
+            total = totals[threadIdx.x];
+        }
+    } else if ((int)threadIdx.x < nb) {
         const uint32_t *c = counts + threadIdx.x;
 #pragma unroll 16
         for (int t = 0; t < tiles; ++t) {
@@ -539,6 +575,7 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
     char *ws = (char *)workspace;
     uint32_t *key[2] = {(uint32_t *)(ws + p.key0), (uint32_t *)(ws + p.key1)}, *pos[2] = {(uint32_t *)(ws + p.pos0), (uint32_t *)(ws + p.pos1)};
     uint32_t *counts = (uint32_t *)(ws + p.counts);
+    uint32_t *sums = (uint32_t *)(ws + p.sums), *totals = sums + ((size_t)p.segs << p.bits);
     uint32_t *begins = (uint32_t *)(ws + p.begins);
     float *part = (float *)(ws + p.part);
     // a pass's share of the rows to clear, 32 KB and more a block
@@ -562,10 +599,15 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
             hipLaunchKernelGGL((k_vec_grad_count<int32_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int32_t *)ids, ki, n, rows, shift, p.bits, counts);
         else
             hipLaunchKernelGGL((k_vec_grad_count<int64_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int64_t *)ids, ki, n, rows, shift, p.bits, counts);
+        if (p.segs > 0) {
+            const dim3 threads(p.bits < 6 ? 64 : 1u << p.bits);
+            hipLaunchKernelGGL(k_vec_grad_running, dim3((unsigned)p.segs), threads, 0, s, counts, p.tiles, p.seg, p.bits, sums);
+            hipLaunchKernelGGL(k_vec_grad_running, dim3(1), threads, 0, s, sums, p.segs, p.segs, p.bits, totals);
+        }
         const dim3 grid = share(pass, (unsigned)p.tiles);
 #define GO(ID, TT)                                                                                                         \
     hipLaunchKernelGGL((k_vec_grad_place<ID, TT>), grid, dim3(1024), (size_t)64 << p.bits, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
-                       counts, p.tiles, key[pass & 1], pos[pass & 1], z)
+                       counts, p.tiles, p.seg, sums, totals, key[pass & 1], pos[pass & 1], z)
         VEC_TYPED(table_type, TT, if (id_bytes == 4) GO(int32_t, TT); else GO(int64_t, TT));
 #undef GO
     }

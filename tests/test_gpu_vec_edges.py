@@ -33,3 +33,61 @@ def test_sums_whose_large_terms_cancel(qb, m, n, k, aligned, ta, tb, st):
     for to in (BF16, F32):
         got = qb.vec_matmul_blocks(a, sa, b, sb, dtype=to)
         assert bool((got == 8).all()), (to, float(got.min()), float(got.max()))
+
+
+# ---------------------------------------------------------- gradient by id --
+def grad64(g, ids, rows, scale):
+    """Sums by id, of magnitudes by id, and counts, in 64 bits, on the host."""
+    g, ids = g.cpu(), ids.cpu()
+    ok = ((ids >= 0) & (ids < rows)).nonzero()[:, 0]
+    at, v = ids[ok].long(), g[ok].double() * float(torch.tensor(scale, dtype=F32))
+    sums = [torch.zeros((rows, x.shape[1]), dtype=torch.float64).index_add_(0, at, x) for x in (v, v.abs(), torch.ones((len(ok), 1), dtype=torch.float64))]
+    return [x.to(dev()) for x in sums]
+
+
+def check_grad(qb, g, ids, rows, to, scale=0.77):
+    want, size, count = grad64(g, ids, rows, scale)
+    got = qb.vec_lookup_grad(g, ids, rows, scale=scale, dtype=to)
+    close(got, want, U * (count + 1) * size * 1.001 + half_step(want, to))
+    assert bool((got[count[:, 0] == 0] == 0).all())
+    assert torch.equal(got, qb.vec_lookup_grad(g, ids, rows, scale=scale, dtype=to))
+    base, store = framed(rnd((rows, g.shape[1]), 6, to))
+    was, old = store.clone(), base.clone()
+    qb.vec_lookup_grad(g, ids, rows, scale=scale, out=base, accumulate=True)
+    ref = old.double() + want
+    close(base, ref, U * ((count + 2) * size + old.double().abs()) * 1.001 + half_step(ref, to))
+    assert torch.equal(base[count[:, 0] == 0], old[count[:, 0] == 0]) and untouched(base, store, was)
+
+
+@pytest.mark.parametrize("t,to", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("rows,d,n,kind", [(100_003, 24, 262_144, "skew"), (5000, 130, 200_001, "skew"), (700, 9, 131_073, "one"), (40, 300, 140_000, "even"),
+                                           (3, 16, 500_003, "even"), (1_100_000, 5, 300_000, "outside"), (70_000, 8, 1_200_007, "skew"), (900, 4, 2_100_001, "one"),
+                                           (600_000, 3, 1_048_577, "even"), (3, 2, 700_003, "even")])
+def test_gradient_of_many_ids(qb, rows, d, n, kind, t, to):
+    """Whole pieces of 64 positions, ids whose runs cross thousands of them, up to hundreds of tiles of the sort."""
+    u = torch.rand((n,), generator=torch.Generator().manual_seed(rows), dtype=torch.float64)
+    ids = {"even": (u * rows).long(), "skew": (rows ** u - 1).long().clamp(0, rows - 1), "one": torch.where(u < 0.9, rows // 2, (u * rows).long()),
+           "outside": torch.where(u < 0.3, -1, ((u * 2 - 0.7) * 1.1 * rows).long())}[kind].to(dev())
+    check_grad(qb, rnd((n, d), 5, t), ids if n % 2 else ids.int(), rows, to)
+
+
+def test_time_of_the_gradient_grows_with_the_ids(qb):
+    """32 times as many ids, into the same table: not more than 64 times the time (sums over all pairs of tiles would take 1024 times)."""
+    def us(n):
+        ids = torch.randint(0, 1 << 20, (n,), device=dev(), dtype=torch.int32, generator=torch.Generator(device=dev()).manual_seed(1))
+        g = torch.ones((n, 1), dtype=BF16, device=dev())
+        out = torch.empty((1 << 20, 1), dtype=F32, device=dev())
+        w = torch.empty(qb.vec_lookup_grad_workspace_bytes(n, 1 << 20, 1), dtype=torch.uint8, device=dev())
+        best = math.inf
+        for _ in range(3):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            qb.vec_lookup_grad(g, ids, 1 << 20, out=out, workspace=w)
+            b.record()
+            b.synchronize()
+            best = min(best, a.elapsed_time(b) * 1000)
+        assert torch.equal(out[:, 0], torch.bincount(ids, minlength=1 << 20).float())
+        return best
+    few, many = us(1 << 20), us(1 << 25)
+    print(f"2^20 ids {few:.0f} us, 2^25 {many:.0f} us")
+    assert many <= 64 * few, (few, many)
