@@ -88,7 +88,7 @@ int vec_norm_grad(const void *dy, int64_t ld_dy, const void *h, int64_t ld_h, co
  *   scale = E8M0: the smallest power of two with a <= L * scale, at least 2^-127
  *           F32:  a / L, at least 2^-126          1 where a = 0
  *   q     = the float32 quotient x / scale, rounded to q_type; NaN, and infinity in E4M3, become NaN
- *   x [dev][n][d] of type F32, BF16 or F16
+ *   x [dev][n][d] of type F32, BF16 or F16; n ceil(d / 128) < 2^35
  *   transposed == 0: blocks run along a row:   q [dev][n][d], scales [dev][n][ceil(d / 128)]
  *   transposed == 1: blocks run along a column, and the result is transposed (the factors of a weight gradient):
  *                                              q [dev][d][n], scales [dev][d][ceil(n / 128)]
@@ -101,7 +101,8 @@ int vec_quantize_blocks(const void *x, int64_t ld_x, int type, int64_t n, int64_
  *   a [dev][m][k], b [dev][n][k] of type E4M3 or E5M2 (each its own); both scales of scale_type E8M0 or F32
  *   c [dev][m][n] of c_type F32, BF16 or F16
  * Products are exact and their sums are in float32.
- * E8M0 scales are applied to the values (what is below 2^-126 may then count as zero), F32 scales to each block's sum.  k == 0 gives zeros.  m, n, k < 2^31.
+ * E8M0 scales are applied to the values (what is below 2^-126 may then count as zero), F32 scales to each block's sum.  k == 0 gives zeros.  m, n, k < 2^31, and
+ * with m > 32 less than 2^24 tiles of 128 x 128 of c.
  *   workspace >= vec_matmul_blocks_workspace_bytes(m, n, k) (may be 0), 256-byte aligned, any content
  */
 size_t vec_matmul_blocks_workspace_bytes(int64_t m, int64_t n, int64_t k);

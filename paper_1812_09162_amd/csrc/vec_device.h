@@ -216,7 +216,16 @@ __device__ __forceinline__ void vec_put_scale(void *scales, int64_t at, const Ve
     else ((float *)scales)[at] = s.scale;
 }
 
+// The block's number in a launch of vec_grid's; the last ones may be beyond what was asked for.
+__device__ __forceinline__ int64_t vec_block() { return blockIdx.y == 0 ? (int64_t)blockIdx.x : (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ---------------------------------------------------------------------- host
+#define VEC_MAX_BLOCKS 0x7fffffffLL
+// A grid of at least `blocks` blocks (1 to VEC_MAX_BLOCKS).  One dimension's blocks times threads stay below 2^32, so that more take a second.
+static inline dim3 vec_grid(int64_t blocks, int threads) {
+    const int64_t most = 0xffffffffLL / threads, y = (blocks + most - 1) / most;
+    return dim3((unsigned)((blocks + y - 1) / y), (unsigned)y);
+}
 static inline bool vec_is_wide(int t) { return t == VEC_F32 || t == VEC_BF16 || t == VEC_F16; }
 static inline bool vec_is_8bit(int t) { return t == VEC_E4M3 || t == VEC_E5M2; }
 static inline bool vec_is_scale(int t) { return t == VEC_E8M0 || t == VEC_F32; }

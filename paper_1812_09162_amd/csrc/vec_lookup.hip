@@ -9,9 +9,9 @@ template <class TI, class TO, class ID>
 __global__ void __launch_bounds__(256)
 k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table, const ID *__restrict__ ids, int64_t n,
              float scale, TO *__restrict__ out, int64_t ld_out, int rpb, int pieces, uint32_t magic) {
-    const int64_t row0 = (int64_t)blockIdx.x * rpb;
+    const int64_t row0 = vec_block() * rpb;
     const int nrow = (int)(n - row0 < rpb ? n - row0 : rpb);
-    const int total = nrow * pieces;
+    const int total = nrow * pieces;  // (0 or less behind the last row)
     for (int e0 = threadIdx.x; e0 < total; e0 += 256 * 4) {
         vec_pack<TI> v[4];
         int64_t to[4];
@@ -53,12 +53,12 @@ extern "C" int vec_lookup(const void *table, int64_t rows, int d, int64_t ld_tab
     // 1024 pieces a block, whole rows; a row of more is a block of its own
     const int rpb = pieces >= 1024 ? 1 : 1024 / pieces;
     const int64_t blocks = (n + rpb - 1) / rpb;
-    VEC_REQUIRE(blocks <= 0x7fffffffLL, "vec_lookup: n=%lld too large for one call", (long long)n);
+    VEC_REQUIRE(blocks <= VEC_MAX_BLOCKS, "vec_lookup: n=%lld too large for one call", (long long)n);
     // e / pieces for e < 1024, pieces > 1: exact as 1024 pieces < 2^32
     const uint32_t magic = (uint32_t)((((uint64_t)1 << 32) + pieces - 1) / pieces);
     hipStream_t s = (hipStream_t)stream;
 #define GO(TI, TO, ID)                                                                                                    \
-    hipLaunchKernelGGL((k_vec_lookup<TI, TO, ID>), dim3((unsigned)blocks), dim3(256), 0, s, (const TI *)table, rows, d,    \
+    hipLaunchKernelGGL((k_vec_lookup<TI, TO, ID>), vec_grid(blocks, 256), dim3(256), 0, s, (const TI *)table, rows, d,    \
                        ld_table, (const ID *)ids, n, scale, (TO *)out, ld_out, rpb, pieces, magic)
     VEC_TYPED(table_type, TI, VEC_TYPED(out_type, TO, if (id_bytes == 4) GO(TI, TO, int32_t); else GO(TI, TO, int64_t)));
 #undef GO

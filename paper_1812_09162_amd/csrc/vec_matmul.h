@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(64 * MAT_FEW_WAVES)
 k_vec_mat_few(const MatArgs p, int kshare) {
     __shared__ vec_f4 sums[MAT_FEW_WAVES][MF][64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t tile = (int64_t)blockIdx.x * (MAT_FEW_WAVES / kshare) + wave / kshare;
+    const int64_t tile = vec_block() * (MAT_FEW_WAVES / kshare) + wave / kshare;
     const int share = wave % kshare;
     const int steps = (int)((p.k + VEC_BLOCK - 1) / VEC_BLOCK);
     const int64_t n0 = tile * 16, nr = n0 + (lane & 15) < p.n ? n0 + (lane & 15) : p.n - 1;

@@ -35,7 +35,7 @@ static MatPlan mat_plan(int64_t m, int64_t n, int64_t k, bool pow2, bool async) 
     for (int tile = MAT_128; tile <= (async && pow2 ? MAT_256 : MAT_128); ++tile) {
         const int side = tile == MAT_256 ? 256 : 128;
         const int64_t tm = (m + side - 1) / side, tn = (n + side - 1) / side;
-        if (tm * tn > 0x7fffffffLL) continue;
+        if (tm * tn * (tile == MAT_256 ? 512 : 256) > 0xffffffffLL) continue;  // (threads of a launch)
         for (int64_t s = 1; s <= 32 && (s == 1 || (s * 4 <= steps && tm * tn * s <= 512)); ++s) {
             const int64_t per = (steps + s - 1) / s, rounds = (tm * tn * s + 255) / 256;
             const bool one = rounds == 1;

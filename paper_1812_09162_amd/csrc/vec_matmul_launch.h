@@ -13,7 +13,7 @@ static int go_tiles(const MatArgs &p, hipStream_t s) {
 template <bool P2, int MF>
 static int go_few(const MatArgs &p, const MatPlan &plan, hipStream_t s) {
     const int64_t tiles = (p.n + 15) / 16, per = MAT_FEW_WAVES / plan.kshare;
-    hipLaunchKernelGGL((k_vec_mat_few<MAT_FA, MAT_FB, P2, MF>), dim3((unsigned)((tiles + per - 1) / per)), dim3(64 * MAT_FEW_WAVES), 0, s, p, plan.kshare);
+    hipLaunchKernelGGL((k_vec_mat_few<MAT_FA, MAT_FB, P2, MF>), vec_grid((tiles + per - 1) / per, 64 * MAT_FEW_WAVES), dim3(64 * MAT_FEW_WAVES), 0, s, p, plan.kshare);
     QADC_LAUNCH_CHECK("k_vec_mat_few");
     return PQ_OK;
 }

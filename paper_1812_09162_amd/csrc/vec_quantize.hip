@@ -12,7 +12,7 @@ struct QuantOut {
 template <class T>
 __global__ void __launch_bounds__(256)
 k_vec_quantize(const T *__restrict__ x, int64_t ld, int64_t n, int64_t d, int64_t nb, QuantOut o) {
-    const int64_t b = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;  // block of the matrix
+    const int64_t b = vec_block() * 16 + threadIdx.x / 16;  // block of the matrix
     const int64_t row = b / nb, col = (b - row * nb) * VEC_BLOCK + (threadIdx.x & 15) * 8;
     const bool in = row < n;
     const vec_f8 f = vec_wide<T>(vec_load(x + (in ? row * ld + col : 0), in ? d - col : 0, col));
@@ -31,7 +31,8 @@ __global__ void __launch_bounds__(256)
 k_vec_quantize_t(const T *__restrict__ x, int64_t ld, int64_t n, int64_t d, int64_t ncol, QuantOut o) {
     __shared__ float top[16][VEC_BLOCK];
     __shared__ __align__(16) uint8_t tile[VEC_BLOCK * QT_LD];
-    const int64_t rb = blockIdx.x / ncol, row0 = rb * VEC_BLOCK, col0 = (blockIdx.x - rb * ncol) * VEC_BLOCK;
+    const int64_t b = vec_block(), rb = b / ncol, row0 = rb * VEC_BLOCK, col0 = (b - rb * ncol) * VEC_BLOCK;
+    if (row0 >= n) return;
     const int tr = threadIdx.x / 16, tc = threadIdx.x & 15;
     vec_pack<T> v[8];
 #pragma unroll
@@ -97,11 +98,11 @@ extern "C" int vec_quantize_blocks(const void *x, int64_t ld_x, int type, int64_
     VEC_REQUIRE(n < ((int64_t)1 << 40) && d < ((int64_t)1 << 40) && nb <= ((int64_t)1 << 40) / (transposed ? ncol : n), "vec_quantize_blocks: n=%lld, d=%lld too large",
                 (long long)n, (long long)d);
     const int64_t blocks = transposed ? nb * ncol : (n * nb + 15) / 16;
-    VEC_REQUIRE(blocks <= 0x7fffffffLL, "vec_quantize_blocks: n=%lld, d=%lld too large for one call", (long long)n, (long long)d);
+    VEC_REQUIRE(blocks <= VEC_MAX_BLOCKS, "vec_quantize_blocks: n=%lld, d=%lld too large for one call", (long long)n, (long long)d);
     if (transposed)
-        VEC_TYPED(type, T, hipLaunchKernelGGL((k_vec_quantize_t<T>), dim3((unsigned)blocks), dim3(256), 0, s, (const T *)x, ld_x, n, d, ncol, o));
+        VEC_TYPED(type, T, hipLaunchKernelGGL((k_vec_quantize_t<T>), vec_grid(blocks, 256), dim3(256), 0, s, (const T *)x, ld_x, n, d, ncol, o));
     else
-        VEC_TYPED(type, T, hipLaunchKernelGGL((k_vec_quantize<T>), dim3((unsigned)blocks), dim3(256), 0, s, (const T *)x, ld_x, n, d, nb, o));
+        VEC_TYPED(type, T, hipLaunchKernelGGL((k_vec_quantize<T>), vec_grid(blocks, 256), dim3(256), 0, s, (const T *)x, ld_x, n, d, nb, o));
     QADC_LAUNCH_CHECK(transposed ? "k_vec_quantize_t" : "k_vec_quantize");
     return PQ_OK;
 }

@@ -35,6 +35,65 @@ def test_sums_whose_large_terms_cancel(qb, m, n, k, aligned, ta, tb, st):
         assert bool((got == 8).all()), (to, float(got.min()), float(got.max()))
 
 
+# --------------------------------------------------------------- quantizer --
+def test_more_blocks_of_rows_than_a_launch_has_in_a_row(qb):
+    """2^28 + 100 rows of one value: more blocks of threads than one dimension of a launch takes."""
+    n = (1 << 28) + 100
+    x = torch.zeros((n, 1), dtype=BF16, device=dev())
+    at = torch.tensor([0, 1, (1 << 27) + 5, (1 << 28) - 1, 1 << 28, n - 1], device=dev())
+    vals = torch.tensor([1.0, -3.0, 5.0, 0.25, -7.0, 448.0], device=dev()).to(BF16)[:, None]
+    x[at] = vals
+    q, s = torch.full((n, 1), 9, dtype=torch.uint8, device=dev()), torch.full((n, 1), 9, dtype=torch.uint8, device=dev())
+    qb.vec_quantize_blocks(x, out=(q.view(E4M3), s.view(E8M0)))
+    want, ws = quantized(vals.cpu(), E4M3, E8M0)
+    assert same_values(q[at].view(E4M3), want) and torch.equal(s[at].view(E8M0).cpu().double(), ws)
+    assert int((q != 0).sum()) == len(at) and int((s != 127).sum()) == int((ws != 1).sum())
+
+
+def test_more_blocks_of_columns_than_a_launch_has_in_a_row(qb):
+    """2^31 + 200 rows of one value, in blocks along the column."""
+    n = (1 << 31) + 200
+    x = torch.zeros((n, 1), dtype=BF16, device=dev())
+    at = torch.tensor([0, 300, (1 << 30) + 5, (1 << 31) - 1, 1 << 31, n - 1], device=dev())
+    vals = torch.tensor([1.0, -3.0, 5.0, 0.25, -7.0, 448.0], device=dev()).to(BF16)[:, None]
+    x[at] = vals
+    q, s = torch.full((1, n), 9, dtype=torch.uint8, device=dev()), torch.full((1, -(-n // 128)), 9, dtype=torch.uint8, device=dev())
+    qb.vec_quantize_blocks(x, transposed=True, out=(q.view(E4M3), s.view(E8M0)))
+    want, ws = quantized(vals.cpu(), E4M3, E8M0)
+    assert same_values(q[0, at, None].view(E4M3), want) and torch.equal(s[0, at // 128, None].view(E8M0).cpu().double(), ws)
+    assert int((q != 0).sum()) == len(at) and int((s != 127).sum()) == int((ws != 1).sum())
+
+
+def test_look_up_of_more_rows_than_a_launch_has_blocks(qb):
+    """2^24 + 3 rows of 4097 values, a block of threads each."""
+    n, d = (1 << 24) + 3, 4097
+    table = rnd((5, d), 1, BF16)
+    ids = torch.zeros(n, dtype=torch.int32, device=dev())
+    at = torch.tensor([1, (1 << 23) + 1, (1 << 24) - 1, 1 << 24, n - 1], device=dev())
+    ids[at] = torch.tensor([1, 2, 3, 4, -1], dtype=torch.int32, device=dev())
+    out = torch.empty((n, d), dtype=BF16, device=dev())
+    qb.vec_lookup(table, ids, out=out)
+    assert torch.equal(out[at[:4]], table[1:]) and bool((out[n - 1] == 0).all())
+    for i in (0, 2, 1 << 23, (1 << 24) - 2, (1 << 24) + 1):
+        assert torch.equal(out[i], table[0])
+    del out
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("st", [E8M0, F32])
+def test_one_row_against_very_many(qb, st):
+    """2^30 + 40 rows of sixteen bytes: more blocks of threads than one dimension of a launch takes."""
+    n, k = (1 << 30) + 40, 16
+    b = torch.zeros((n, k), dtype=torch.uint8, device=dev())
+    sb = torch.full((n, 1), 127, dtype=torch.uint8, device=dev()).view(E8M0) if st == E8M0 else torch.ones((n, 1), device=dev())
+    at = torch.tensor([0, 17, (1 << 29) + 1, (1 << 30) - 1, 1 << 30, n - 1], device=dev())
+    vals = torch.randint(-8, 9, (6, k), generator=torch.Generator().manual_seed(1)).float().to(E4M3).to(dev())
+    b[at] = vals.view(torch.uint8)
+    a, sa = torch.ones((1, k), device=dev()).to(E4M3), torch.ones((1, 1), device=dev()).to(st)
+    got = qb.vec_matmul_blocks(a, sa, b.view(E4M3), sb)
+    assert torch.equal(got[0, at].float(), vals.float().sum(1)) and int((got != 0).sum()) == int((vals.float().sum(1) != 0).sum())
+
+
 # ---------------------------------------------------------- gradient by id --
 def grad64(g, ids, rows, scale):
     """Sums by id, of magnitudes by id, and counts, in 64 bits, on the host."""

@@ -155,3 +155,10 @@ def test_rows_of_too_many_columns_are_refused():
     for d in ((1 << 24) + 1, (1 << 31) - 1):
         refused(lib.vec_lookup(P, 5, d, d, BF16, P, 8, 3, 1.0, P, d, BF16, None), f"d={d}")
         refused(lib.vec_lookup_grad(P, 3, d, d, BF16, P, 8, 1.0, 0, P, 5, d, BF16, P, 1 << 40, None), f"d={d}")
+
+
+def test_products_of_more_tiles_than_a_launch_has_threads_are_refused():
+    """2^24 tiles of 256 threads, 2^23 of 512: 2^32 threads."""
+    n = (1 << 31) - 1
+    refused(matmul(m=33, n=n, k=16, lda=16, ldb=16, ldas=1, ldbs=1, ldc=n), "too large")
+    refused(matmul(m=33, n=n, k=16, lda=17, ldb=17, ldas=1, ldbs=1, ldc=n), "too large")
