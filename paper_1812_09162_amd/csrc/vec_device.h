@@ -171,13 +171,15 @@ __device__ __forceinline__ VecScale vec_scale(float top, bool e5m2, bool pow2) {
     if (!pow2) {
         s.scale = top == 0.0f ? 1.0f : fmaxf(top / (e5m2 ? 57344.0f : 448.0f), 1.17549435e-38f);
         s.inverse = 1.0f / s.scale;
-        s.divide = s.scale < 7.9e-31f || (__float_as_uint(s.scale) & 0x7fffffu) == 0x7fffffu;
+        s.divide = s.scale < 2.58493941e-26f || (__float_as_uint(s.scale) & 0x7fffffu) == 0x7fffffu;
     }
     return s;
 }
 // f over the scale as a division rounds it, in three operations: with r = 1 / scale rounded to nearest, q = f r is within one step of the
 // quotient, f - q scale is exact, and q + r (f - q scale) rounds to the quotient's nearest (Markstein, 1990) unless scale's bits are
-// all ones or the remainder falls below the smallest numbers; those take the division.
+// all ones or the remainder falls below the smallest numbers; those take the division.  The remainder is a multiple of q's last bit times scale's.
+// Quotients matter from 2^-18 on (E5M2's smallest border between two values is 2^-17), where q's last bit is 2^-41 or more: with scales from 2^-85
+// on the product is 2^-149, the smallest number, or more.  (Searched next to such borders, scales of 2^-88 and less gave other bytes.)
 __device__ __forceinline__ float vec_quotient(float f, const VecScale &s) {
     const float q = f * s.inverse;
     return __fmaf_rn(__fmaf_rn(-q, s.scale, f), s.inverse, q);

@@ -36,6 +36,40 @@ def test_sums_whose_large_terms_cancel(qb, m, n, k, aligned, ta, tb, st):
 
 
 # --------------------------------------------------------------- quantizer --
+def test_quotients_of_tiny_scales(qb):
+    """Quotients next to a tie of the 8-bit type, with scales so small that a remainder's last bits lie below the smallest float32."""
+    hexes = {E4M3: [("0x1.bffff8p-93", "0x1.fffff8p-112"), ("0x1.bffffap-91", "0x1.fffffcp-110"), ("0x1.bffff4p-89", "0x1.fffff4p-108"),
+                    ("0x1.bffffap-87", "0x1.fffffcp-106"), ("0x1.c00004p-87", "0x1.800002p-104")],
+             E5M2: [("0x1.bfd04p-84", "0x1.ffc97p-117"), ("0x1.c0154p-85", "0x1.400f2ep-115"), ("0x1.bffffap-83", "0x1.fffffcp-116"),
+                    ("0x1.bffff6p-80", "0x1.fffff4p-113"), ("0x1.c00008p-79", "0x1.c00006p-109"), ("0x1.bffffep-76", "0x1p-108"),
+                    ("0x1.bffffap-73", "0x1.fffffcp-106"), ("0x1.c00004p-73", "0x1.800002p-104")]}
+    for qt, pairs in hexes.items():
+        x = torch.zeros((len(pairs), 128))
+        for i, (top, f) in enumerate(pairs):
+            x[i, 0], x[i, 1], x[i, 2] = float.fromhex(top), float.fromhex(f), -float.fromhex(f)
+        want, ws = quantized(x, qt, F32)
+        for transposed in (False, True):
+            q, s = qb.vec_quantize_blocks((x.t().contiguous() if transposed else x).to(dev()), dtype=qt, scale_dtype=F32, transposed=transposed)
+            assert torch.equal(s.cpu().double(), ws) and same_values(q, want), qt
+
+
+@pytest.mark.parametrize("qt", [E4M3, E5M2])
+def test_quotients_next_to_ties(qb, qt):
+    """Scales of every power from 2^-126 to 2^-60, values within three steps of a tie."""
+    g = torch.Generator().manual_seed(7)
+    n, least = 67 * 40, 2.0 ** (-10 if qt == E4M3 else -17)
+    power = torch.arange(-126, -59).repeat_interleave(40).double()
+    scale = ((1 + torch.randint(0, 1 << 23, (n,), generator=g).double() * 2 ** -23) * torch.exp2(power)).float()
+    scale[::4] = (torch.exp2(power[::4]) * (2 - torch.randint(1, 8, (len(power[::4]),), generator=g).double() * 2 ** -23)).float()
+    ties = (2 * torch.randint(0, 6, (n, 127), generator=g) + 1).double() * least
+    f = (ties * scale[:, None].double()).float()
+    f = (f.view(torch.int32) + torch.randint(-3, 4, (n, 127), generator=g, dtype=torch.int32)).clamp(min=0).view(torch.float32)
+    x = torch.cat([(scale * (448.0 if qt == E4M3 else 57344.0))[:, None], f], 1)
+    want, ws = quantized(x, qt, F32)
+    q, s = qb.vec_quantize_blocks(x.to(dev()), dtype=qt, scale_dtype=F32)
+    assert torch.equal(s.cpu().double(), ws) and same_values(q, want)
+
+
 def test_more_blocks_of_rows_than_a_launch_has_in_a_row(qb):
     """2^28 + 100 rows of one value: more blocks of threads than one dimension of a launch takes."""
     n = (1 << 28) + 100
