@@ -16,6 +16,7 @@ k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table
         vec_pack<TI> v[4];
         int64_t to[4];
         int left[4];
+        float by[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int e = e0 + u * 256;
@@ -26,6 +27,7 @@ k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table
             const int64_t id = (int64_t)ids[row0 + r];
             const bool known = id >= 0 && id < rows;
             left[u] = d - col;
+            by[u] = known ? scale : 0.0f;  // (zeros of an unknown id take no sign, infinity or NaN of the scale)
             to[u] = (row0 + r) * ld_out + col;
             v[u] = vec_load(table + (known ? id * ld_table + col : 0), known ? left[u] : 0, col);
         }
@@ -34,7 +36,7 @@ k_vec_lookup(const TI *__restrict__ table, int64_t rows, int d, int64_t ld_table
             if (left[u] > 0) {
                 vec_f8 f = vec_wide<TI>(v[u]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= scale;
+                for (int i = 0; i < 8; ++i) f[i] *= by[u];
                 vec_store(out + to[u], left[u], f);
             }
     }

@@ -128,6 +128,19 @@ def test_one_row_against_very_many(qb, st):
     assert torch.equal(got[0, at].float(), vals.float().sum(1)) and int((got != 0).sum()) == int((vals.float().sum(1) != 0).sum())
 
 
+# ----------------------------------------------------------------- look-up --
+@pytest.mark.parametrize("scale", [-2.0, math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("to", [F32, BF16, F16])
+def test_rows_of_unknown_ids_are_zeros(qb, scale, to):
+    """... whatever the scale, and zeros without a sign."""
+    table = rnd((6, 37), 1, to)
+    ids = torch.tensor([0, -1, 6, 5, -(2 ** 40), 2 ** 40], device=dev())
+    got = qb.vec_lookup(table, ids, scale=scale)
+    bits = got[[1, 2, 4, 5]].contiguous().view(torch.uint8)
+    assert bool((bits == 0).all())
+    assert same_values(got[[0, 3]], (table[[0, 5]].float() * scale).to(to))
+
+
 # ---------------------------------------------------------- gradient by id --
 def grad64(g, ids, rows, scale):
     """Sums by id, of magnitudes by id, and counts, in 64 bits, on the host."""
