@@ -533,6 +533,11 @@ class _Call:
             return n, d, t.data_ptr(), d or 1
         return (n, d, *self.rows(what, t, n, d, t.dtype))
 
+    def columns(self, d: int) -> None:
+        """(ctypes would pass the low 32 bits of a C int)"""
+        if d > 0x7FFFFFFF:
+            _refuse(self.name, f"d={d}")
+
     def vector(self, what: str, t: torch.Tensor, n: Optional[int] = None, dtype=None) -> int:
         if t.get_device() != self.index or (dtype is not None and t.dtype != dtype) or not t.is_contiguous() or (
                 n is not None and (t.dim() != 1 or t.numel() != n)):
@@ -585,6 +590,7 @@ def vec_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype
     """scale * table[ids] as [*ids.shape, d]; zeros where an id is outside the table (a search pads with -1)."""
     call = _Call("vec_lookup", table, stream)
     rows, d, ptr, ld = call.first_rows("table", table)
+    call.columns(d)
     idp, id_bytes = call.ids(ids)
     n = ids.numel()
     to = call.out_type(out, dtype, table.dtype)
@@ -613,6 +619,7 @@ def vec_lookup_grad(grad: torch.Tensor, ids: torch.Tensor, rows: int, scale: flo
             _refuse(call.name, "grad of other than two dimensions is contiguous")
         grad = grad.view(-1, grad.shape[-1])
     n, d = ids.numel(), grad.shape[1]
+    call.columns(d)
     ptr, ld = call.rows("grad", grad, n, d, grad.dtype)
     idp, id_bytes = call.ids(ids)
     if accumulate and out is None:
@@ -653,6 +660,7 @@ def vec_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Ten
     residual)."""
     call = _Call("vec_norm", x, stream)
     n, d, xp, ldx = call.first_rows("x", x)
+    call.columns(d)
     t = x.dtype
     rp = hp = yp = qp = sp = None
     ldr = ldh = ldy = ldq = lds = 0
@@ -693,6 +701,7 @@ def vec_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, dh: O
     `out`: the same two, to be written (dx may be dy or dh; dweight is float32)."""
     call = _Call("vec_norm_grad", dy, stream)
     n, d, yp, ldy = call.first_rows("dy", dy)
+    call.columns(d)
     t = dy.dtype
     hp, ldh = call.rows("h", h, n, d, t)
     ep, lde = call.rows("dh", dh, n, d, t) if dh is not None else (None, 0)

@@ -141,6 +141,17 @@ def test_rows_of_unknown_ids_are_zeros(qb, scale, to):
     assert same_values(got[[0, 3]], (table[[0, 5]].float() * scale).to(to))
 
 
+def test_rows_of_2_to_the_32_columns_are_refused(qb):
+    """Counts of columns are 32 bits behind the binding: 2^32 + 8 are not 8."""
+    wide = torch.empty((1, (1 << 32) + 8), dtype=BF16, device=dev())
+    ids = torch.zeros(1, dtype=torch.int64, device=dev())
+    for call in (lambda: qb.vec_lookup(wide, ids, out=wide), lambda: qb.vec_lookup_grad(wide, ids, 1, out=wide),
+                 lambda: qb.vec_norm(wide, wide[0], out=(wide, None, None, None)), lambda: qb.vec_norm_grad(wide, wide, wide[0])):
+        with pytest.raises(qb.QadcError) as e:
+            call()
+        assert e.value.code == qb.PQ_EINVAL and str((1 << 32) + 8) in str(e.value)
+
+
 # ---------------------------------------------------------- gradient by id --
 def grad64(g, ids, rows, scale):
     """Sums by id, of magnitudes by id, and counts, in 64 bits, on the host."""
