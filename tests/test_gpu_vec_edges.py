@@ -35,6 +35,46 @@ def test_sums_whose_large_terms_cancel(qb, m, n, k, aligned, ta, tb, st):
         assert bool((got == 8).all()), (to, float(got.min()), float(got.max()))
 
 
+@pytest.mark.parametrize("rows", [5, 70, 600])
+@pytest.mark.parametrize("k", [200, 640])
+def test_products_of_the_smallest_power(qb, rows, k):
+    """A scale byte of 0 is 2^-127 (what the quantizer gives to tiny blocks)."""
+    n, nb = 1500, -(-k // 128)
+    a, b = torch.full((rows, k), 256.0, device=dev()).to(E4M3), torch.full((n, k), 1.5, device=dev()).to(E4M3)
+    sa, sb = torch.zeros((rows, nb), dtype=torch.uint8, device=dev()).view(E8M0), torch.full((n, nb), 2.0 ** 119, device=dev()).to(E8M0)
+    want = k * 1.5
+    for x, sx, y, sy in ((a, sa, b, sb), (b[:rows], sb[:rows], a[:1].expand(n, k).contiguous(), sa[:1].expand(n, nb).contiguous())):
+        for to in (F32, BF16):
+            assert bool((qb.vec_matmul_blocks(x, sx, y, sy, dtype=to) == torch.tensor(want).to(to).to(dev())).all())
+
+
+@pytest.mark.parametrize("st", [E8M0, F32])
+@pytest.mark.parametrize("rows", [5, 70, 600])
+@pytest.mark.parametrize("k", [200, 640])
+def test_products_of_infinities_and_nan(qb, rows, k, st):
+    """Infinities of E5M2 meet positive, negative and zero factors; a NaN scale meets zeros."""
+    n, nb = 1500, -(-k // 128)
+    a, b = torch.ones((rows, k)), torch.ones((n, k))
+    sa, sb = torch.ones((rows, nb), device=dev()).to(st), torch.ones((n, nb), device=dev()).to(st)
+    a[2, 150], a[4, 7], a[4, k - 1] = math.inf, math.inf, -math.inf
+    a[1, :] = 0.0
+    b[11, 150], b[12, 150] = -1.0, 0.0
+    a, b = a.to(E5M2).to(dev()), b.to(E4M3).to(dev())
+    want = torch.full((rows, n), float(k), device=dev())
+    want[1] = 0
+    want[:, 11], want[:, 12] = want[:, 11] - 2 * (want[:, 11] != 0), want[:, 12] - 1.0 * (want[:, 12] != 0)
+    want[2], want[4] = math.inf, math.nan
+    want[2, 11], want[2, 12] = -math.inf, math.nan
+    if st == E8M0:
+        sb.view(torch.uint8)[20, 1] = 255
+    else:
+        sb[20, 1] = math.nan
+    want[:, 20] = math.nan
+    for to in (F32, F16, BF16):
+        got = qb.vec_matmul_blocks(a, sa, b, sb, dtype=to)
+        assert same_values(got, want.to(to)), to
+
+
 # --------------------------------------------------------------- quantizer --
 def test_quotients_of_tiny_scales(qb):
     """Quotients next to a tie of the 8-bit type, with scales so small that a remainder's last bits lie below the smallest float32."""
@@ -186,6 +226,25 @@ def test_gradient_of_many_ids(qb, rows, d, n, kind, t, to):
     ids = {"even": (u * rows).long(), "skew": (rows ** u - 1).long().clamp(0, rows - 1), "one": torch.where(u < 0.9, rows // 2, (u * rows).long()),
            "outside": torch.where(u < 0.3, -1, ((u * 2 - 0.7) * 1.1 * rows).long())}[kind].to(dev())
     check_grad(qb, rnd((n, d), 5, t), ids if n % 2 else ids.int(), rows, to)
+
+
+@pytest.mark.parametrize("n", [50, 3000, 9000, 140_000])
+def test_gradient_of_rows_that_are_not_finite(qb, n):
+    """Infinities and NaN stay with their ids; those of positions without a row of the table go nowhere."""
+    rows, d = 200, 40
+    ids = torch.randint(10, rows, (n,), generator=torch.Generator().manual_seed(n)).to(dev())
+    g = rnd((n, d), 1)
+    at = torch.tensor([1, 2, 5, 7, 11, 13, 17, 19], device=dev())
+    ids[at] = torch.tensor([0, 1, 2, 2, -1, rows, 2 ** 33, 3], device=dev())
+    g[at[0]] = math.inf
+    g[at[1], 3] = math.nan
+    g[at[2]], g[at[3]] = math.inf, -math.inf
+    g[at[4]], g[at[5]], g[at[6]] = math.nan, math.inf, -math.inf
+    g[at[7]] = -math.inf
+    got = qb.vec_lookup_grad(g, ids, rows, scale=2.0)
+    assert bool((got[0] == math.inf).all()) and bool(got[2].isnan().all()) and bool((got[3] == -math.inf).all())
+    assert bool(got[1, 3].isnan()) and bool(got[1, :3].isfinite().all()) and bool(got[1, 4:].isfinite().all())
+    assert bool((got[4:10] == 0).all()) and bool(got[10:].isfinite().all())
 
 
 def test_time_of_the_gradient_grows_with_the_ids(qb):
