@@ -100,9 +100,9 @@ int vec_quantize_blocks(const void *x, int64_t ld_x, int type, int64_t n, int64_
  * c[i][j] = sum over k of (a[i][k] * a_scales[i][k / 128]) * (b[j][k] * b_scales[j][k / 128])
  *   a [dev][m][k], b [dev][n][k] of type E4M3 or E5M2 (each its own); both scales of scale_type E8M0 or F32
  *   c [dev][m][n] of c_type F32, BF16 or F16
- * Products are exact and their sums are in float32.
- * E8M0 scales are applied to the values (what is below 2^-126 may then count as zero), F32 scales to each block's sum.  k == 0 gives zeros.  m, n, k < 2^31, and
- * with m > 32 less than 2^24 tiles of 128 x 128 of c.
+ * Products are exact and their sums are in float32.  E8M0 scales are applied to the values (what is below 2^-126 may then count as zero); F32
+ * scales to each block's sum, by the product of the two in float32 (2^-126 to 2^128: beyond it the sum loses bits, or is 0, infinite or NaN).
+ * k == 0 gives zeros.  m, n, k < 2^31, and with m > 32 less than 2^24 tiles of 128 x 128 of c.
  *   workspace >= vec_matmul_blocks_workspace_bytes(m, n, k) (may be 0), 256-byte aligned, any content
  */
 size_t vec_matmul_blocks_workspace_bytes(int64_t m, int64_t n, int64_t k);

