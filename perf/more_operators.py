@@ -142,7 +142,7 @@ def prepare(case, seed):
         return state
     n, din, dout, r, count = (case[k] for k in ("n", "din", "dout", "r", "adapters"))
     state.update(index=_ids(case, seed), x=_values(n, din, seed, 10, t),
-                 a=_values(count * r, din, seed, 30, t, din ** -0.5).view(count, r, din), b=_values(count * dout, r, seed, 40, t, 0.5).view(count, dout, r),
+                 a=_values(count * r, din, seed, 30, t, din ** -0.5).view(count, r, din), b=_values(count * r, dout, seed, 40, t, 0.5).view(count, r, dout),
                  scales=torch.exp2(torch.randint(-2, 3, (count,), generator=_gen(seed, 4), device=_dev()).float()) * 0.7)
     if path == "adapter":
         if case["base"]:
@@ -215,10 +215,10 @@ def _plain_adapter(state):
     if n <= count:  # every row its own weights
         of = state["index"].long().clamp(min=0)
         t = (state["a"][of].float() @ x.unsqueeze(2)).squeeze(2) * s
-        y = (state["b"][of].float() @ t.unsqueeze(2)).squeeze(2)
+        y = (t.unsqueeze(1) @ state["b"][of].float()).squeeze(1)
     else:  # all adapters' products, of which a row keeps its own
         t = torch.where(_of_adapters(state).unsqueeze(2), (x @ state["a"].float().view(count * r, -1).t()).view(n, count, r), 0.0) * s.unsqueeze(2)
-        y = t.view(n, count * r) @ state["b"].float().transpose(1, 2).reshape(count * r, dout)
+        y = t.view(n, count * r) @ state["b"].float().view(count * r, dout)
         t = t.sum(dim=1)
     if state["base"]:
         y = y + state["y0"].float()
@@ -230,7 +230,7 @@ def _plain_adapter_grad(state):
     n, r, count, dout = state["n"], state["r"], state["adapters"], state["dout"]
     x, mask, s = _dropped(state)
     dy, its = state["dy"].float(), _of_adapters(state).unsqueeze(2)
-    a, b = state["a"].float().view(count * r, -1), state["b"].float().transpose(1, 2).reshape(count * r, dout)
+    a, b = state["a"].float().view(count * r, -1), state["b"].float().view(count * r, dout)
     u = (torch.where(its, (dy @ b.t()).view(n, count, r), 0.0) * s.unsqueeze(2)).view(n, count * r)
     t = torch.where(its, state["kept"].unsqueeze(1), 0.0).view(n, count * r)
     dx = u @ a
@@ -238,8 +238,8 @@ def _plain_adapter_grad(state):
         dx = torch.where(mask, dx, 0.0)
     if state["base"]:
         dx = dx + state["dx0"].float()
-    da, db = (u.t() @ x).view(count, r, -1), (t.t() @ dy).view(count, r, dout).transpose(1, 2)
-    return {"dx": dx.to(TYPES[state["t"]]), "da": da.to(TYPES[state["to"]]), "db": db.to(TYPES[state["to"]]).contiguous()}
+    da, db = (u.t() @ x).view(count, r, -1), (t.t() @ dy).view(count, r, dout)
+    return {"dx": dx.to(TYPES[state["t"]]), "da": da.to(TYPES[state["to"]]), "db": db.to(TYPES[state["to"]])}
 
 
 # ------------------------------------------------------ the framework's calls --
@@ -300,17 +300,17 @@ def exact(case, seed):
         t = torch.zeros((n, case["r"]), dtype=torch.float64, device=_dev())
         for e, at in rows.items():
             t[at] = (x[at] @ state["a"][e].double().t()) * state["scales"][e].double()
-            y[at] += t[at] @ state["b"][e].double().t()
+            y[at] += t[at] @ state["b"][e].double()
         return {"y": y, "t": t} if case["keep_t"] else {"y": y}
     dx = state["dx0"].double() if case["base"] else torch.zeros_like(x)
     da, db = torch.zeros(state["a"].shape, dtype=torch.float64, device=_dev()), torch.zeros(state["b"].shape, dtype=torch.float64, device=_dev())
     for e, at in rows.items():
         dy = state["dy"][at].double()
-        u = (dy @ state["b"][e].double()) * state["scales"][e].double()
+        u = (dy @ state["b"][e].double().t()) * state["scales"][e].double()
         part = u @ state["a"][e].double()
         dx[at] += part * mask[at] * factor if case["p"] else part
         da[e] = u.t() @ x[at]
-        db[e] = dy.t() @ state["kept"][at].double()
+        db[e] = state["kept"][at].double().t() @ dy
     return {"dx": dx, "da": da, "db": db}
 
 
