@@ -1,8 +1,8 @@
 /*
  * qadc_vec.h -- operators on the vectors that libqadc searches: where they come from (rows of a table, looked up by
- * id, and the gradient that trains it), the root-mean-square norm in front of a projection, and products of 8-bit
+ * id, and the gradient that trains it), the root-mean-square norm in front of a projection, products of 8-bit
  * matrices with a scale for each block of 128 values (the projection itself, its gradients, or the scores of queries
- * against vectors kept in 8 bits).
+ * against vectors kept in 8 bits), low-rank adapters of many requests beside a shared projection, and dropout.
  *
  * The conventions of qadc.h hold: [dev] pointers are the caller's, every call only enqueues work on `stream`, nothing
  * is allocated, 0 or a negative code comes back and pq_last_error() says what was wrong.  Beyond them:
@@ -30,7 +30,10 @@ enum { VEC_F32 = 0, VEC_BF16 = 1, VEC_F16 = 2, VEC_E4M3 = 3, VEC_E5M2 = 4, VEC_E
 
 #define VEC_BLOCK 128         /* consecutive values that share a scale */
 #define VEC_MAX_NORM_DIM 16384 /* columns of vec_norm and vec_norm_grad */
-#define VEC_MAX_ROW_DIM (1 << 24) /* columns of vec_lookup and vec_lookup_grad */
+#define VEC_MAX_ROW_DIM (1 << 24) /* columns of vec_lookup, vec_lookup_grad and vec_dropout */
+#define VEC_MAX_RANK 256          /* of vec_adapter and vec_adapter_grad: ranks, */
+#define VEC_MAX_ADAPTERS 65535    /* adapters, */
+#define VEC_MAX_ADAPTER_DIM (1 << 20) /* columns */
 
 /*
  * out[i] = scale * table[ids[i]].  An id outside 0..rows-1 (a search pads its results with -1) gives a row of zeros.
@@ -110,6 +113,58 @@ int vec_matmul_blocks(const void *a, int64_t ld_a, int a_type, const void *a_sca
                       int64_t ld_b, int b_type, const void *b_scales, int64_t ld_b_scales, int scale_type, int64_t m,
                       int64_t n, int64_t k, void *c, int64_t ld_c, int c_type, void *workspace, size_t workspace_bytes,
                       void *stream);
+
+/*
+ * Dropout: y[i][j] = residual[i][j] + (kept(i, j) ? x[i][j] / (1 - p) : 0), without a residual the second term alone.  The mask is made
+ * from (i, j, seed, step, layer) and never stored: the gradient of x is the same call on the gradient of y (of residual: that gradient itself).
+ *   p      the rate, in units of 2^-16 (the nearest; 0 <= p <= 65535/65536); 1 / (1 - p) is of that rate, in float32
+ *   state  [dev][2], 8-byte aligned: seed, step (its low 32 bits); NULL where p is 0.  Read when the call runs, so that a recorded call takes what is there on each replay
+ *   layer  tells apart the masks that one step needs
+ *   x, residual (or NULL), y [dev][n][d] of one type, F32, BF16 or F16; y may be x or residual (same pointer and ld); n < 2^32, 1 <= d <= VEC_MAX_ROW_DIM
+ * kept(i, j): Philox4x32-10 of key seed and counter (j / 8, i, step, layer) gives four words, words 0 to 3, low half first, are the sixteen-bit numbers of
+ * columns 8 (j / 8) .. + 7, and those of at least 65536 p are kept.  A dropped element counts as 0 whatever it is.
+ */
+int vec_dropout(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, int type, int64_t n, int64_t d, double p,
+                const uint64_t *state, uint32_t layer, void *y, int64_t ld_y, void *stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection.  Row i has adapter e = ids[i]; with x'[i] the row after dropout (vec_dropout with
+ * p, state and layer, without a residual; not stored):
+ *   t[i] = scales[e] * x'[i] a[e]^T                       float32
+ *   y[i] = base[i] + t[i] b[e]
+ * An id outside 0..adapters-1 means no adapter: t[i] = 0, y[i] = base[i], and x[i] is not read.  Adapters without a row are not read.
+ *   x      [dev][n][din], a [dev][adapters][rank][din], b [dev][adapters][rank][dout], all of `type` F32, BF16 or F16; stride_a and stride_b: the
+ *          distance of two adapters in elements, 0 or more
+ *   scales [dev][adapters] float32, or NULL (1)           ids [dev][n], int32 or int64, in any order
+ *   base   [dev][n][dout] or NULL (0), y [dev][n][dout], of y_type: `type` or F32; y may be base (same pointer and ld)
+ *   t      [dev][n][rank] float32 without padding, what the gradient reads, or NULL
+ * Products are of the values of `type` with float32 sums; t is not rounded to fewer bits.  An infinity among x, a, b or t gives an infinity or NaN in
+ * the results that it enters.
+ * n < 2^31, 1 <= din, dout <= VEC_MAX_ADAPTER_DIM, 1 <= rank <= VEC_MAX_RANK, 0 <= adapters <= VEC_MAX_ADAPTERS.
+ *   workspace >= vec_adapter_workspace_bytes(...), 256-byte aligned, any content
+ */
+size_t vec_adapter_workspace_bytes(int64_t n, int din, int dout, int rank, int adapters, int type);
+int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t ld_a, int64_t stride_a, const void *b, int64_t ld_b, int64_t stride_b, int type,
+                int adapters, int rank, const float *scales, const void *ids, int id_bytes, int64_t n, int din, int dout, const void *base,
+                int64_t ld_base, void *y, int64_t ld_y, int y_type, double p, const uint64_t *state, uint32_t layer, float *t, void *workspace,
+                size_t workspace_bytes, void *stream);
+
+/*
+ * The gradient of vec_adapter, from dy, the gradient of y (which is that of base too), and t, what the forward call gave.  With
+ * u[i] = scales[e] / (1 - p) * dy[i] b[e]^T in float32 and x'[i] = x[i] where kept, else 0:
+ *   dx[i] = dx_base[i] + (u[i] a[e] where kept)           rows without an adapter: dx_base[i]
+ *   da[e] = sum over the rows of e of u[i]^T x'[i]        db[e] = sum over the rows of e of t[i]^T dy[i]
+ * da and db of all adapters are written, those without a row with zeros; accumulate: the sums are added to them, and adapters without a row left alone.
+ *   dy [dev][n][dout], x, dx_base and dx [dev][n][din] of `type`; dx may be NULL (then dx_base too), dx_base NULL (0) or dx itself (same pointer and ld)
+ *   da [dev][adapters][rank][din], db [dev][adapters][rank][dout], of grad_type: `type` or F32; the adapters' must not overlap
+ * p, state and layer as in the forward call, with the same state's contents.
+ */
+size_t vec_adapter_grad_workspace_bytes(int64_t n, int din, int dout, int rank, int adapters, int type);
+int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *t, const void *a, int64_t ld_a, int64_t stride_a,
+                     const void *b, int64_t ld_b, int64_t stride_b, int type, int adapters, int rank, const float *scales, const void *ids,
+                     int id_bytes, int64_t n, int din, int dout, const void *dx_base, int64_t ld_dx_base, void *dx, int64_t ld_dx, double p,
+                     const uint64_t *state, uint32_t layer, int accumulate, void *da, int64_t ld_da, int64_t stride_da, void *db, int64_t ld_db,
+                     int64_t stride_db, int grad_type, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,7 @@ EXPORTS = [
 VEC_EXPORTS = [
     "vec_lookup", "vec_lookup_grad_workspace_bytes", "vec_lookup_grad", "vec_norm", "vec_norm_grad_workspace_bytes",
     "vec_norm_grad", "vec_quantize_blocks", "vec_matmul_blocks_workspace_bytes", "vec_matmul_blocks",
+    "vec_dropout", "vec_adapter_workspace_bytes", "vec_adapter", "vec_adapter_grad_workspace_bytes", "vec_adapter_grad",
 ]
 PQ_KEY_BOUND_UNKNOWN = 0xFFFFFFFF
 (PQ_OPT_SCAN_BLOCKS, PQ_OPT_PILOT_CODES, PQ_OPT_PILOT_CODES_SINGLE, PQ_OPT_PILOT_BLOCKS, PQ_OPT_IVF_THREADS,
@@ -128,6 +129,12 @@ def load() -> ctypes.CDLL:
     lib.vec_quantize_blocks.argtypes = [vp, i64, i32, i64, i64, i32, vp, i64, i32, vp, i64, i32, vp]
     lib.vec_matmul_blocks_workspace_bytes.argtypes = [i64, i64, i64]
     lib.vec_matmul_blocks.argtypes = [vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, i32, i64, i64, i64, vp, i64, i32, vp, sz, vp]
+    f64, u32 = ctypes.c_double, ctypes.c_uint32
+    lib.vec_dropout.argtypes = [vp, i64, vp, i64, i32, i64, i64, f64, vp, u32, vp, i64, vp]
+    lib.vec_adapter_workspace_bytes.argtypes = lib.vec_adapter_grad_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    factors = [vp, i64, i64, vp, i64, i64, i32, i32, i32, vp, vp, i32, i64, i32, i32]
+    lib.vec_adapter.argtypes = [vp, i64, *factors, vp, i64, vp, i64, i32, f64, vp, u32, vp, vp, sz, vp]
+    lib.vec_adapter_grad.argtypes = [vp, i64, vp, i64, vp, *factors, vp, i64, vp, i64, f64, vp, u32, i32, vp, i64, i64, vp, i64, i64, i32, vp, sz, vp]
     for name in VEC_EXPORTS:
         getattr(lib, name).restype = sz if name.endswith("_bytes") else i32
     _lib = lib
@@ -554,6 +561,26 @@ class _Call:
             return t.data_ptr(), nbytes, t
         return self.vector("workspace", t), t.numel() * t.element_size(), t
 
+    def matrices(self, what: str, t: torch.Tensor, count: int, n: int, d: int, dtype):
+        """Address of [count, n, d], the distances of its rows and of its matrices, checked."""
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 3 or shape[0] != count or shape[1] != n or shape[2] != d or t.dtype != dtype or t.get_device() != self.index:
+            _refuse(self.name, f"{what}: {t.dtype} of shape {tuple(shape)} on {t.device}, not {dtype} of {(count, n, d)} on {self.device}")
+        ld = stride[1] if n > 1 else d
+        if ld < d or (stride[2] != 1 and d > 1):
+            _refuse(self.name, f"{what}'s rows of {d} are {ld} apart, the values of a row {stride[2]}")
+        return t.data_ptr(), ld, stride[0] if count > 1 else 0
+
+    def mask(self, p: float, state: Optional[torch.Tensor], layer: int):
+        """Dropout's arguments: the rate, the address of seed and step, the layer."""
+        if not 0 <= layer <= 0xFFFFFFFF:
+            _refuse(self.name, f"layer={layer}")
+        if p == 0 or state is None:
+            return p, None, layer
+        if state.numel() != 2 or (state.dtype != torch.int64 and state.dtype != torch.uint64):
+            _refuse(self.name, f"state of {state.dtype}, shape {tuple(state.shape)}: seed and step, int64")
+        return p, self.vector("state", state), layer
+
     def type(self, what: str, dtype) -> int:
         t = _VEC_TYPE.get(dtype)
         if t is None:
@@ -757,3 +784,111 @@ def vec_matmul_blocks(a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, 
     call.launch(lib.vec_matmul_blocks, ap, lda, call.type("a", a.dtype), asp, ldas, bp, ldb, call.type("b", b.dtype), bsp, ldbs,
                 call.type("scales", st), m, n, k, cp, ldc, call.type("out", to), wptr, wbytes)
     return out
+
+
+def vec_dropout(x: torch.Tensor, p: float, state: Optional[torch.Tensor] = None, layer: int = 0, residual: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """residual + x / (1 - p) where kept.  state: int64 [seed, step] on the GPU, from which, with `layer`, the mask is made; the gradient
+    of x is the same call on the result's gradient, without a residual.  `out` may be x or residual."""
+    call = _Call("vec_dropout", x, stream)
+    n, d, xp, ldx = call.first_rows("x", x)
+    rp, ldr = call.rows("residual", residual, n, d, x.dtype) if residual is not None else (None, 0)
+    p, sp, layer = call.mask(p, state, layer)
+    if out is None:
+        out = call.empty(x.dtype, n, d)
+        yp, ldy = out.data_ptr(), d
+    else:
+        yp, ldy = call.rows("out", out, n, d, x.dtype)
+    call.launch((_lib or load()).vec_dropout, xp, ldx, rp, ldr, call.type("x", x.dtype), n, d, p, sp, layer, yp, ldy)
+    return out
+
+
+def _adapters(call: _Call, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, scales: Optional[torch.Tensor]):
+    """What both calls of the adapters take: rows, columns, ranks, adapters; x's address and distance; and the C arguments from a to dout."""
+    n, din, xp, ldx = call.first_rows("x", x)
+    if a.dim() != 3 or b.dim() != 3:
+        _refuse(call.name, f"a and b of shapes {tuple(a.shape)} and {tuple(b.shape)}, not [adapters, rank, columns]")
+    count, rank, dout = a.shape[0], a.shape[1], b.shape[2]
+    for v in (din, dout, rank, count):
+        call.columns(v)
+    ap, lda, sta = call.matrices("a", a, count, rank, din, x.dtype)
+    bp, ldb, stb = call.matrices("b", b, count, rank, dout, x.dtype)
+    idp, id_bytes = call.ids(ids)
+    if ids.numel() != n:
+        _refuse(call.name, f"{ids.numel()} ids for {n} rows")
+    sp = call.vector("scales", scales, count, torch.float32) if scales is not None else None
+    t = call.type("x", x.dtype)
+    return n, din, dout, rank, count, t, xp, ldx, (ap, lda, sta, bp, ldb, stb, t, count, rank, sp, idp, id_bytes, n, din, dout)
+
+
+def vec_adapter_workspace_bytes(n: int, din: int, dout: int, rank: int, adapters: int, dtype: torch.dtype) -> int:
+    return int(load().vec_adapter_workspace_bytes(n, din, dout, rank, adapters, _VEC_TYPE[dtype]))
+
+
+def vec_adapter(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, scales: Optional[torch.Tensor] = None,
+                base: Optional[torch.Tensor] = None, p: float = 0.0, state: Optional[torch.Tensor] = None, layer: int = 0,
+                dtype: Optional[torch.dtype] = None, want_t: bool = False, out=None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Low-rank adapters of many requests: y = base + t b[e] with t = scales[e] * dropout(x) a[e]^T and e the row's id, y = base where
+    that is outside.  a [adapters, rank, din], b [adapters, rank, dout]; p, state and layer as in vec_dropout.  Returns (y, t), t (float32,
+    for the gradient) where wanted, else None.  `out`: the same two, to be written (y may be base; its type x's or float32)."""
+    call = _Call("vec_adapter", x, stream)
+    n, din, dout, rank, count, tx, xp, ldx, args = _adapters(call, x, a, b, ids, scales)
+    p, statep, layer = call.mask(p, state, layer)
+    if out is None:
+        to = dtype or (base.dtype if base is not None else x.dtype)
+        y = call.empty(to, n, dout)
+        yp, ldy = y.data_ptr(), dout
+        t = call.empty(torch.float32, n, rank) if want_t else None
+        tp = t.data_ptr() if want_t else None
+    else:
+        y, t = out
+        to = call.out_type(y, dtype, None)
+        yp, ldy = call.rows("y", y, n, dout, to)
+        tp = None
+        if t is not None:
+            tp, ldt = call.rows("t", t, n, rank, torch.float32)
+            if ldt != rank:
+                _refuse(call.name, f"t's rows of {rank} are {ldt} apart")
+    bp, ldb = call.rows("base", base, n, dout, to) if base is not None else (None, 0)
+    lib = _lib or load()
+    wptr, wbytes, keep = call.workspace(workspace, _vec_bytes("vec_adapter_workspace_bytes", n, din, dout, rank, count, tx))
+    call.launch(lib.vec_adapter, xp, ldx, *args, bp, ldb, yp, ldy, call.type("y", to), p, statep, layer, tp, wptr, wbytes)
+    return y, t
+
+
+def vec_adapter_grad_workspace_bytes(n: int, din: int, dout: int, rank: int, adapters: int, dtype: torch.dtype) -> int:
+    return int(load().vec_adapter_grad_workspace_bytes(n, din, dout, rank, adapters, _VEC_TYPE[dtype]))
+
+
+def vec_adapter_grad(dy: torch.Tensor, x: torch.Tensor, t: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor,
+                     scales: Optional[torch.Tensor] = None, dx_base: Optional[torch.Tensor] = None, p: float = 0.0,
+                     state: Optional[torch.Tensor] = None, layer: int = 0, dtype: Optional[torch.dtype] = None, want_dx: bool = True,
+                     accumulate: bool = False, out=None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(dx, da, db) of vec_adapter: t is its second result, dx_base the gradient that reaches x past the adapters; da and db are float32
+    unless `dtype` says x's type, and zeros for adapters without a row.  `out`: the same three, to be written (dx may be None or dx_base); with
+    `accumulate` the sums are added to its da and db."""
+    call = _Call("vec_adapter_grad", x, stream)
+    n, din, dout, rank, count, tx, xp, ldx, args = _adapters(call, x, a, b, ids, scales)
+    dyp, lddy = call.rows("dy", dy, n, dout, x.dtype)
+    tp, ldt = call.rows("t", t, n, rank, torch.float32)
+    if ldt != rank and n > 1:
+        _refuse(call.name, f"t's rows of {rank} are {ldt} apart")
+    p, statep, layer = call.mask(p, state, layer)
+    if accumulate and out is None:
+        _refuse(call.name, "accumulate needs an out to add to")
+    if out is None:
+        to = dtype or torch.float32
+        dx = call.empty(x.dtype, n, din) if want_dx else None
+        da, db = call.empty(to, count, rank, din), call.empty(to, count, rank, dout)
+    else:
+        dx, da, db = out
+        to = call.out_type(da, dtype, None)
+    dxp, lddx = call.rows("dx", dx, n, din, x.dtype) if dx is not None else (None, 0)
+    ep, lde = call.rows("dx_base", dx_base, n, din, x.dtype) if dx_base is not None else (None, 0)
+    dap, ldda, stda = call.matrices("da", da, count, rank, din, to)
+    dbp, lddb, stdb = call.matrices("db", db, count, rank, dout, to)
+    lib = _lib or load()
+    wptr, wbytes, keep = call.workspace(workspace, _vec_bytes("vec_adapter_grad_workspace_bytes", n, din, dout, rank, count, tx))
+    call.launch(lib.vec_adapter_grad, dyp, lddy, xp, ldx, tp, *args, ep, lde, dxp, lddx, p, statep, layer, int(accumulate), dap, ldda, stda, dbp, lddb, stdb,
+                call.type("da", to), wptr, wbytes)
+    return dx, da, db

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqadc.so")
 SOURCES = ["index.hip", "tables.hip", "quantize.hip", "scan.hip", "scan_mx.hip", "scan_mx_wide.hip", "ivf.hip", "coarse.hip", "coarse_half.hip", "encode.hip",
            "vec_lookup.hip", "vec_norm.hip", "vec_quantize.hip", "vec_matmul.hip", "vec_matmul_e4m3_e4m3.hip", "vec_matmul_e4m3_e5m2.hip",
-           "vec_matmul_e5m2_e4m3.hip", "vec_matmul_e5m2_e5m2.hip"]
+           "vec_matmul_e5m2_e4m3.hip", "vec_matmul_e5m2_e5m2.hip",
+           "vec_dropout.hip", "vec_adapter.hip", "vec_adapter_f32.hip", "vec_adapter_bf16.hip", "vec_adapter_f16.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -1,0 +1,183 @@
+// vec_adapter and vec_adapter_grad: checks, plans and launches (kernels: vec_adapter.h).
+#include "vec_adapter_launch.h"
+
+// vec_lookup.hip: the stable sort of positions by id; ids outside 0..rows-1 come last, with key `rows`
+size_t qadc_vec_sort_bytes(int64_t n, int64_t rows);
+void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char *ws, const uint32_t **keys, const uint32_t **pos, hipStream_t s);
+
+#define AD_MOST_UNSORTED 512  // rows of several adapters up to which each is a tile of its own
+#define AD_MAX_SLABS 16
+
+struct AdPlan {
+    bool sorted;
+    int tp;                    // positions of a tile
+    int rp;                    // ranks of a row of partial sums
+    int slabs, per;            // of the contraction over columns
+    int len_a, len_b;          // positions of a piece of the sums over rows
+    int dpad_a, dpad_b;
+    size_t part, part_a, part_b, total;  // bytes from the workspace's start
+};
+
+static int ad_len(int64_t n, int d, int rank, int type) {
+    const int64_t across = (int64_t)((d + 63) / 64 + 7) / 8 * (type == VEC_F32 ? 2 : 1) * ((rank + 63) / 64);
+    int len = 1024;
+    while (len > AD_STAGE && (n + len - 1) / len * across < 512) len /= 2;
+    return len;
+}
+
+static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int type, bool grad) {
+    AdPlan p = {};
+    p.sorted = grad || (adapters > 1 && n > AD_MOST_UNSORTED);
+    p.tp = p.sorted || adapters <= 1 ? (n <= 1024 ? 16 : (rank <= 32 ? 64 : 32)) : 1;
+    p.rp = (rank + 15) & ~15;
+    const int d = grad ? dout : din;
+    const int64_t tiles = (n + p.tp - 1) / p.tp, want = tiles >= 512 ? 1 : (512 + tiles - 1) / tiles;
+    const int64_t slabs = want < AD_MAX_SLABS ? want : AD_MAX_SLABS, per = ((d + slabs - 1) / slabs + 255) / 256 * 256;
+    p.per = (int)per;
+    p.slabs = (int)((d + per - 1) / per);
+    size_t at = p.sorted ? qadc_vec_sort_bytes(n, adapters) : 0;
+    auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
+    p.part = take((size_t)p.slabs * n * p.rp * 4);
+    if (grad) {
+        p.len_a = ad_len(n, din, rank, type);
+        p.len_b = ad_len(n, dout, rank, type);
+        p.dpad_a = (din + 7) & ~7;
+        p.dpad_b = (dout + 7) & ~7;
+        p.part_a = take((size_t)((n + p.len_a - 1) / p.len_a) * 2 * rank * p.dpad_a * 4);
+        p.part_b = take((size_t)((n + p.len_b - 1) / p.len_b) * 2 * rank * p.dpad_b * 4);
+    }
+    p.total = at;
+    return p;
+}
+
+static bool ad_sizes(int64_t n, int din, int dout, int rank, int adapters) {
+    return n >= 0 && n <= 0x7fffffffLL && din >= 1 && din <= VEC_MAX_ADAPTER_DIM && dout >= 1 && dout <= VEC_MAX_ADAPTER_DIM && rank >= 1 &&
+           rank <= VEC_MAX_RANK && adapters >= 0 && adapters <= VEC_MAX_ADAPTERS;
+}
+
+extern "C" size_t vec_adapter_workspace_bytes(int64_t n, int din, int dout, int rank, int adapters, int type) {
+    return n > 0 && adapters > 0 && ad_sizes(n, din, dout, rank, adapters) ? ad_plan(n, din, dout, rank, adapters, type, false).total : 0;
+}
+extern "C" size_t vec_adapter_grad_workspace_bytes(int64_t n, int din, int dout, int rank, int adapters, int type) {
+    return n > 0 && adapters > 0 && ad_sizes(n, din, dout, rank, adapters) ? ad_plan(n, din, dout, rank, adapters, type, true).total : 0;
+}
+
+static int ad_column_blocks(int64_t n, int tp, int d, int type) {
+    const int64_t tiles = (n + tp - 1) / tp, most = type == VEC_F32 ? (d + 255) / 256 : (d + 511) / 512;
+    const int64_t want = tiles >= 2048 ? 1 : (2048 + tiles - 1) / tiles;
+    return (int)(want < most ? want : most);
+}
+
+#define AD_CHECK(name)                                                                                                                              \
+    uint32_t threshold;                                                                                                                             \
+    float factor;                                                                                                                                   \
+    VEC_REQUIRE(ad_sizes(n, din, dout, rank, adapters), name ": n=%lld, din=%d, dout=%d (1..%d), rank=%d (1..%d), adapters=%d (0..%d)", (long long)n, \
+                din, dout, VEC_MAX_ADAPTER_DIM, rank, VEC_MAX_RANK, adapters, VEC_MAX_ADAPTERS);                                                    \
+    VEC_REQUIRE(vec_rate(p, &threshold, &factor), name ": p=%g is not in 0..65535/65536", p);                                                       \
+    VEC_REQUIRE(vec_is_wide(type), name ": types: %d is not F32, BF16 or F16", type);                                                               \
+    VEC_REQUIRE(id_bytes == 4 || id_bytes == 8, name ": ids of %d bytes", id_bytes);                                                                \
+    VEC_REQUIRE(threshold == 0 || (state && ((uintptr_t)state & 7u) == 0), name ": state null or misaligned");                                      \
+    VEC_REQUIRE(ld_a >= din && ld_b >= dout && stride_a >= 0 && stride_b >= 0, name ": a distance of rows is below their length, or one of adapters below 0")
+
+#define AD_WORKSPACE(name, need)                                                                            \
+    do {                                                                                                    \
+        VEC_REQUIRE(workspace && ((uintptr_t)workspace & 255u) == 0, name ": workspace null or not 256-byte aligned"); \
+        if (workspace_bytes < (need)) {                                                                     \
+            qadc_set_error(name ": workspace of %zu bytes, %zu needed", workspace_bytes, (size_t)(need));   \
+            return PQ_ENOMEM;                                                                               \
+        }                                                                                                   \
+    } while (0)
+
+extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t ld_a, int64_t stride_a, const void *b, int64_t ld_b, int64_t stride_b, int type,
+                           int adapters, int rank, const float *scales, const void *ids, int id_bytes, int64_t n, int din, int dout, const void *base,
+                           int64_t ld_base, void *y, int64_t ld_y, int y_type, double p, const uint64_t *state, uint32_t layer, float *t, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    AD_CHECK("vec_adapter");
+    VEC_REQUIRE(y_type == type || y_type == VEC_F32, "vec_adapter: types %d and %d (y)", type, y_type);
+    VEC_REQUIRE(ld_x >= din && (!base || ld_base >= dout) && ld_y >= dout, "vec_adapter: a distance of rows is below their length");
+    VEC_REQUIRE(base != y || !base || ld_base == ld_y, "vec_adapter: y in place of base with other distances of rows");
+    if (n == 0) return PQ_OK;
+    VEC_REQUIRE(x && y && ids && (adapters == 0 || (a && b)), "vec_adapter: null pointer");
+    VEC_REQUIRE(vec_aligned(x, type) && vec_aligned(a, type) && vec_aligned(b, type) && vec_aligned(base, y_type) && vec_aligned(y, y_type) &&
+                    vec_aligned(scales, VEC_F32) && vec_aligned(t, VEC_F32) && ((uintptr_t)ids & (uintptr_t)(id_bytes - 1)) == 0,
+                "vec_adapter: misaligned pointer");
+    hipStream_t s = (hipStream_t)stream;
+    const AdPlan plan = ad_plan(n, din, dout, rank, adapters, type, false);
+    AdRows rows = {ids, id_bytes, plan.tp, n, adapters, nullptr, nullptr};
+    char *ws = (char *)workspace;
+    float *part = nullptr;
+    const VecMask mask = {state, layer, threshold}, none = {nullptr, 0, 0};
+    if (adapters > 0) {
+        AD_WORKSPACE("vec_adapter", plan.total);
+        part = (float *)(ws + plan.part);
+        if (plan.sorted) qadc_vec_sort(ids, id_bytes, n, adapters, ws, &rows.keys, &rows.pos, s);
+        const AdMatrix m = {a, ld_a, stride_a, rank, din};
+        VEC_TYPED(type, T, AdLaunch<T>::down(rows, x, ld_x, m, mask, part, n * plan.rp, plan.rp, plan.slabs, plan.per, s));
+    }
+    const AdFactor f = {part, plan.rp, n * plan.rp, plan.slabs, scales, factor};
+    const AdMatrix m = {b, ld_b, stride_b, rank, dout};
+    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, t, ad_column_blocks(n, plan.tp, dout, type), s));
+    QADC_LAUNCH_CHECK("vec_adapter's kernels");
+    return PQ_OK;
+}
+
+extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *t, const void *a, int64_t ld_a, int64_t stride_a,
+                                const void *b, int64_t ld_b, int64_t stride_b, int type, int adapters, int rank, const float *scales, const void *ids,
+                                int id_bytes, int64_t n, int din, int dout, const void *dx_base, int64_t ld_dx_base, void *dx, int64_t ld_dx, double p,
+                                const uint64_t *state, uint32_t layer, int accumulate, void *da, int64_t ld_da, int64_t stride_da, void *db, int64_t ld_db,
+                                int64_t stride_db, int grad_type, void *workspace, size_t workspace_bytes, void *stream) {
+    AD_CHECK("vec_adapter_grad");
+    VEC_REQUIRE(grad_type == type || grad_type == VEC_F32, "vec_adapter_grad: types %d and %d (da, db)", type, grad_type);
+    VEC_REQUIRE(dx || !dx_base, "vec_adapter_grad: dx_base without dx");
+    VEC_REQUIRE(ld_x >= din && ld_dy >= dout && (!dx || ld_dx >= din) && (!dx_base || ld_dx_base >= din) && ld_da >= din && ld_db >= dout,
+                "vec_adapter_grad: a distance of rows is below their length");
+    VEC_REQUIRE(adapters <= 1 || (stride_da >= (int64_t)(rank - 1) * ld_da + din && stride_db >= (int64_t)(rank - 1) * ld_db + dout),
+                "vec_adapter_grad: the adapters' gradients overlap");
+    VEC_REQUIRE(!dx || dx_base != dx || ld_dx_base == ld_dx, "vec_adapter_grad: dx in place of dx_base with other distances of rows");
+    VEC_REQUIRE((adapters == 0 || (da && db)) && (n == 0 || (ids && (adapters == 0 || (dy && x && t && a && b)))), "vec_adapter_grad: null pointer");
+    VEC_REQUIRE(vec_aligned(dy, type) && vec_aligned(x, type) && vec_aligned(t, VEC_F32) && vec_aligned(a, type) && vec_aligned(b, type) &&
+                    vec_aligned(scales, VEC_F32) && vec_aligned(dx_base, type) && vec_aligned(dx, type) && vec_aligned(da, grad_type) && vec_aligned(db, grad_type) &&
+                    ((uintptr_t)ids & (uintptr_t)(id_bytes - 1)) == 0, "vec_adapter_grad: misaligned pointer");
+    if (n == 0 && (adapters == 0 || accumulate)) return PQ_OK;
+    hipStream_t s = (hipStream_t)stream;
+    const VecMask mask = {state, layer, threshold}, none = {nullptr, 0, 0};
+    const bool narrow = grad_type == type;
+    AdRows rows = {ids, id_bytes, 1, n, adapters, nullptr, nullptr};
+    AdPlan plan = {};
+    plan.len_a = plan.len_b = AD_STAGE;
+    plan.dpad_a = (din + 7) & ~7;
+    plan.dpad_b = (dout + 7) & ~7;
+    AdOuter oa = {da, ld_da, stride_da, nullptr, plan.dpad_a, accumulate}, ob = {db, ld_db, stride_db, nullptr, plan.dpad_b, accumulate};
+    if (n > 0) {
+        plan = ad_plan(n, din, dout, rank, adapters, type, true);
+        rows.tp = plan.tp;
+        char *ws = (char *)workspace;
+        const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
+        AdFactor u = {nullptr, plan.rp, n * plan.rp, plan.slabs, scales, factor};
+        if (adapters > 0) {
+            AD_WORKSPACE("vec_adapter_grad", plan.total);
+            float *part = (float *)(ws + plan.part);
+            u.p = part;
+            oa.part = (float *)(ws + plan.part_a);
+            ob.part = (float *)(ws + plan.part_b);
+            qadc_vec_sort(ids, id_bytes, n, adapters, ws, &rows.keys, &rows.pos, s);
+            const AdFactor kept = {t, rank, 0, 1, nullptr, 1.0f};
+            VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, none, part, n * plan.rp, plan.rp, plan.slabs, plan.per, s);
+                      AdLaunch<T>::outer(rows, plan.len_b, kept, rank, dy, ld_dy, dout, none, ob, narrow, s);
+                      AdLaunch<T>::outer(rows, plan.len_a, u, rank, x, ld_x, din, mask, oa, narrow, s));
+        }
+        if (dx)
+            VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, mask, nullptr, ad_column_blocks(n, plan.tp, din, type), s));
+    }
+    if (adapters > 0) {
+        auto join = [&](const AdOuter &o, int len, int d) {
+            const int64_t pieces = (int64_t)rank * (o.dpad / 8);
+            const dim3 grid((unsigned)(pieces <= 256 * 64 ? (pieces + 255) / 256 : 64), (unsigned)adapters);
+            VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, len, rank, d, o));
+        };
+        join(oa, plan.len_a, din);
+        join(ob, plan.len_b, dout);
+    }
+    QADC_LAUNCH_CHECK("vec_adapter_grad's kernels");
+    return PQ_OK;
+}

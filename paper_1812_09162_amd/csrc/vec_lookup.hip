@@ -116,23 +116,18 @@ struct GradPlan {
     size_t key0, key1, pos0, pos1, counts, sums, begins, part, total;
 };
 
-static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
-    GradPlan p = {};
-    p.few = n <= (rows < (1 << GRAD_BITS) ? GRAD_FEW / 2 : GRAD_FEW);
-    if (p.few) return p;
+// the sort's part of it
+static void grad_plan_sort(GradPlan &p, int64_t n, int64_t rows) {
     int bits = 1;
     while (((int64_t)1 << bits) <= rows) ++bits;  // ids 0..rows, `rows` standing for those that take no part
     p.passes = (bits + GRAD_BITS - 1) / GRAD_BITS;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tiles = (int)((n + GRAD_TILE - 1) / GRAD_TILE);
-    p.len = n <= 32768 ? GRAD_CHUNK / 4 : (n <= 131072 ? GRAD_CHUNK / 2 : GRAD_CHUNK);
-    p.chunks = (int)((n + p.len - 1) / p.len);
     if (p.tiles > GRAD_TILES_ALONE) {
         p.seg = 1;
         while ((int64_t)p.seg * p.seg < p.tiles) p.seg *= 2;
         p.segs = (p.tiles + p.seg - 1) / p.seg;
     }
-    p.dpad = (d + 7) & ~7;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
     p.key0 = take((size_t)n * 4);
@@ -141,6 +136,19 @@ static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
     p.pos1 = take((size_t)n * 4);
     p.counts = take(((size_t)p.tiles << p.bits) * 4);
     p.sums = p.segs > 0 ? take(((size_t)(p.segs + 1) << p.bits) * 4) : 0;
+    p.total = at;
+}
+
+static GradPlan grad_plan(int64_t n, int64_t rows, int d) {
+    GradPlan p = {};
+    p.few = n <= (rows < (1 << GRAD_BITS) ? GRAD_FEW / 2 : GRAD_FEW);
+    if (p.few) return p;
+    grad_plan_sort(p, n, rows);
+    p.len = n <= 32768 ? GRAD_CHUNK / 4 : (n <= 131072 ? GRAD_CHUNK / 2 : GRAD_CHUNK);
+    p.chunks = (int)((n + p.len - 1) / p.len);
+    p.dpad = (d + 7) & ~7;
+    size_t at = p.total;
+    auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
     p.begins = take((size_t)rows * 4);
     p.part = take((size_t)p.chunks * 2 * p.dpad * 4);
     p.total = at;
@@ -535,6 +543,55 @@ k_vec_grad_join(const uint32_t *__restrict__ keys, int64_t n, const uint32_t *__
     }
 }
 
+struct GradSorted {
+    const uint32_t *keys, *pos;
+};
+// The launches of the sort; share(pass, blocks) says what a pass's second kernel clears besides, and its grid.
+template <class SHARE>
+static GradSorted grad_sort(const GradPlan &p, const void *ids, int id_bytes, int64_t n, int64_t rows, char *ws, int table_type, SHARE share, hipStream_t s) {
+    uint32_t *key[2] = {(uint32_t *)(ws + p.key0), (uint32_t *)(ws + p.key1)}, *pos[2] = {(uint32_t *)(ws + p.pos0), (uint32_t *)(ws + p.pos1)};
+    uint32_t *counts = (uint32_t *)(ws + p.counts);
+    uint32_t *sums = (uint32_t *)(ws + p.sums), *totals = sums + ((size_t)p.segs << p.bits);
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const uint32_t *ki = pass ? key[(pass - 1) & 1] : nullptr, *pi = pass ? pos[(pass - 1) & 1] : nullptr;
+        const int shift = pass * p.bits;
+        if (id_bytes == 4)
+            hipLaunchKernelGGL((k_vec_grad_count<int32_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int32_t *)ids, ki, n, rows, shift, p.bits, counts);
+        else
+            hipLaunchKernelGGL((k_vec_grad_count<int64_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int64_t *)ids, ki, n, rows, shift, p.bits, counts);
+        if (p.segs > 0) {
+            const dim3 threads(p.bits < 6 ? 64 : 1u << p.bits);
+            hipLaunchKernelGGL(k_vec_grad_running, dim3((unsigned)p.segs), threads, 0, s, counts, p.tiles, p.seg, p.bits, sums);
+            hipLaunchKernelGGL(k_vec_grad_running, dim3(1), threads, 0, s, sums, p.segs, p.segs, p.bits, totals);
+        }
+        GradClear z;
+        const dim3 grid = share(pass, (unsigned)p.tiles, z);
+#define GO(ID, TT)                                                                                                         \
+    hipLaunchKernelGGL((k_vec_grad_place<ID, TT>), grid, dim3(1024), (size_t)64 << p.bits, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
+                       counts, p.tiles, p.seg, sums, totals, key[pass & 1], pos[pass & 1], z)
+        VEC_TYPED(table_type, TT, if (id_bytes == 4) GO(int32_t, TT); else GO(int64_t, TT));
+#undef GO
+    }
+    return {key[(p.passes - 1) & 1], pos[(p.passes - 1) & 1]};
+}
+
+size_t qadc_vec_sort_bytes(int64_t n, int64_t rows) {
+    GradPlan p = {};
+    grad_plan_sort(p, n, rows);
+    return p.total;
+}
+void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char *ws, const uint32_t **keys, const uint32_t **pos, hipStream_t s) {
+    GradPlan p = {};
+    grad_plan_sort(p, n, rows);
+    auto nothing = [](int, unsigned own, GradClear &z) {
+        z = {nullptr, 0, 0, 1, 1, 1, (int)own};
+        return dim3(own);
+    };
+    const GradSorted sorted = grad_sort(p, ids, id_bytes, n, rows, ws, VEC_F32, nothing, s);
+    *keys = sorted.keys;
+    *pos = sorted.pos;
+}
+
 extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_grad, int grad_type, const void *ids, int id_bytes,
                                float scale, int accumulate, void *table_grad, int64_t rows, int64_t ld_table, int table_type,
                                void *workspace, size_t workspace_bytes, void *stream) {
@@ -575,45 +632,25 @@ extern "C" int vec_lookup_grad(const void *grad, int64_t n, int d, int64_t ld_gr
         return PQ_OK;
     }
     char *ws = (char *)workspace;
-    uint32_t *key[2] = {(uint32_t *)(ws + p.key0), (uint32_t *)(ws + p.key1)}, *pos[2] = {(uint32_t *)(ws + p.pos0), (uint32_t *)(ws + p.pos1)};
-    uint32_t *counts = (uint32_t *)(ws + p.counts);
-    uint32_t *sums = (uint32_t *)(ws + p.sums), *totals = sums + ((size_t)p.segs << p.bits);
     uint32_t *begins = (uint32_t *)(ws + p.begins);
     float *part = (float *)(ws + p.part);
     // a pass's share of the rows to clear, 32 KB and more a block
     const size_t row_bytes = vec_bytes(table_type) * (size_t)d;
-    GradClear z = {table_grad, 0, 0, ld_table, d, (int)(row_bytes >= 32768 ? 1 : 32768 / row_bytes), 0};
-    auto share = [&](int pass, unsigned own) {
-        z.after = (int)own;
-        z.lo = z.hi;
-        z.hi = accumulate ? 0 : rows * (pass + 1) / p.passes;
-        int64_t blocks = (z.hi - z.lo + z.each - 1) / z.each;
+    GradClear clear = {table_grad, 0, 0, ld_table, d, (int)(row_bytes >= 32768 ? 1 : 32768 / row_bytes), 0};
+    auto share = [&](int pass, unsigned own, GradClear &z) {
+        clear.after = (int)own;
+        clear.lo = clear.hi;
+        clear.hi = accumulate ? 0 : rows * (pass + 1) / p.passes;
+        int64_t blocks = (clear.hi - clear.lo + clear.each - 1) / clear.each;
         while (blocks > (1 << 20)) {
-            z.each *= 2;
-            blocks = (z.hi - z.lo + z.each - 1) / z.each;
+            clear.each *= 2;
+            blocks = (clear.hi - clear.lo + clear.each - 1) / clear.each;
         }
+        z = clear;
         return dim3(own + (unsigned)blocks);
     };
-    for (int pass = 0; pass < p.passes; ++pass) {
-        const uint32_t *ki = pass ? key[(pass - 1) & 1] : nullptr, *pi = pass ? pos[(pass - 1) & 1] : nullptr;
-        const int shift = pass * p.bits;
-        if (id_bytes == 4)
-            hipLaunchKernelGGL((k_vec_grad_count<int32_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int32_t *)ids, ki, n, rows, shift, p.bits, counts);
-        else
-            hipLaunchKernelGGL((k_vec_grad_count<int64_t>), dim3((unsigned)p.tiles), dim3(1024), 0, s, (const int64_t *)ids, ki, n, rows, shift, p.bits, counts);
-        if (p.segs > 0) {
-            const dim3 threads(p.bits < 6 ? 64 : 1u << p.bits);
-            hipLaunchKernelGGL(k_vec_grad_running, dim3((unsigned)p.segs), threads, 0, s, counts, p.tiles, p.seg, p.bits, sums);
-            hipLaunchKernelGGL(k_vec_grad_running, dim3(1), threads, 0, s, sums, p.segs, p.segs, p.bits, totals);
-        }
-        const dim3 grid = share(pass, (unsigned)p.tiles);
-#define GO(ID, TT)                                                                                                         \
-    hipLaunchKernelGGL((k_vec_grad_place<ID, TT>), grid, dim3(1024), (size_t)64 << p.bits, s, (const ID *)ids, ki, pi, n, rows, shift, p.bits, \
-                       counts, p.tiles, p.seg, sums, totals, key[pass & 1], pos[pass & 1], z)
-        VEC_TYPED(table_type, TT, if (id_bytes == 4) GO(int32_t, TT); else GO(int64_t, TT));
-#undef GO
-    }
-    const uint32_t *ks = key[(p.passes - 1) & 1], *ps = pos[(p.passes - 1) & 1];
+    const GradSorted sorted = grad_sort(p, ids, id_bytes, n, rows, ws, table_type, share, s);
+    const uint32_t *ks = sorted.keys, *ps = sorted.pos;
     VEC_TYPED(grad_type, TG, VEC_TYPED(table_type, TT, GRAD_WIDTHS(d, hipLaunchKernelGGL(
         (k_vec_grad_chunks<TG, TT, E>), dim3((unsigned)((p.chunks + 3) / 4), (unsigned)((d + 64 * E - 1) / (64 * E))), dim3(256), 0, s, (const TG *)grad,
         d, ld_grad, ks, ps, n, rows, scale, accumulate, (TT *)table_grad, ld_table, begins, part, p.dpad, p.chunks, p.len))));
