@@ -14,7 +14,7 @@
 #pragma once
 #include "vec_random.h"
 
-#define AD_COLS(T) (16 / (int)sizeof(T))  // columns that a lane holds in `up` and `outer`: sixteen bytes
+#define AD_COLS(T) (16 / (int)sizeof(T))  // columns that a lane holds in `up` and `outer`: sixteen bytes, or one where the matrix has fewer columns
 
 struct AdRows {
     const void *ids;
@@ -23,13 +23,11 @@ struct AdRows {
     int adapters;
     const uint32_t *keys, *pos;   // sorted: position p holds row pos[p] of adapter keys[p] (= adapters: none); null: rows as they come
 };
-// float32 factors: the sum of `slabs` parts, times scales[e] factor
+// float32 factors: the sum of `slabs` parts
 struct AdFactor {
     const float *p;
     int64_t ld, stride;
     int slabs;
-    const float *scales;
-    float factor;
 };
 struct AdMatrix {
     const void *p;
@@ -47,6 +45,12 @@ __device__ __forceinline__ uint32_t ad_row(const AdRows &r, int64_t p) { return 
 typedef __bf16 ad_b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 ad_h8 __attribute__((ext_vector_type(8)));
 typedef uint32_t ad_u4 __attribute__((ext_vector_type(4)));
+template <int N>
+struct AdWords {
+    typedef uint32_t type __attribute__((ext_vector_type(N)));
+};
+template <int N>
+using ad_words = typename AdWords<N>::type;
 
 __device__ __forceinline__ vec_f4 ad_mma(ad_b8 a, ad_b8 b, vec_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ vec_f4 ad_mma(ad_h8 a, ad_h8 b, vec_f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -85,6 +89,15 @@ struct AdWide {  // bfloat16, fp16: f = p[0] + p[1] + p[2], each the upper eight
                 f[2 * i + 1] -= ad_cut(f[2 * i + 1]);
             }
     }
+    // zeros for those of the eight values whose bit is not set
+    __device__ __forceinline__ void only(uint32_t in) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t m = (in >> (2 * i) & 1 ? 0xffffu : 0u) | (in >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int s = 0; s < 3; ++s) p[s][i] &= m;
+        }
+    }
 };
 template <>
 struct AdWide<float> {
@@ -93,6 +106,10 @@ struct AdWide<float> {
     __device__ __forceinline__ void set(vec_f8 f) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = __float_as_uint(f[i]);
+    }
+    __device__ __forceinline__ void only(uint32_t in) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = in >> i & 1 ? p[i >> 2][i & 3] : 0u;
     }
 };
 // Eight values of T (along the contraction) for it: fp16 as two bfloat16 numbers.
@@ -108,9 +125,9 @@ template <>
 struct AdNarrow<float> {
     float p[8];
 };
-// Rows raw[0..7], AD_COLS(T) columns each: column m.
-template <class T>
-__device__ __forceinline__ AdNarrow<T> ad_column(const vec_pack<T, AD_COLS(T)> *raw, int m) {
+// Rows raw[0..7], E columns each: column m.
+template <class T, int E>
+__device__ __forceinline__ AdNarrow<T> ad_column(const vec_pack<T, E> *raw, int m) {
     AdNarrow<T> o;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -118,8 +135,13 @@ __device__ __forceinline__ AdNarrow<T> ad_column(const vec_pack<T, AD_COLS(T)> *
     } else {
         ad_u4 u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            u[i] = __builtin_amdgcn_perm(__builtin_bit_cast(ad_u4, raw[2 * i + 1])[m >> 1], __builtin_bit_cast(ad_u4, raw[2 * i])[m >> 1], m & 1 ? 0x07060302u : 0x05040100u);
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (E == 1)
+                u[i] = (uint32_t)__builtin_bit_cast(uint16_t, (T)raw[2 * i + 1][0]) << 16 | __builtin_bit_cast(uint16_t, (T)raw[2 * i][0]);
+            else
+                u[i] = __builtin_amdgcn_perm(__builtin_bit_cast(ad_words<E / 2>, raw[2 * i + 1])[m >> 1], __builtin_bit_cast(ad_words<E / 2>, raw[2 * i])[m >> 1],
+                                             m & 1 ? 0x07060302u : 0x05040100u);
+        }
         if constexpr (__is_same(T, __bf16)) {
             o.p[0] = u;
         } else {
@@ -160,20 +182,74 @@ __device__ __forceinline__ vec_f4 ad_mul(const AdNarrow<T> &n, const AdWide<T> &
     return c;
 }
 
-// Elements of a mask of eight columns that hold E columns from the one at `col` on.
+// Which of the eight columns 8 col8 and on are kept, a bit each.
+__device__ __forceinline__ uint32_t ad_bits(VecKey key, const VecMask &mask, uint32_t row, uint32_t col8) {
+    const vec_i4 k = vec_random(key, mask.layer, row, col8);
+    uint32_t b = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const uint32_t u = (uint32_t)k[w];
+        b |= ((u & 0xffffu) >= mask.threshold ? 1u : 0u) << (2 * w) | ((u >> 16) >= mask.threshold ? 2u : 0u) << (2 * w);
+    }
+    return b;
+}
+// The same of the E columns from `from` on (a lane's own, or at the matrix's end any).
+template <int E>
+__device__ __forceinline__ uint32_t ad_kept(VecKey key, const VecMask &mask, uint32_t row, int from) {
+    const int shift = from & 7;
+    uint32_t b = ad_bits(key, mask, row, (uint32_t)from >> 3);
+    if (shift + E > 8) b |= ad_bits(key, mask, row, ((uint32_t)from >> 3) + 1) << 8;
+    return b >> shift;
+}
+// Zeros in place of what is dropped.
 template <class T, int E>
-__device__ __forceinline__ vec_pack<T, E> ad_drop(vec_pack<T, E> v, vec_i4 kept, int64_t col) {
-    if constexpr (E == 8) {
-        return vec_drop<T>(v, kept);
+__device__ __forceinline__ vec_pack<T, E> ad_drop(vec_pack<T, E> v, uint32_t kept) {
+    if constexpr (E > 1 && sizeof(T) == 2) {
+        auto u = __builtin_bit_cast(ad_words<E / 2>, v);
+#pragma unroll
+        for (int w = 0; w < E / 2; ++w) u[w] &= (kept >> (2 * w) & 1 ? 0xffffu : 0u) | (kept >> (2 * w + 1) & 1 ? 0xffff0000u : 0u);
+        return __builtin_bit_cast(vec_pack<T, E>, u);
     } else {
-        static_assert(E == 4 && sizeof(T) == 4, "");
-        const bool second = col & 4;
-        const int a = second ? kept[2] : kept[0], b = second ? kept[3] : kept[1];
-        v[0] = a & 1 ? v[0] : 0.0f;
-        v[1] = a >> 16 & 1 ? v[1] : 0.0f;
-        v[2] = b & 1 ? v[2] : 0.0f;
-        v[3] = b >> 16 & 1 ? v[3] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (!(kept >> i & 1)) v[i] = 0;
         return v;
+    }
+}
+// The same for eight rows.  whole: the wave's columns are all there; neighbouring lanes that hold halves of eight columns then make four rows' bits each.
+template <class T, int E, class ROW>
+__device__ __forceinline__ void ad_drop8(vec_pack<T, E> *v, VecKey key, const VecMask &mask, ROW row, int from, bool whole) {
+    if (E == 4 && whole) {
+        const int half = threadIdx.x & 1;
+        uint32_t mine = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mine |= ad_bits(key, mask, row(4 * half + q), (uint32_t)from >> 3) << (8 * q);
+        const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0xb1, 0xf, 0xf, true);  // (of the lane beside)
+        const uint32_t low = half ? other : mine, high = half ? mine : other;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = ad_drop<T, E>(v[q], (q < 4 ? low : high) >> (8 * (q & 3) + 4 * half));
+    } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = ad_drop<T, E>(v[q], ad_kept<E>(key, mask, row(q), from));
+    }
+}
+
+// A lane's E columns from col on, where the matrix ends: every lane reads E columns, those at the end the last E (d >= E; matrices of fewer
+// columns take E = 1), and writes what is its own of them.  (Reads of part of the columns cost the loops twice their registers.)
+template <int E>
+__device__ __forceinline__ int ad_from(int col, int d) { return col + E <= d ? col : d - E; }
+template <class T, int E>
+__device__ __forceinline__ vec_pack<T, E> ad_load(const T *row, int from) { return *(const vec_pack<T, E> *)(row + from); }
+template <class T, int E>
+__device__ __forceinline__ void ad_store(T *row, int col, int d, vec_f<E> v) {
+    const vec_pack<T, E> o = __builtin_convertvector(v, vec_pack<T, E>);
+    const int from = ad_from<E>(col, d);
+    if (from == col) {
+        *(vec_pack<T, E> *)(row + col) = o;
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (from + i >= col) row[from + i] = o[i];
     }
 }
 
@@ -184,8 +260,8 @@ struct AdTile {
     uint32_t row;
     bool in;
 };
-__device__ __forceinline__ AdTile ad_tile(const AdRows &r, int lane) {
-    const int64_t p = vec_block() * r.tp + lane;
+__device__ __forceinline__ AdTile ad_tile(const AdRows &r, int64_t tile, int lane) {
+    const int64_t p = tile * r.tp + lane;
     AdTile t = {r.adapters, 0, lane < r.tp && p < r.n};
     if (t.in) {
         t.id = ad_id(r, p);
@@ -201,14 +277,25 @@ __device__ __forceinline__ int ad_list(uint64_t bits, uint32_t row, uint32_t *li
 }
 
 // -------------------------------------------------------------------- down --
-// part[slab][row][rank] = sum over the slab's columns of (kept) x_row W_e^T, rows padded to `rp` ranks, with zeros.  A block takes a
-// tile of positions, 16 RK ranks and a slab of columns; its four waves take turns at 32 columns each and join their sums through LDS.  W's rows are the
-// instruction's first factor, so that a lane holds four neighbouring ranks of a row.  Rows of x go to registers as the matrix cores want them, without LDS.
+// part[slab][row][rank] = by the sum over the slab's columns of (kept) x_row W_e^T, rows padded to `rp` ranks, with zeros.  A block takes a
+// tile of positions and a slab of columns (one slab unless there are few rows); its waves (4 or 8) take turns at 32 columns each and join their sums
+// through LDS.  W's rows are the instruction's first factor, so that a lane holds four neighbouring ranks of a row.  Rows of x go to registers as the matrix
+// cores want them, without LDS.  Neighbouring blocks begin at different columns: rows are often a multiple of 4 KB apart, and blocks that read the same columns of
+// their rows at the same time would ask few of the memory's channels.
+#define AD_DOWN_WAVES 8
+// (rows without an adapter)
+__device__ __forceinline__ void ad_zeros(uint64_t bits, uint32_t row, uint32_t *list, int rank, float *__restrict__ keep) {
+    if (!bits) return;
+    const int count = ad_list(bits, row, list, threadIdx.x & 63);
+    for (int i = threadIdx.x; i < count * rank; i += blockDim.x) keep[(int64_t)list[i / rank] * rank + i % rank] = 0.0f;
+    __builtin_amdgcn_wave_barrier();
+}
 template <class T, int RK, int NT, bool MASK>
-__device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ w, int64_t ld_w, int d, int kb, int ke, int rank, int j0,
-                                        const uint32_t *list, int count, const VecMask &mask, VecKey key, vec_f4 *red, float *__restrict__ part, int rp) {
-    constexpr int U = sizeof(T) == 4 ? 1 : 2;  // steps on their way
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+__device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ w, int64_t ld_w, int d, int kb, int ke, int turn, int rank, int j0, float by,
+                                        const uint32_t *list, int count, const VecMask &mask, VecKey key, vec_f4 *red, float *__restrict__ part, int rp,
+                                        float *__restrict__ keep) {
+    constexpr int U = sizeof(T) == 4 || NT * RK > 8 ? 1 : 2;  // steps on their way
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, c = lane & 15, g = lane >> 4;
     const T *xp[NT], *wp[RK];
     uint32_t row[NT];
     // (lanes without a row or a rank read another's: what they give is not stored)
@@ -232,21 +319,25 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
             for (int j = 0; j < RK; ++j) acc[t][j] = ad_mul<T>(wv[j], xv[t], acc[t][j]);
         }
     };
-    const int whole = ke < d ? ke : d / 32 * 32;  // steps that begin below hold 32 columns
-    int k = kb + 32 * wave;
-    for (; k + (U - 1) * 128 + 32 <= whole; k += 128 * U) {
-        vec_pack<T> xv[U][NT], wv[U][RK];
+    const int span = waves * 32 * U, whole = ((ke < d ? ke : d / 32 * 32) - kb) / span;  // turns whose columns are all there
+    if (whole > 0) {
+        turn %= whole;
+        for (int i = 0; i < whole; ++i) {
+            const int k = kb + turn * span + 32 * wave + 8 * g;
+            if (++turn == whole) turn = 0;
+            vec_pack<T> xv[U][NT], wv[U][RK];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) xv[u][t] = *(const vec_pack<T> *)(xp[t] + k + 128 * u + 8 * g);
+                for (int t = 0; t < NT; ++t) xv[u][t] = *(const vec_pack<T> *)(xp[t] + k + waves * 32 * u);
 #pragma unroll
-            for (int j = 0; j < RK; ++j) wv[u][j] = *(const vec_pack<T> *)(wp[j] + k + 128 * u + 8 * g);
+                for (int j = 0; j < RK; ++j) wv[u][j] = *(const vec_pack<T> *)(wp[j] + k + waves * 32 * u);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) step(xv[u], wv[u], k + waves * 32 * u);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) step(xv[u], wv[u], k + 128 * u + 8 * g);
     }
-    for (; k < ke; k += 128) {
+    for (int k = kb + whole * span + 32 * wave; k < ke; k += waves * 32) {
         vec_pack<T> xv[NT], wv[RK];
         const int col = k + 8 * g;
 #pragma unroll
@@ -255,42 +346,44 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
         for (int j = 0; j < RK; ++j) wv[j] = vec_load(wp[j] + (col < d ? col : 0), d - col, col);
         step(xv, wv, col);
     }
-    // sums of the four waves, TR tiles' a round
-    constexpr int TR = NT * RK <= 8 ? NT : (RK <= 4 ? 8 / RK : 1);
+    // sums of the waves, G pairs of tiles a round
+    constexpr int G = NT * RK < 4 ? NT * RK : 4;
 #pragma unroll
-    for (int t0 = 0; t0 < NT; t0 += TR) {
+    for (int p0 = 0; p0 < NT * RK; p0 += G) {
         __syncthreads();
 #pragma unroll
-        for (int t = 0; t < TR; ++t)
-#pragma unroll
-            for (int j = 0; j < RK; ++j) red[((wave * TR + t) * RK + j) * 64 + lane] = acc[t0 + t][j];
+        for (int q = 0; q < G; ++q) red[(wave * G + q) * 64 + lane] = acc[(p0 + q) / RK][(p0 + q) % RK];
         __syncthreads();
-        for (int i = threadIdx.x; i < TR * RK * 64; i += 256) {
-            const int l = i & 63, j = (i >> 6) % RK, t = (i >> 6) / RK;
-            const int at = 16 * (t0 + t) + (l & 15), to = j0 + 16 * j + 4 * (l >> 4);
+        for (int i = threadIdx.x; i < G * 64; i += blockDim.x) {
+            const int l = i & 63, q = p0 + (i >> 6);
+            const int at = 16 * (q / RK) + (l & 15), to = j0 + 16 * (q % RK) + 4 * (l >> 4);
             if (at >= count || to >= rp) continue;
             vec_f4 s = red[i];
+            for (int v = 1; v < waves; ++v) s += red[v * G * 64 + i];
 #pragma unroll
-            for (int v = 1; v < 4; ++v) s += red[v * TR * RK * 64 + i];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) s[q] = to + q < rank ? s[q] : 0.0f;
+            for (int r = 0; r < 4; ++r) s[r] = to + r < rank ? s[r] * by : 0.0f;
             *(vec_f4 *)(part + (int64_t)list[at] * rp + to) = s;
+            if (keep) vec_store<float, 4>(keep + (int64_t)list[at] * rank + to, rank - to, s);
         }
     }
 }
 
 template <class T, int RK, bool MASK>
-__global__ void __launch_bounds__(256)
-k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, VecMask mask, float *__restrict__ part, int64_t part_stride, int rp, int per) {
-    __shared__ uint32_t lists[4][64];
-    __shared__ vec_f4 red[4 * (RK == 1 ? 4 : 8) * 64];
+__global__ void __launch_bounds__(64 * AD_DOWN_WAVES)
+k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, const float *__restrict__ scales, float factor, VecMask mask, float *__restrict__ part,
+              int64_t part_stride, int rp, int slabs, int per, float *__restrict__ keep) {
+    __shared__ uint32_t lists[AD_DOWN_WAVES][64];
+    extern __shared__ __align__(16) unsigned char smem[];  // [waves][4][64] sums
     const int lane = threadIdx.x & 63;
     uint32_t *list = lists[threadIdx.x >> 6];
-    const AdTile tile = ad_tile(rows, lane);
+    const int64_t block = vec_block(), at = slabs == 1 ? block : block / slabs;
+    const int slab = (int)(block - at * slabs);
+    const AdTile tile = ad_tile(rows, at, lane);
     VecKey key = {0, 0, 0};
     if (MASK) key = vec_key(mask);
-    const int kb = blockIdx.z * per, ke = kb + per < m.d ? kb + per : m.d;
-    part += blockIdx.z * part_stride;
+    const int kb = slab * per, ke = kb + per < m.d ? kb + per : m.d;
+    part += slab * part_stride;
+    if (keep) ad_zeros(__ballot(tile.in && tile.id == rows.adapters), tile.row, list, m.rank, keep);
     uint64_t todo = __ballot(tile.id < rows.adapters);
     while (todo) {
         const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
@@ -298,12 +391,14 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, Ve
         todo &= ~bits;
         const int count = ad_list(bits, tile.row, list, lane);
         const T *w = (const T *)m.p + e * m.stride;
+        const float by = scales ? scales[e] * factor : factor;
         for (int j0 = 0; j0 < m.rank; j0 += 16 * RK) {
-            if (RK <= 2 && count > 32) ad_down<T, RK, RK <= 2 ? 4 : 1, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, m.rank, j0, list, count, mask, key, red, part, rp);
-            else if (count > 16) ad_down<T, RK, 2, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, m.rank, j0, list, count, mask, key, red, part, rp);
-            else ad_down<T, RK, 1, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, m.rank, j0, list, count, mask, key, red, part, rp);
+#define GO(NT) ad_down<T, RK, NT, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, (int)(at & 0xffff), m.rank, j0, by, list, count, mask, key, (vec_f4 *)smem, part, rp, keep)
+            if (RK <= 2 && count > 32) GO(RK <= 2 ? 4 : 1);
+            else if (count > 16) GO(2);
+            else GO(1);
+#undef GO
         }
-        __syncthreads();  // (other waves read their lists' rows for the last stores; these are equal, the sums' buffer is not)
     }
 }
 
@@ -311,66 +406,65 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, Ve
 // y_row = base_row + (kept) f_row W_e.  A block takes a tile of positions and 64 AD_COLS columns at a time, a quarter a wave.  The factor f is made ready
 // in LDS once (its parts as the matrix cores take them); a lane reads eight ranks of AD_COLS columns of W, whose columns are put together from
 // their halves by byte permutations.  Lane c reads column group 4 (c % 4) + c / 4, so that the four lanes of a row hold neighbouring groups of the result.
-template <class T, class Y, bool MASK>
+template <class T, class Y, bool MASK, int E>
 struct AdUp {
-    static constexpr int E = AD_COLS(T);
     const Y *base;
     Y *y;
     int64_t ld_base, ld_y;
-    int d, c0;
+    int d;
     VecMask mask;
     VecKey key;
 
-    __device__ __forceinline__ void write(const vec_f4 *acc, uint32_t row) const {  // acc: a lane's groups 4 i + lane / 16, column m of each
+    // a lane's groups 4 i + lane / 16 of a row
+    __device__ __forceinline__ void read(vec_pack<Y, E> *b, uint32_t row, int c0) const {
         const int g = (threadIdx.x & 63) >> 4;
-        vec_pack<Y, E> b[4];
+        if (!base) return;
+        const Y *p = base + (int64_t)row * ld_base;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = c0 + E * (4 * i + g);
-            if (base) b[i] = vec_load<Y, E>(base + row * ld_base + (col < d ? col : 0), d - col, col);
-        }
+        for (int i = 0; i < 4; ++i) b[i] = ad_load<Y, E>(p, ad_from<E>(c0 + E * (4 * i + g), d));
+    }
+    __device__ __forceinline__ void write(const vec_f4 *acc, const vec_pack<Y, E> *b, uint32_t row, int c0) const {  // acc[m]: column m of each
+        const int g = (threadIdx.x & 63) >> 4;
+        Y *p = y + (int64_t)row * ld_y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int col = c0 + E * (4 * i + g);
             if (col >= d) continue;
-            vec_pack<float, E> f;
+            vec_f<E> f;
 #pragma unroll
             for (int m = 0; m < E; ++m) f[m] = acc[m][i];
             if (MASK) {
-                const vec_i4 kept = vec_kept(vec_random(key, mask.layer, row, (uint32_t)col >> 3), mask.threshold);
+                const uint32_t kept = ad_kept<E>(key, mask, row, ad_from<E>(col, d));
 #pragma unroll
-                for (int m = 0; m < E; ++m) {
-                    const int at = (col & 7) + m;
-                    const int word = E == 8 ? kept[m >> 1] : (col & 4 ? kept[2 + (m >> 1)] : kept[m >> 1]);
-                    f[m] = word >> (16 * (at & 1)) & 1 ? f[m] : 0.0f;
-                }
+                for (int m = 0; m < E; ++m) f[m] = kept >> m & 1 ? f[m] : 0.0f;
             }
-            vec_f<E> v = f;
-            if (base) v += vec_wide<Y, E>(b[i]);
-            vec_store<Y, E>(y + row * ld_y + col, d - col, v);
+            if (base) f += vec_wide<Y, E>(b[i]);
+            ad_store<Y, E>(p, col, d, f);
+            __builtin_amdgcn_sched_barrier(0);  // (a group after the other: together they take registers that a third wave needs)
         }
     }
 };
 
 // f of the list's rows, 32 ranks (chunk kc) a slot: lane holds row lane % 16 of the tile and ranks 8 (lane / 16) and on.
 template <class T>
-__device__ __forceinline__ void ad_ready(const AdFactor &f, float by, int rank, int chunks, const uint32_t *list, int count, int tiles, ad_u4 *ready, float *keep, int64_t ld_keep) {
+__device__ __forceinline__ void ad_ready(const AdFactor &f, int rank, int chunks, const uint32_t *list, int count, int tiles, ad_u4 *ready, float *__restrict__ keep) {
     constexpr int P = AdWide<T>::parts;
     for (int i = threadIdx.x; i < tiles * chunks * 64; i += 256) {
         const int l = i & 63, t = (i >> 6) % tiles, kc = (i >> 6) / tiles;
         const int at = 16 * t + (l & 15), r0 = 32 * kc + 8 * (l >> 4);
         vec_f8 v = (vec_f8)0.0f;
-        if (at < count && r0 < rank) {
+        if (at < count && r0 < f.ld) {  // (rows are padded to sixteen ranks, with zeros)
             const float *p = f.p + (int64_t)list[at] * f.ld + r0;
-            for (int s = 0; s < f.slabs; ++s) {
-                const vec_f4 a = *(const vec_f4 *)p, b = *(const vec_f4 *)(p + 4);  // (rows are padded to sixteen ranks, with zeros)
+            v = *(const vec_f8 *)p;
+            for (int s = 1; s < f.slabs; s += 3) {  // three on their way
+                vec_f8 w[3];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] += a[q], v[4 + q] += b[q];
-                p += f.stride;
+                for (int u = 0; u < 3; ++u) w[u] = *(const vec_f8 *)(p + (s + u < f.slabs ? s + u : 0) * f.stride);
+#pragma unroll
+                for (int u = 0; u < 3; ++u)
+                    if (s + u < f.slabs) v += w[u];
             }
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = r0 + q < rank ? v[q] * by : 0.0f;
-            if (keep) vec_store<float>(keep + (int64_t)list[at] * ld_keep + r0, rank - r0, v);
+            if (keep) vec_store<float>(keep + (int64_t)list[at] * rank + r0, rank - r0, v);
         }
         AdWide<T> o;
         o.set(v);
@@ -379,99 +473,134 @@ __device__ __forceinline__ void ad_ready(const AdFactor &f, float by, int rank, 
     }
 }
 
-template <class T, class Y, bool MASK, bool ONE>  // ONE: at most 32 ranks
-__global__ void __launch_bounds__(256)
-k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y, VecMask mask, float *__restrict__ keep) {
-    constexpr int E = AD_COLS(T), P = AdWide<T>::parts;
+// The rows of a list and a wave's 16 E columns from c0 on: requested, then computed.
+template <class T, class Y, bool MASK, bool ONE, int E>
+struct AdUpPass {
+    static constexpr int P = AdWide<T>::parts;
+    const AdUp<T, Y, MASK, E> &up;
+    const AdMatrix &m;
+    const T *w;  // null: no adapter
+    const uint32_t *list;
+    int count, chunks, c0;
+    vec_pack<T, E> raw[8];
+    vec_pack<Y, E> b[4];
+
+    // (lanes without a rank read the last one's: their part of the factor is zero)
+    __device__ __forceinline__ void weights(int kc) {
+        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, from = ad_from<E>(c0 + E * (4 * (c & 3) + (c >> 2)), m.d);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int r = 32 * kc + 8 * g + q;
+            raw[q] = ad_load<T, E>(w + (int64_t)(r < m.rank ? r : m.rank - 1) * m.ld, from);
+        }
+    }
+    __device__ __forceinline__ uint32_t row(int t) const {
+        const int i = 16 * t + (threadIdx.x & 15);
+        return list[i < count ? i : 0];
+    }
+    __device__ __forceinline__ void request(int from) {
+        c0 = from;
+        if (w) weights(0);
+        up.read(b, row(0), c0);
+    }
+    __device__ __forceinline__ void run(const ad_u4 *ready) {
+        const int lane = threadIdx.x & 63, c = lane & 15, tiles = (count + 15) / 16;
+        auto factor = [&](int kc, int t) {
+            AdWide<T> o;
+#pragma unroll
+            for (int s = 0; s < P; ++s) o.p[s] = ready[((kc * tiles + t) * P + s) * 64 + lane];
+            return o;
+        };
+        if constexpr (ONE) {
+            for (int t = 0; t < tiles; ++t) {
+                vec_pack<Y, E> next[4];
+                if (t + 1 < tiles) up.read(next, row(t + 1), c0);
+                vec_f4 acc[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) acc[i] = (vec_f4)0.0f;
+                if (w) {
+                    const AdWide<T> a = factor(0, t);
+                    if constexpr (sizeof(T) == 2 && E > 1)  // (fp16 columns as two bfloat16 numbers, all at once, are registers that the rows on their way need)
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) asm volatile("" : "+v"(raw[q]));
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        acc[i] = ad_mul<T, false>(ad_column<T, E>(raw, i), a, acc[i]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                if (16 * t + c < count) up.write(acc, b, row(t), c0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = next[i];
+            }
+        } else {  // (tiles of at most 32 positions)
+            vec_f4 acc[2][E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) acc[0][i] = acc[1][i] = (vec_f4)0.0f;
+            for (int kc = 0; kc < (w ? chunks : 0); ++kc) {
+                vec_pack<T, E> here[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) here[q] = raw[q];
+                if (kc + 1 < chunks) weights(kc + 1);
+                const AdWide<T> a = factor(kc, 0), a1 = factor(kc, tiles > 1 ? 1 : 0);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const AdNarrow<T> o = ad_column<T, E>(here, i);
+                    acc[0][i] = ad_mul<T, false>(o, a, acc[0][i]);
+                    if (tiles > 1) acc[1][i] = ad_mul<T, false>(o, a1, acc[1][i]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (c < count) up.write(acc[0], b, row(0), c0);
+            if (tiles > 1) up.read(b, row(1), c0);
+            if (16 + c < count) up.write(acc[1], b, row(1), c0);
+        }
+    }
+};
+
+template <class T, class Y, bool MASK, bool ONE, int E>  // ONE: at most 32 ranks
+__global__ void __launch_bounds__(256, 2)
+k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y, VecMask mask, int column_blocks, float *__restrict__ keep) {
     extern __shared__ __align__(16) unsigned char smem[];
     ad_u4 *ready = (ad_u4 *)smem;  // [chunk][tile][part][lane]
     __shared__ uint32_t lists[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t *list = lists[wave];
-    const AdTile tile = ad_tile(rows, lane);
+    const int64_t block = vec_block(), at = block / column_blocks;
+    const int first = (int)(block - at * column_blocks) * 64 * E + wave * 16 * E, step = column_blocks * 64 * E;
+    const AdTile tile = ad_tile(rows, at, lane);
     const int chunks = ONE ? 1 : (m.rank + 31) / 32;
-    AdUp<T, Y, MASK> up = {base, y, ld_base, ld_y, m.d, 0, mask, {0, 0, 0}};
+    AdUp<T, Y, MASK, E> up = {base, y, ld_base, ld_y, m.d, mask, {0, 0, 0}};
     if (MASK) up.key = vec_key(mask);
+    if (block != at * column_blocks) keep = nullptr;  // (a tile's first block writes it)
+    if (keep) ad_zeros(__ballot(tile.in && tile.id == rows.adapters), tile.row, list, m.rank, keep);
     uint64_t todo = __ballot(tile.in);
     while (todo) {
         const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
         const uint64_t bits = __ballot(tile.in && tile.id == e);
         todo &= ~bits;
         const bool none = e == rows.adapters;
-        if (none && base == y && !keep) continue;
+        if (none && base == y) continue;
         const int count = ad_list(bits, tile.row, list, lane), tiles = (count + 15) / 16;
-        float *const kept = blockIdx.z == 0 ? keep : nullptr;
-        if (none) {
-            if (kept)
-                for (int i = threadIdx.x; i < count * m.rank; i += 256) kept[(int64_t)list[i / m.rank] * m.rank + i % m.rank] = 0.0f;
-            if (base == y) continue;
-        } else {
-            const float by = f.scales ? f.scales[e] * f.factor : f.factor;
-            ad_ready<T>(f, by, m.rank, chunks, list, count, tiles, ready, kept, m.rank);
+        const T *w = none ? nullptr : (const T *)m.p + e * m.stride;
+        // what the first tile needs is asked for before the factor is made ready
+        AdUpPass<T, Y, MASK, ONE, E> pass = {up, m, w, list, count, chunks};
+        if (first < m.d) pass.request(first);
+        if (!none) {
+            ad_ready<T>(f, m.rank, chunks, list, count, tiles, ready, keep);
             __syncthreads();
         }
-        const T *w = (const T *)m.p + (none ? 0 : e * m.stride);
-        for (up.c0 = (blockIdx.z * 4 + wave) * 16 * E; up.c0 < m.d; up.c0 += gridDim.z * 64 * E) {
-            const int col = up.c0 + E * (4 * (c & 3) + (c >> 2));
-            auto weights = [&](int kc, AdNarrow<T> *o) {
-                vec_pack<T, E> raw[8];
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int r = 32 * kc + 8 * g + q;
-                    raw[q] = vec_load<T, E>(w + (r < m.rank && col < m.d ? r * m.ld + col : 0), r < m.rank ? m.d - col : 0, col);
-                }
-#pragma unroll
-                for (int i = 0; i < E; ++i) o[i] = ad_column<T>(raw, i);
-            };
-            auto factor = [&](int kc, int t) {
-                AdWide<T> o;
-#pragma unroll
-                for (int s = 0; s < P; ++s) o.p[s] = ready[((kc * tiles + t) * P + s) * 64 + lane];
-                return o;
-            };
-            if (none) {
-                vec_f4 acc[E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) acc[i] = (vec_f4)0.0f;
-                for (int t = 0; t < tiles; ++t)
-                    if (16 * t + c < count) up.write(acc, list[16 * t + c]);
-            } else if (ONE) {
-                AdNarrow<T> o[E];
-                weights(0, o);
-                for (int t = 0; t < tiles; ++t) {
-                    const AdWide<T> a = factor(0, t);
-                    vec_f4 acc[E];
-#pragma unroll
-                    for (int i = 0; i < E; ++i) acc[i] = ad_mul<T, false>(o[i], a, (vec_f4)0.0f);
-                    if (16 * t + c < count) up.write(acc, list[16 * t + c]);
-                }
-            } else {  // (tiles of at most 32 positions)
-                vec_f4 acc[2][E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) acc[0][i] = acc[1][i] = (vec_f4)0.0f;
-                for (int kc = 0; kc < chunks; ++kc) {
-                    AdNarrow<T> o[E];
-                    weights(kc, o);
-                    const AdWide<T> a = factor(kc, 0);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) acc[0][i] = ad_mul<T, false>(o[i], a, acc[0][i]);
-                    if (tiles > 1) {
-                        const AdWide<T> b = factor(kc, 1);
-#pragma unroll
-                        for (int i = 0; i < E; ++i) acc[1][i] = ad_mul<T, false>(o[i], b, acc[1][i]);
-                    }
-                }
-                if (c < count) up.write(acc[0], list[c]);
-                if (16 + c < count) up.write(acc[1], list[16 + c]);
-            }
+        for (int c0 = first; c0 < m.d; c0 += step) {
+            if (c0 != first) pass.request(c0);
+            pass.run(ready);
         }
-        __syncthreads();
+        if (todo) __syncthreads();
     }
 }
 
 // ------------------------------------------------------------------- outer --
-// G_e[j][col] = sum over the rows of e of f_row[j] (kept) x_row[col].  A block takes `len` sorted positions and 64 AD_COLS columns, a quarter a wave, and goes through
-// the runs of equal ids among them.  Runs that lie within the block's positions are written; the others' sums go to part[chunk][0] (began before)
+// G_e[j][col] = sum over the rows of e of f_row[j] (kept) x_row[col].  A block takes `len` sorted positions and 64 AD_COLS columns, a quarter a wave, in steps of 32
+// positions whatever runs of equal ids these hold: the rows of a step are read once, and each run among them takes its own and zeros for the others.  Runs that lie within the block's positions are written; the others' sums go to part[chunk][0] (began before)
 // or part[chunk][1], which k_vec_ad_join adds up in order.  Per step a lane reads eight rows of AD_COLS columns.
 #define AD_STAGE 128  // positions whose factors are made ready at once
 struct AdOuter {
@@ -481,122 +610,174 @@ struct AdOuter {
     int dpad, accumulate;
 };
 template <class O, int E>
-__device__ __forceinline__ void ad_put(O *p, int64_t left, vec_f<E> v, int64_t before, bool accumulate) {
-    if (accumulate) v += vec_wide<O, E>(vec_load<O, E>(p, left, before));
-    vec_store<O, E>(p, left, v);
+__device__ __forceinline__ void ad_put(O *row, int col, int d, vec_f<E> v, bool accumulate) {
+    if (accumulate) v += vec_wide<O, E>(ad_load<O, E>(row, ad_from<E>(col, d)));
+    ad_store<O, E>(row, col, d, v);
 }
 
-template <class T, class O, int RK, bool MASK>
-__global__ void __launch_bounds__(256)
-k_vec_ad_outer(AdRows rows, int len, AdFactor f, int rank, const T *__restrict__ x, int64_t ld_x, int d, VecMask mask, AdOuter o) {
-    constexpr int E = AD_COLS(T), P = AdWide<T>::parts, STEPS = AD_STAGE / 32;
-    __shared__ ad_u4 ready[STEPS][RK][P][64];
-    __shared__ uint32_t at[AD_STAGE];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-    const int64_t chunk = blockIdx.x, p0 = chunk * len, p1 = p0 + len < rows.n ? p0 + len : rows.n;
-    const int col = (blockIdx.y * 4 + wave) * 16 * E + E * c, j0 = blockIdx.z * 16 * RK;
+#define AD_MAX_LEN 1024  // positions of a block at most
+#define AD_MAX_LEN 1024  // positions of a block at most
+template <class T, class O, int RK, bool MASK, int E>
+__global__ void __launch_bounds__(256, 2)
+k_vec_ad_outer(AdRows rows, int len, AdFactor f, int rank, const T *__restrict__ x, int64_t ld_x, int d, VecMask mask, AdOuter o, int column_blocks) {
+    constexpr int P = AdWide<T>::parts;
+    __shared__ ad_u4 ready[AD_STAGE / 32 * RK * P * 64];  // [step][16 ranks][part][lane]
+    __shared__ uint32_t keys[AD_MAX_LEN], at[AD_MAX_LEN];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int64_t block = vec_block(), chunk = block / column_blocks, p0 = chunk * len;
+    if (p0 >= rows.n) return;
+    const int size = (int)(rows.n - p0 < len ? rows.n - p0 : len);
+    const int c0 = ((int)(block - chunk * column_blocks) * 4 + wave) * 16 * E, col = c0 + E * (lane & 15), from = ad_from<E>(col, d), j0 = blockIdx.z * 16 * RK;
     VecKey key = {0, 0, 0};
     if (MASK) key = vec_key(mask);
-    for (int64_t a = p0; a < p1;) {
-        const uint32_t e = rows.keys[a];
-        if (e >= (uint32_t)rows.adapters) break;  // (rows without an adapter come last)
-        int64_t b = a + 1;
-        for (;;) {  // the run's end
-            const uint64_t other = __ballot(b + lane >= p1 || rows.keys[b + lane] != e);
-            if (other) {
-                b += __builtin_ctzll(other);
-                break;
-            }
-            b += 64;
+    int total = size;
+    if (size > 0 && rows.keys[p0 + size - 1] >= (uint32_t)rows.adapters) {  // (rows without an adapter come last)
+        total = 0;
+        for (int i = lane; i < (size + 63) / 64 * 64; i += 64) total += __popcll(__ballot(i < size && rows.keys[p0 + (i < size ? i : 0)] < (uint32_t)rows.adapters));
+    }
+    if (total == 0) return;
+    for (int i = threadIdx.x; i < total; i += 256) {
+        keys[i] = rows.keys[p0 + i];
+        at[i] = rows.pos[p0 + i];
+    }
+    const uint32_t before_key = p0 > 0 ? rows.keys[p0 - 1] : 0xffffffffu, behind_key = p0 + total < rows.n ? rows.keys[p0 + total] : 0xffffffffu;
+    __syncthreads();
+    auto request = [&](vec_pack<T, E> *v, int s0) {  // positions s0 + 8 g and on; behind the last that one again, beside zeros of the factor
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int i = s0 + 8 * g + q;
+            v[q] = ad_load<T, E>(x + (int64_t)at[i < total ? i : total - 1] * ld_x, from);
         }
-        const float by = f.scales ? f.scales[e] * f.factor : f.factor;
-        vec_f4 acc[RK][E];
+    };
+    vec_f4 acc[RK][E];
+    auto clear = [&]() {
 #pragma unroll
         for (int j = 0; j < RK; ++j)
 #pragma unroll
             for (int i = 0; i < E; ++i) acc[j][i] = (vec_f4)0.0f;
-        for (int64_t s0 = a; s0 < b; s0 += AD_STAGE) {
-            const int m = (int)(b - s0 < AD_STAGE ? b - s0 : AD_STAGE);
-            __syncthreads();
-            if (threadIdx.x < AD_STAGE) at[threadIdx.x] = (int)threadIdx.x < m ? rows.pos[s0 + threadIdx.x] : 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < STEPS * RK * 64; i += 256) {
-                const int l = i & 63, j = (i >> 6) % RK, st = (i >> 6) / RK;
-                const int r = j0 + 16 * j + (l & 15), q0 = 32 * st + 8 * (l >> 4);
-                vec_f8 v;
+    };
+    clear();
+    vec_pack<T, E> raw[8];
+    request(raw, 0);
+    const bool whole = __builtin_amdgcn_readfirstlane(c0) + 16 * E <= d;
+    int a = 0;  // where the run in hand begins
+    for (int s0 = 0; s0 < total; s0 += AD_STAGE) {
+        const int m = total - s0 < AD_STAGE ? total - s0 : AD_STAGE;
+        __syncthreads();
+        for (int i = threadIdx.x; i < (m + 31) / 32 * RK * 64; i += 256) {
+            const int l = i & 63, j = (i >> 6) % RK, st = (i >> 6) / RK;
+            const int r = j0 + 16 * j + (l & 15), q0 = 32 * st + 8 * (l >> 4);
+            const float *p = f.p + (r < rank ? r : 0);
+            vec_f8 v;
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    float sum = 0.0f;
-                    if (q0 + q < m && r < rank) {
-                        const float *p = f.p + (int64_t)at[q0 + q] * f.ld + r;
-                        for (int s = 0; s < f.slabs; ++s) sum += p[s * f.stride];
-                        sum *= by;
-                    }
-                    v[q] = sum;
-                }
-                AdWide<T> w;
-                w.set(v);
+            for (int q = 0; q < 8; ++q) v[q] = p[(int64_t)at[s0 + (q0 + q < m ? q0 + q : 0)] * f.ld];
+            for (int s = 1; s < f.slabs; ++s)
 #pragma unroll
-                for (int s = 0; s < P; ++s) ready[st][j][s][l] = w.p[s];
-            }
-            __syncthreads();
-            for (int st = 0; 32 * st < m; ++st) {
-                vec_pack<T, E> raw[8];
+                for (int q = 0; q < 8; ++q) v[q] += p[s * f.stride + (int64_t)at[s0 + (q0 + q < m ? q0 + q : 0)] * f.ld];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    const int i = 32 * st + 8 * g + q;
-                    const bool in = i < m && col < d;
-                    const uint32_t row = at[i];
-                    raw[q] = vec_load<T, E>(x + (in ? row * ld_x + col : 0), in ? d - col : 0, col);
-                    if (MASK && in) raw[q] = ad_drop<T, E>(raw[q], vec_kept(vec_random(key, mask.layer, row, (uint32_t)col >> 3), mask.threshold), col);
-                }
-                AdWide<T> w[RK];
+            for (int q = 0; q < 8; ++q) v[q] = q0 + q < m && r < rank ? __builtin_canonicalizef(v[q]) : 0.0f;
+            AdWide<T> w;
+            w.set(v);
 #pragma unroll
-                for (int j = 0; j < RK; ++j)
-#pragma unroll
-                    for (int s = 0; s < P; ++s) w[j].p[s] = ready[st][j][s][lane];
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const AdNarrow<T> v = ad_column<T>(raw, i);
-#pragma unroll
-                    for (int j = 0; j < RK; ++j) acc[j][i] = ad_mul<T, true>(v, w[j], acc[j][i]);
-                }
-            }
+            for (int s = 0; s < P; ++s) ready[((st * RK + j) * P + s) * 64 + l] = w.p[s];
         }
-        const bool before = a == p0 && p0 > 0 && rows.keys[p0 - 1] == e, behind = b == p1 && p1 < rows.n && rows.keys[p1] == e;
+        __syncthreads();
+        for (int st = 0; 32 * st < m; ++st) {
+            const int here = s0 + 32 * st, behind = here + 32 < total ? here + 32 : total;
+            vec_pack<T, E> next[8];
+            if (here + 32 < total) request(next, here + 32);
+            if (MASK)
+                ad_drop8<T, E>(raw, key, mask, [&](int q) { return at[here + 8 * g + q < total ? here + 8 * g + q : total - 1]; }, from, whole);
+            // the runs that the step holds, or parts of
+            const uint32_t mine = keys[here + (lane & 31) < behind ? here + (lane & 31) : behind - 1];
+            const uint64_t heads = __ballot(lane < behind - here && (here + lane == 0 || keys[here + lane > 0 ? here + lane - 1 : 0] != mine)) | 1ull << (behind - here);
+            for (int lo = here; lo < behind;) {
+                const int hi = here + __builtin_ctzll(heads >> (lo - here + 1)) + (lo - here + 1);
+                const bool alone = lo == here && hi == behind;  // all of the step's rows are of this run
+                uint32_t in = 0xff;
+                AdNarrow<T> v[E];
+                if (alone) {
 #pragma unroll
-        for (int j = 0; j < RK; ++j)
+                    for (int i = 0; i < E; ++i) v[i] = ad_column<T, E>(raw, i);
+                } else {  // others' rows take no part, whatever they hold
+                    vec_pack<T, E> its[8];
+                    in = 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int r = j0 + 16 * j + 4 * g + q;
-                if (r >= rank || col >= d) continue;
-                vec_f<E> v;
+                    for (int q = 0; q < 8; ++q) {
+                        const bool has = here + 8 * g + q >= lo && here + 8 * g + q < hi;
+                        in |= (has ? 1u : 0u) << q;
+                        its[q] = has ? raw[q] : (vec_pack<T, E>)(T)0.0f;
+                    }
 #pragma unroll
-                for (int i = 0; i < E; ++i) v[i] = acc[j][i][q];
-                if (before || behind) vec_store<float, E>(o.part + ((chunk * 2 + (before ? 0 : 1)) * rank + r) * (int64_t)o.dpad + col, o.dpad - col, v);
-                else ad_put<O, E>((O *)o.out + e * o.stride + r * o.ld + col, d - col, v, col, o.accumulate);
+                    for (int i = 0; i < E; ++i) v[i] = ad_column<T, E>(its, i);
+                }
+#pragma unroll
+                for (int j = 0; j < RK; ++j) {
+                    AdWide<T> w;
+#pragma unroll
+                    for (int s = 0; s < P; ++s) w.p[s] = ready[((st * RK + j) * P + s) * 64 + lane];
+                    if (!alone) w.only(in);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) acc[j][i] = ad_mul<T, true>(v[i], w, acc[j][i]);
+                    __builtin_amdgcn_sched_barrier(0);  // (all ranks' factors at once are registers that the rows on their way need)
+                }
+                const uint32_t e = keys[lo];
+                const bool goes_on = hi < total ? keys[hi] == e : behind_key == e;
+                if (hi == total || !goes_on) {  // write the run's sum, or the block's part of it
+                    const bool before = a == 0 && before_key == e;
+                    int r0 = j0 + 4 * g;
+                    asm volatile("" : "+v"(r0));  // (addresses of all ranks are made here, not kept over the loops)
+#pragma unroll
+                    for (int j = 0; j < RK; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int r = r0 + 16 * j + q;
+                            if (r >= rank || col >= d) continue;
+                            vec_f<E> v;
+#pragma unroll
+                            for (int i = 0; i < E; ++i) v[i] = acc[j][i][q];
+                            if (before || goes_on) ad_store<float, E>(o.part + ((chunk * 2 + (before ? 0 : 1)) * rank + r) * (int64_t)o.dpad, col, d, v);
+                            else ad_put<O, E>((O *)o.out + e * o.stride + r * o.ld, col, d, v, o.accumulate);
+                        }
+                    clear();
+                    a = hi;
+                }
+                lo = hi;
             }
-        a = b;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) raw[q] = next[q];
+        }
     }
 }
 
-// The sums of ids whose positions several blocks held, and zeros for those without a row.
+// The sums of ids whose positions several blocks held, and zeros for those without a row; both gradients in one launch (blockIdx.z).
+struct AdJoin {
+    AdOuter o;
+    int len, d;
+};
 template <class O>
 __global__ void __launch_bounds__(256)
-k_vec_ad_join(AdRows rows, int len, int rank, int d, AdOuter o) {
-    const int64_t n = rows.n;
+k_vec_ad_join(AdRows rows, int rank, AdJoin ja, AdJoin jb) {
+    const AdJoin &j = blockIdx.z ? jb : ja;
+    const AdOuter &o = j.o;
+    __shared__ int64_t found[2];
     const uint32_t e = blockIdx.y;
-    auto first = [&](uint32_t key) {  // the first position whose key is at least this
-        int64_t lo = 0, hi = n;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (wave < 2) {  // the first position whose key is at least e (at least e + 1), a 64th of what is left a round
+        int64_t lo = 0, hi = rows.n;
         while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (rows.keys[mid] < key) lo = mid + 1;
-            else hi = mid;
+            const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
+            const uint64_t below = __ballot(p < hi && rows.keys[p < hi ? p : lo] < e + wave);  // (a prefix of the lanes)
+            const int k = __popcll(below);
+            if (k == 0) break;
+            hi = lo + k * step < hi ? lo + k * step : hi;
+            lo += (k - 1) * step + 1;
         }
-        return lo;
-    };
-    const int64_t lo = first(e), hi = first(e + 1);
-    const int64_t from = lo / len, to = lo < hi ? (hi - 1) / len : 0;
+        if (lane == 0) found[wave] = lo;
+    }
+    __syncthreads();
+    const int64_t lo = found[0], hi = found[1];
+    const int64_t from = lo / j.len, to = lo < hi ? (hi - 1) / j.len : 0;
     if (lo < hi ? from == to : o.accumulate) return;
     const int pieces = o.dpad / 8;
     for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < (int64_t)rank * pieces; i += gridDim.x * 256) {
@@ -606,9 +787,96 @@ k_vec_ad_join(AdRows rows, int len, int rank, int d, AdOuter o) {
             const int64_t each = 2 * (int64_t)rank * o.dpad;
             const float *p = o.part + (int64_t)r * o.dpad + col;
             sum = *(const vec_f8 *)(p + from * each + each / 2);
-#pragma unroll 8
-            for (int64_t k = from + 1; k <= to; ++k) sum += *(const vec_f8 *)(p + k * each);
+            int64_t k = from + 1;
+            for (; k + 8 <= to + 1; k += 8) {
+                vec_f8 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = *(const vec_f8 *)(p + (k + u) * each);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) sum += v[u];
+            }
+            for (; k <= to; ++k) sum += *(const vec_f8 *)(p + k * each);
         }
-        ad_put<O, 8>((O *)o.out + e * o.stride + r * o.ld + col, d - col, sum, col, o.accumulate);
+        O *out = (O *)o.out + e * o.stride + r * o.ld + col;
+        if (o.accumulate) sum += vec_wide<O>(vec_load<O>(out, j.d - col, col));
+        vec_store<O>(out, j.d - col, sum);
+    }
+}
+
+// ----------------------------------------------------------------- grouping --
+// Positions sorted by id (stable), up to AD_GROUP_ROWS rows and AD_GROUP_ADAPTERS adapters: one launch.  A block places AD_GROUP_TILE positions.  It counts all ids itself,
+// those before its own apart (16,384 ids are 128 KB from the L2 cache); neighbours with one id count at once, so that runs do not queue for one counter.
+#define AD_GROUP_TILE 256
+#define AD_GROUP_ROWS 65536
+#define AD_GROUP_ADAPTERS 4095
+template <class ID>
+__global__ void __launch_bounds__(1024)
+k_vec_ad_group(const ID *__restrict__ ids, int n, int adapters, uint32_t *__restrict__ keys, uint32_t *__restrict__ pos) {
+    __shared__ uint32_t early[AD_GROUP_ADAPTERS + 1], late[AD_GROUP_ADAPTERS + 1], wide[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * AD_GROUP_TILE;
+    auto norm = [&](ID id) { return id >= 0 && id < adapters ? (uint32_t)id : (uint32_t)adapters; };
+    for (int i = threadIdx.x; i <= adapters; i += 1024) early[i] = late[i] = 0;
+    __syncthreads();
+    for (int i0 = wave * 64; i0 < n; i0 += 8 * 1024) {
+        ID id[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) id[u] = ids[i0 + u * 1024 + lane < n ? i0 + u * 1024 + lane : n - 1];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int i = i0 + u * 1024 + lane;
+            const uint32_t key = norm(id[u]), left = (uint32_t)__shfl_up((int)key, 1);
+            const bool in = i < n, head = in && (lane == 0 || left != key);
+            const uint64_t heads = __ballot(head), all = __ballot(in);
+            if (head) {
+                const uint64_t behind = lane == 63 ? 0 : heads >> (lane + 1);
+                const int length = behind ? __builtin_ctzll(behind) + 1 : __popcll(all) - lane;
+                atomicAdd(i < first ? &early[key] : &late[key], (uint32_t)length);
+            }
+        }
+    }
+    __syncthreads();
+    // where the block's first position of each id goes: the ids below it, and those before it
+    uint32_t mine[4], sum = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int b = threadIdx.x * 4 + u;
+        mine[u] = b <= adapters ? early[b] + late[b] : 0;
+        sum += mine[u];
+    }
+    uint32_t s = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t v = __shfl_up(s, o);
+        if (lane >= o) s += v;
+    }
+    if (lane == 63) wide[wave] = s;
+    __syncthreads();
+    uint32_t at = s - sum;
+    for (int v = 0; v < wave; ++v) at += wide[v];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int b = threadIdx.x * 4 + u;
+        if (b <= adapters) early[b] += at;
+        at += mine[u];
+    }
+    __syncthreads();
+    const int i = first + (int)threadIdx.x;
+    const bool in = threadIdx.x < AD_GROUP_TILE && i < n;
+    const uint32_t key = in ? norm(ids[i]) : 0;
+    uint64_t same = __ballot(in);
+    for (int b = 0; adapters >> b; ++b) {
+        const uint64_t v = __ballot(key >> b & 1);
+        same &= key >> b & 1 ? v : ~v;
+    }
+#pragma unroll
+    for (int v = 0; v < AD_GROUP_TILE / 64; ++v) {  // a wave after the other
+        if (wave == v && in) {
+            const uint32_t to = early[key] + __popcll(same & ((1ull << lane) - 1));
+            keys[to] = key;
+            pos[to] = (uint32_t)i;
+        }
+        __syncthreads();
+        if (wave == v && in && (same >> lane) == 1) early[key] += __popcll(same);  // the id's last lane
+        __syncthreads();
     }
 }

@@ -5,42 +5,53 @@
 size_t qadc_vec_sort_bytes(int64_t n, int64_t rows);
 void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char *ws, const uint32_t **keys, const uint32_t **pos, hipStream_t s);
 
-#define AD_MOST_UNSORTED 512  // rows of several adapters up to which each is a tile of its own
+#define AD_FEW_ROWS 64  // rows that are not sorted
 #define AD_MAX_SLABS 16
 
 struct AdPlan {
-    bool sorted;
+    bool sorted, grouped;      // grouped: by k_vec_ad_group
     int tp;                    // positions of a tile
     int rp;                    // ranks of a row of partial sums
-    int slabs, per;            // of the contraction over columns
+    int waves, slabs, per;     // of the contraction over columns
     int len_a, len_b;          // positions of a piece of the sums over rows
     int dpad_a, dpad_b;
     size_t part, part_a, part_b, total;  // bytes from the workspace's start
 };
 
-static int ad_len(int64_t n, int d, int rank, int type) {
-    const int64_t across = (int64_t)((d + 63) / 64 + 7) / 8 * (type == VEC_F32 ? 2 : 1) * ((rank + 63) / 64);
-    int len = 1024;
-    while (len > AD_STAGE && (n + len - 1) / len * across < 512) len /= 2;
+static int ad_len(int64_t n, int d, int rank) {
+    const int64_t across = (int64_t)ad_outer_blocks(d) * ((rank + 63) / 64);
+    int len = AD_MAX_LEN;
+    while (len > 64 && (n + len - 1) / len * across < 512) len /= 2;
     return len;
 }
 
 static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int type, bool grad) {
     AdPlan p = {};
-    p.sorted = grad || (adapters > 1 && n > AD_MOST_UNSORTED);
-    p.tp = p.sorted || adapters <= 1 ? (n <= 1024 ? 16 : (rank <= 32 ? 64 : 32)) : 1;
+    // half as many positions a tile as an adapter has rows on average: few tiles then hold more than two or three; and at least 256 tiles, if tiles of sixteen give them
+    const int64_t each = n / (adapters > 1 ? adapters : 1);
+    p.tp = rank <= 32 && din >= 8 && dout >= 8 ? 64 : 32;  // (of k_vec_ad_up's other form at most 32)
+    while (p.tp > 1 && 2 * p.tp > each) p.tp /= 2;
+    while (p.tp > 16 && n / p.tp < 256) p.tp /= 2;
+    p.sorted = grad || (adapters > 1 && n > AD_FEW_ROWS && p.tp > 1);
+    p.grouped = n <= AD_GROUP_ROWS && adapters <= AD_GROUP_ADAPTERS;
     p.rp = (rank + 15) & ~15;
     const int d = grad ? dout : din;
-    const int64_t tiles = (n + p.tp - 1) / p.tp, want = tiles >= 512 ? 1 : (512 + tiles - 1) / tiles;
-    const int64_t slabs = want < AD_MAX_SLABS ? want : AD_MAX_SLABS, per = ((d + slabs - 1) / slabs + 255) / 256 * 256;
+    const int64_t tiles = (n + p.tp - 1) / p.tp;
+    p.waves = d >= 1024 ? 8 : 4;
+    int64_t slabs = tiles * p.waves >= 1024 ? 1 : 1024 / (tiles * p.waves);
+    if (slabs > d / (p.waves * 64)) slabs = d / (p.waves * 64);
+    if (slabs > AD_MAX_SLABS) slabs = AD_MAX_SLABS;
+    if (slabs < 1) slabs = 1;
+    const int64_t per = ((d + slabs - 1) / slabs + 255) / 256 * 256;
     p.per = (int)per;
     p.slabs = (int)((d + per - 1) / per);
-    size_t at = p.sorted ? qadc_vec_sort_bytes(n, adapters) : 0;
+    size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
+    if (p.sorted) at = p.grouped ? 2 * vec_up256((size_t)n * 4) : qadc_vec_sort_bytes(n, adapters);
     p.part = take((size_t)p.slabs * n * p.rp * 4);
     if (grad) {
-        p.len_a = ad_len(n, din, rank, type);
-        p.len_b = ad_len(n, dout, rank, type);
+        p.len_a = ad_len(n, din, rank);
+        p.len_b = ad_len(n, dout, rank);
         p.dpad_a = (din + 7) & ~7;
         p.dpad_b = (dout + 7) & ~7;
         p.part_a = take((size_t)((n + p.len_a - 1) / p.len_a) * 2 * rank * p.dpad_a * 4);
@@ -48,6 +59,19 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     }
     p.total = at;
     return p;
+}
+
+static void ad_sort(const AdPlan &p, AdRows &rows, char *ws, hipStream_t s) {
+    if (!p.grouped) {
+        qadc_vec_sort(rows.ids, rows.id_bytes, rows.n, rows.adapters, ws, &rows.keys, &rows.pos, s);
+        return;
+    }
+    uint32_t *keys = (uint32_t *)ws, *pos = (uint32_t *)(ws + vec_up256((size_t)rows.n * 4));
+    const dim3 grid((unsigned)((rows.n + AD_GROUP_TILE - 1) / AD_GROUP_TILE));
+    if (rows.id_bytes == 4) hipLaunchKernelGGL((k_vec_ad_group<int32_t>), grid, dim3(1024), 0, s, (const int32_t *)rows.ids, (int)rows.n, rows.adapters, keys, pos);
+    else hipLaunchKernelGGL((k_vec_ad_group<int64_t>), grid, dim3(1024), 0, s, (const int64_t *)rows.ids, (int)rows.n, rows.adapters, keys, pos);
+    rows.keys = keys;
+    rows.pos = pos;
 }
 
 static bool ad_sizes(int64_t n, int din, int dout, int rank, int adapters) {
@@ -62,8 +86,9 @@ extern "C" size_t vec_adapter_grad_workspace_bytes(int64_t n, int din, int dout,
     return n > 0 && adapters > 0 && ad_sizes(n, din, dout, rank, adapters) ? ad_plan(n, din, dout, rank, adapters, type, true).total : 0;
 }
 
-static int ad_column_blocks(int64_t n, int tp, int d, int type) {
-    const int64_t tiles = (n + tp - 1) / tp, most = type == VEC_F32 ? (d + 255) / 256 : (d + 511) / 512;
+// column blocks of `up`: fewer than hold the columns where there are many tiles, each then takes some in turn
+static int ad_up_blocks(int64_t n, int tp, int d, int type) {
+    const int64_t tiles = (n + tp - 1) / tp, most = ad_column_blocks(d, (int)vec_bytes(type));
     const int64_t want = tiles >= 2048 ? 1 : (2048 + tiles - 1) / tiles;
     return (int)(want < most ? want : most);
 }
@@ -103,6 +128,8 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
                 "vec_adapter: misaligned pointer");
     hipStream_t s = (hipStream_t)stream;
     const AdPlan plan = ad_plan(n, din, dout, rank, adapters, type, false);
+    const int64_t tiles = (n + plan.tp - 1) / plan.tp;
+    VEC_REQUIRE(tiles * plan.slabs <= VEC_MAX_BLOCKS && tiles * ad_up_blocks(n, plan.tp, dout, type) <= VEC_MAX_BLOCKS, "vec_adapter: n=%lld too large for one call", (long long)n);
     AdRows rows = {ids, id_bytes, plan.tp, n, adapters, nullptr, nullptr};
     char *ws = (char *)workspace;
     float *part = nullptr;
@@ -110,13 +137,15 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
     if (adapters > 0) {
         AD_WORKSPACE("vec_adapter", plan.total);
         part = (float *)(ws + plan.part);
-        if (plan.sorted) qadc_vec_sort(ids, id_bytes, n, adapters, ws, &rows.keys, &rows.pos, s);
+        if (plan.sorted) ad_sort(plan, rows, ws, s);
         const AdMatrix m = {a, ld_a, stride_a, rank, din};
-        VEC_TYPED(type, T, AdLaunch<T>::down(rows, x, ld_x, m, mask, part, n * plan.rp, plan.rp, plan.slabs, plan.per, s));
+        VEC_TYPED(type, T, AdLaunch<T>::down(rows, x, ld_x, m, scales, factor, mask, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per,
+                                             plan.slabs == 1 ? t : nullptr, s));
     }
-    const AdFactor f = {part, plan.rp, n * plan.rp, plan.slabs, scales, factor};
+    float *const keep = adapters > 0 && plan.slabs == 1 ? nullptr : t;
+    const AdFactor f = {part, plan.rp, n * plan.rp, plan.slabs};
     const AdMatrix m = {b, ld_b, stride_b, rank, dout};
-    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, t, ad_column_blocks(n, plan.tp, dout, type), s));
+    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, ad_up_blocks(n, plan.tp, dout, type), keep, s));
     QADC_LAUNCH_CHECK("vec_adapter's kernels");
     return PQ_OK;
 }
@@ -144,39 +173,40 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     const bool narrow = grad_type == type;
     AdRows rows = {ids, id_bytes, 1, n, adapters, nullptr, nullptr};
     AdPlan plan = {};
-    plan.len_a = plan.len_b = AD_STAGE;
+    plan.len_a = plan.len_b = AD_MAX_LEN;
     plan.dpad_a = (din + 7) & ~7;
     plan.dpad_b = (dout + 7) & ~7;
     AdOuter oa = {da, ld_da, stride_da, nullptr, plan.dpad_a, accumulate}, ob = {db, ld_db, stride_db, nullptr, plan.dpad_b, accumulate};
     if (n > 0) {
         plan = ad_plan(n, din, dout, rank, adapters, type, true);
         rows.tp = plan.tp;
+        const int64_t tiles = (n + plan.tp - 1) / plan.tp;
+        VEC_REQUIRE(tiles * plan.slabs <= VEC_MAX_BLOCKS && tiles * ad_up_blocks(n, plan.tp, din, type) <= VEC_MAX_BLOCKS &&
+                        (n / plan.len_a + 1) * ad_outer_blocks(din) <= VEC_MAX_BLOCKS &&
+                        (n / plan.len_b + 1) * ad_outer_blocks(dout) <= VEC_MAX_BLOCKS, "vec_adapter_grad: n=%lld too large for one call", (long long)n);
         char *ws = (char *)workspace;
         const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
-        AdFactor u = {nullptr, plan.rp, n * plan.rp, plan.slabs, scales, factor};
+        AdFactor u = {nullptr, plan.rp, n * plan.rp, plan.slabs};
         if (adapters > 0) {
             AD_WORKSPACE("vec_adapter_grad", plan.total);
             float *part = (float *)(ws + plan.part);
             u.p = part;
             oa.part = (float *)(ws + plan.part_a);
             ob.part = (float *)(ws + plan.part_b);
-            qadc_vec_sort(ids, id_bytes, n, adapters, ws, &rows.keys, &rows.pos, s);
-            const AdFactor kept = {t, rank, 0, 1, nullptr, 1.0f};
-            VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, none, part, n * plan.rp, plan.rp, plan.slabs, plan.per, s);
+            ad_sort(plan, rows, ws, s);
+            const AdFactor kept = {t, rank, 0, 1};
+            VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, scales, factor, none, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per, nullptr, s);
                       AdLaunch<T>::outer(rows, plan.len_b, kept, rank, dy, ld_dy, dout, none, ob, narrow, s);
                       AdLaunch<T>::outer(rows, plan.len_a, u, rank, x, ld_x, din, mask, oa, narrow, s));
         }
         if (dx)
-            VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, mask, nullptr, ad_column_blocks(n, plan.tp, din, type), s));
+            VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, mask, ad_up_blocks(n, plan.tp, din, type), nullptr, s));
     }
     if (adapters > 0) {
-        auto join = [&](const AdOuter &o, int len, int d) {
-            const int64_t pieces = (int64_t)rank * (o.dpad / 8);
-            const dim3 grid((unsigned)(pieces <= 256 * 64 ? (pieces + 255) / 256 : 64), (unsigned)adapters);
-            VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, len, rank, d, o));
-        };
-        join(oa, plan.len_a, din);
-        join(ob, plan.len_b, dout);
+        const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
+        const dim3 grid((unsigned)(pieces <= 256 * 64 ? (pieces + 255) / 256 : 64), (unsigned)adapters, 2);
+        const AdJoin ja = {oa, plan.len_a, din}, jb = {ob, plan.len_b, dout};
+        VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, rank, ja, jb));
     }
     QADC_LAUNCH_CHECK("vec_adapter_grad's kernels");
     return PQ_OK;

@@ -2,53 +2,58 @@
 #pragma once
 #include "vec_adapter.h"
 
+// blocks of `up` (16 bytes a lane) and `outer` (four columns a lane) that hold d columns
+static inline int ad_blocks(int d, int lane_columns) { return (d + 64 * lane_columns - 1) / (64 * lane_columns); }
+static inline int ad_column_blocks(int d, int bytes) { return ad_blocks(d, d < 16 / bytes ? 1 : 16 / bytes); }
+static inline int ad_outer_blocks(int d) { return ad_blocks(d, d < 4 ? 1 : 4); }
+
 template <class T>
 struct AdLaunch {
-    static void down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const VecMask &mask, float *part, int64_t part_stride, int rp,
-                     int slabs, int per, hipStream_t s);
+    static void down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
+                     int64_t part_stride, int rp, int waves, int slabs, int per, float *keep, hipStream_t s);
     // narrow: the result is of type T, else float32
     static void up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                   const VecMask &mask, float *keep, int column_blocks, hipStream_t s);
+                   const VecMask &mask, int column_blocks, float *keep, hipStream_t s);
     static void outer(const AdRows &rows, int len, const AdFactor &f, int rank, const void *x, int64_t ld_x, int d, const VecMask &mask, const AdOuter &o,
                       bool narrow, hipStream_t s);
 };
 
 #ifdef VEC_ADAPTER_SOURCE
-static dim3 ad_grid(const AdRows &rows, int z) {
-    dim3 g = vec_grid((rows.n + rows.tp - 1) / rows.tp, 256);
-    g.z = (unsigned)z;
-    return g;
-}
+static dim3 ad_grid(const AdRows &rows, int parts, int threads) { return vec_grid((rows.n + rows.tp - 1) / rows.tp * parts, threads); }
 
 template <class T>
-void AdLaunch<T>::down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const VecMask &mask, float *part, int64_t part_stride, int rp,
-                       int slabs, int per, hipStream_t s) {
-    const dim3 grid = ad_grid(rows, slabs);
-#define GO(RK)                                                                                                             \
-    do {                                                                                                                   \
-        if (mask.threshold)                                                                                                \
-            hipLaunchKernelGGL((k_vec_ad_down<T, RK, true>), grid, dim3(256), 0, s, rows, (const T *)x, ld_x, m, mask, part, part_stride, rp, per);  \
-        else                                                                                                               \
-            hipLaunchKernelGGL((k_vec_ad_down<T, RK, false>), grid, dim3(256), 0, s, rows, (const T *)x, ld_x, m, mask, part, part_stride, rp, per); \
+void AdLaunch<T>::down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
+                       int64_t part_stride, int rp, int waves, int slabs, int per, float *keep, hipStream_t s) {
+    const dim3 grid = ad_grid(rows, slabs, 64 * waves);
+    const size_t lds = (size_t)waves * 4096;
+#define GO2(RK, M)                                                                                                         \
+    hipLaunchKernelGGL((k_vec_ad_down<T, RK, M>), grid, dim3(64 * waves), lds, s, rows, (const T *)x, ld_x, m, scales, factor, mask, part, part_stride, rp, slabs, \
+                       per, keep)
+#define GO(RK)                           \
+    do {                                 \
+        if (mask.threshold) GO2(RK, true); \
+        else GO2(RK, false);             \
     } while (0)
     if (m.rank <= 16) GO(1);
     else if (m.rank <= 32) GO(2);
     else if (m.rank <= 64) GO(4);
     else GO(8);
 #undef GO
+#undef GO2
 }
 
 template <class T>
 void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                     const VecMask &mask, float *keep, int column_blocks, hipStream_t s) {
-    const dim3 grid = ad_grid(rows, column_blocks);
+                     const VecMask &mask, int column_blocks, float *keep, hipStream_t s) {
+    const dim3 grid = ad_grid(rows, column_blocks, 256);
     const size_t lds = (size_t)((m.rank + 31) / 32) * ((rows.tp + 15) / 16) * AdWide<T>::parts * 1024;
-#define GO(Y, M, ONE)                                                                                                      \
-    hipLaunchKernelGGL((k_vec_ad_up<T, Y, M, ONE>), grid, dim3(256), lds, s, rows, f, m, (const Y *)base, ld_base, (Y *)y, ld_y, mask, keep)
+#define GO(Y, M, ONE, E)                                                                                                   \
+    hipLaunchKernelGGL((k_vec_ad_up<T, Y, M, ONE, E>), grid, dim3(256), lds, s, rows, f, m, (const Y *)base, ld_base, (Y *)y, ld_y, mask, column_blocks, keep)
 #define GO2(Y, M)                                                                                                          \
     do {                                                                                                                   \
-        if (m.rank <= 32) GO(Y, M, true);                                                                                  \
-        else GO(Y, M, false);                                                                                              \
+        if (m.d < AD_COLS(T)) GO(Y, M, false, 1);                                                                          \
+        else if (m.rank <= 32) GO(Y, M, true, AD_COLS(T));                                                                 \
+        else GO(Y, M, false, AD_COLS(T));                                                                                              \
     } while (0)
     if (mask.threshold) GO2(T, true);  // (a gradient of x, which is of its type)
     else if (narrow) GO2(T, false);
@@ -60,16 +65,19 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
 template <class T>
 void AdLaunch<T>::outer(const AdRows &rows, int len, const AdFactor &f, int rank, const void *x, int64_t ld_x, int d, const VecMask &mask, const AdOuter &o,
                         bool narrow, hipStream_t s) {
-    constexpr int cols = 64 * AD_COLS(T);
-    const unsigned chunks = (unsigned)((rows.n + len - 1) / len), cb = (unsigned)((d + cols - 1) / cols);
-#define GO(O, RK, M)                                                                                                       \
-    hipLaunchKernelGGL((k_vec_ad_outer<T, O, RK, M>), dim3(chunks, cb, (unsigned)((rank + 16 * RK - 1) / (16 * RK))), dim3(256), 0, s, rows, len, f, \
-                       rank, (const T *)x, ld_x, d, mask, o)
+    const int cb = ad_outer_blocks(d);
+    dim3 grid = vec_grid((rows.n + len - 1) / len * cb, 256);
+#define GO(O, RK, M, E)                                                                                                    \
+    do {                                                                                                                   \
+        grid.z = (unsigned)((rank + 16 * RK - 1) / (16 * RK));                                                             \
+        hipLaunchKernelGGL((k_vec_ad_outer<T, O, RK, M, E>), grid, dim3(256), 0, s, rows, len, f, rank, (const T *)x, ld_x, d, mask, o, cb); \
+    } while (0)
 #define GO2(O, M)                                                                                                          \
     do {                                                                                                                   \
-        if (rank <= 16) GO(O, 1, M);                                                                                       \
-        else if (rank <= 32) GO(O, 2, M);                                                                                  \
-        else GO(O, 4, M);                                                                                                  \
+        if (d < 4) GO(O, 1, M, 1);                                                                                         \
+        else if (rank <= 16) GO(O, 1, M, 4);                                                                               \
+        else if (rank <= 32) GO(O, 2, M, 4);                                                                               \
+        else GO(O, 4, M, 4);                                                                                                  \
     } while (0)
     if (mask.threshold) {
         if (narrow) GO2(T, true);

@@ -377,12 +377,9 @@ def test_rows_beyond_32_bits(qb):
     y, _ = qb.vec_adapter(x, a, b, ids, out=(torch.empty_like(x), None))
     rest = torch.ones(n, dtype=torch.bool, device=dev())
     rest[rows] = False
-    for at in [rows, *(((ids == e) & rest).nonzero()[:1, 0] for e in range(3))]:  # (calls of other sizes may add up in another order: not the same bits)
+    for at in [rows, *(((ids == e) & rest).nonzero()[::3000, 0] for e in range(3))]:  # (sums are within their roundings; other places may add up in another order)
         y64, ty, _, _ = forward64(x[at], a, b, ids[at], None, None, 0.0)
         close(y[at], y64, ty + half_step(y64, BF16))
-    for e in range(3):
-        at = ((ids == e) & rest).nonzero()[::1000, 0]
-        assert bool((y[at] == y[at[0]]).all())
     del y
     big = torch.zeros((70, 64, 1 << 20), dtype=BF16, device=dev())
     big[69, 63] = 1.0
