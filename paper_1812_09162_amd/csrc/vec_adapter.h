@@ -278,10 +278,14 @@ __device__ __forceinline__ int ad_list(uint64_t bits, uint32_t row, uint32_t *li
 
 // -------------------------------------------------------------------- down --
 // part[slab][row][rank] = by the sum over the slab's columns of (kept) x_row W_e^T, rows padded to `rp` ranks, with zeros.  A block takes a
-// tile of positions and a slab of columns (one slab unless there are few rows); its waves (4 or 8) take turns at 32 columns each and join their sums
-// through LDS.  W's rows are the instruction's first factor, so that a lane holds four neighbouring ranks of a row.  Rows of x go to registers as the matrix
-// cores want them, without LDS.  Neighbouring blocks begin at different columns: rows are often a multiple of 4 KB apart, and blocks that read the same columns of
-// their rows at the same time would ask few of the memory's channels.
+// tile of positions and a slab of columns (one slab unless there are few rows); its waves take turns at 128 bytes of the rows each and join their sums
+// through LDS.  W's rows are the instruction's first factor, so that a lane holds four neighbouring ranks of a row.
+//
+// Eight neighbouring lanes read 128 bytes of a row, sixteen bytes each, and pass them through LDS to the lanes that the matrix cores want them in (rows of 128 bytes whose
+// sixteen-byte pieces are exchanged by the row's number, so that neither side meets bank conflicts); read directly in that order, neighbouring lanes
+// would hold different rows, and the L1 cache take four times the accesses: 16,384 x 4096 bf16 at rank 16 44 us, 40 this way (134 MB, the rate of
+// a cold read); 4096 x 2048 at rank 64 24 and 15.  Neighbouring blocks begin at different columns: rows are
+// often a multiple of 4 KB apart, and blocks that read the same columns at the same time would ask few of the memory's channels.
 #define AD_DOWN_WAVES 8
 // (rows without an adapter)
 __device__ __forceinline__ void ad_zeros(uint64_t bits, uint32_t row, uint32_t *list, int rank, float *__restrict__ keep) {
@@ -290,64 +294,106 @@ __device__ __forceinline__ void ad_zeros(uint64_t bits, uint32_t row, uint32_t *
     for (int i = threadIdx.x; i < count * rank; i += blockDim.x) keep[(int64_t)list[i / rank] * rank + i % rank] = 0.0f;
     __builtin_amdgcn_wave_barrier();
 }
+// where the sixteen-byte piece p of row r lies
+__device__ __forceinline__ int ad_slot(int r, int p) { return r * 8 + (p ^ (r >> 1 & 7)); }
+
 template <class T, int RK, int NT, bool MASK>
 __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ w, int64_t ld_w, int d, int kb, int ke, int turn, int rank, int j0, float by,
-                                        const uint32_t *list, int count, const VecMask &mask, VecKey key, vec_f4 *red, float *__restrict__ part, int rp,
+                                        const uint32_t *list, int count, const VecMask &mask, VecKey key, ad_u4 *lds, float *__restrict__ part, int rp,
                                         float *__restrict__ keep) {
-    constexpr int U = sizeof(T) == 4 || NT * RK > 8 ? 1 : 2;  // steps on their way
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, c = lane & 15, g = lane >> 4;
-    const T *xp[NT], *wp[RK];
-    uint32_t row[NT];
-    // (lanes without a row or a rank read another's: what they give is not stored)
+    constexpr int E = AD_COLS(T), COLS = 8 * E, KS = COLS / 32, N = NT + RK;  // columns of a piece and of a turn; instructions' worth; tiles
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, c = lane & 15, g = lane >> 4, lr = lane >> 3, lp = lane & 7;
+    ad_u4 *mine = lds + wave * N * 128;  // [tile][16 rows][8 pieces]
+    // (rows without a position and ranks behind the last read another's: what they give is not stored)
+    const T *from[N][2];
+    uint32_t row[NT][2];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        row[t] = list[16 * t + c < count ? 16 * t + c : 0];
-        xp[t] = x + (int64_t)row[t] * ld_x;
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int i = 16 * t + 8 * h + lr;
+            row[t][h] = list[i < count ? i : 0];
+            from[t][h] = x + (int64_t)row[t][h] * ld_x;
+        }
+#pragma unroll
+        for (int j = 0; j < RK; ++j) {
+            const int i = j0 + 16 * j + 8 * h + lr;
+            from[NT + j][h] = w + (int64_t)(i < rank ? i : rank - 1) * ld_w;
+        }
     }
-#pragma unroll
-    for (int j = 0; j < RK; ++j) wp[j] = w + (int64_t)(j0 + 16 * j + c < rank ? j0 + 16 * j + c : rank - 1) * ld_w;
     vec_f4 acc[NT][RK];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int j = 0; j < RK; ++j) acc[t][j] = (vec_f4)0.0f;
-    auto step = [&](vec_pack<T> *xv, const vec_pack<T> *wv, int k) {
+    vec_pack<T, E> v[N][2];
+    auto put = [&](int col) {  // (col: the lane's)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (MASK) xv[t] = vec_drop<T>(xv[t], vec_kept(vec_random(key, mask.layer, row[t], (uint32_t)k >> 3), mask.threshold));
+        for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int j = 0; j < RK; ++j) acc[t][j] = ad_mul<T>(wv[j], xv[t], acc[t][j]);
+            for (int h = 0; h < 2; ++h) {
+                vec_pack<T, E> o = v[t][h];
+                if (MASK && t < NT) o = ad_drop<T, E>(o, ad_bits(key, mask, row[t < NT ? t : 0][h], (uint32_t)col >> 3) >> (E == 4 ? col & 4 : 0));
+                mine[t * 128 + ad_slot(8 * h + lr, lp)] = __builtin_bit_cast(ad_u4, o);
+            }
+    };
+    auto multiply = [&]() {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            auto operand = [&](int t) {
+                const ad_u4 *at = mine + t * 128;
+                if constexpr (sizeof(T) == 2) {
+                    return __builtin_bit_cast(vec_pack<T>, at[ad_slot(c, 4 * ks + g)]);
+                } else {
+                    vec_pack<T> o;
+                    const vec_f4 lo = __builtin_bit_cast(vec_f4, at[ad_slot(c, 2 * g)]), hi = __builtin_bit_cast(vec_f4, at[ad_slot(c, 2 * g + 1)]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = lo[i], o[4 + i] = hi[i];
+                    return o;
+                }
+            };
+            vec_pack<T> wv[RK];
+#pragma unroll
+            for (int j = 0; j < RK; ++j) wv[j] = operand(NT + j);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const vec_pack<T> xv = operand(t);
+#pragma unroll
+                for (int j = 0; j < RK; ++j) acc[t][j] = ad_mul<T>(wv[j], xv, acc[t][j]);
+            }
         }
     };
-    const int span = waves * 32 * U, whole = ((ke < d ? ke : d / 32 * 32) - kb) / span;  // turns whose columns are all there
+    const int span = waves * COLS, whole = ((ke < d ? ke : d / COLS * COLS) - kb) / span;  // turns whose columns are all there
     if (whole > 0) {
         turn %= whole;
+        int col = kb + turn * span + COLS * wave + E * lp;
+        auto request = [&]() {
+#pragma unroll
+            for (int t = 0; t < N; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) v[t][h] = ad_load<T, E>(from[t][h], col);
+        };
+        request();
         for (int i = 0; i < whole; ++i) {
-            const int k = kb + turn * span + 32 * wave + 8 * g;
+            put(col);
             if (++turn == whole) turn = 0;
-            vec_pack<T> xv[U][NT], wv[U][RK];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) xv[u][t] = *(const vec_pack<T> *)(xp[t] + k + waves * 32 * u);
-#pragma unroll
-                for (int j = 0; j < RK; ++j) wv[u][j] = *(const vec_pack<T> *)(wp[j] + k + waves * 32 * u);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) step(xv[u], wv[u], k + waves * 32 * u);
+            col = kb + turn * span + COLS * wave + E * lp;
+            if (i + 1 < whole) request();
+            multiply();
         }
     }
-    for (int k = kb + whole * span + 32 * wave; k < ke; k += waves * 32) {
-        vec_pack<T> xv[NT], wv[RK];
-        const int col = k + 8 * g;
+    for (int k = kb + whole * span + COLS * wave; k < ke; k += span) {
+        const int col = k + E * lp;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) xv[t] = vec_load(xp[t] + (col < d ? col : 0), d - col, col);
+        for (int t = 0; t < N; ++t)
 #pragma unroll
-        for (int j = 0; j < RK; ++j) wv[j] = vec_load(wp[j] + (col < d ? col : 0), d - col, col);
-        step(xv, wv, col);
+            for (int h = 0; h < 2; ++h) v[t][h] = vec_load<T, E>(from[t][h] + (col < d ? col : 0), d - col, col);
+        put(col);
+        multiply();
     }
     // sums of the waves, G pairs of tiles a round
     constexpr int G = NT * RK < 4 ? NT * RK : 4;
+    vec_f4 *red = (vec_f4 *)lds;
 #pragma unroll
     for (int p0 = 0; p0 < NT * RK; p0 += G) {
         __syncthreads();
@@ -359,21 +405,22 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
             const int at = 16 * (q / RK) + (l & 15), to = j0 + 16 * (q % RK) + 4 * (l >> 4);
             if (at >= count || to >= rp) continue;
             vec_f4 s = red[i];
-            for (int v = 1; v < waves; ++v) s += red[v * G * 64 + i];
+            for (int u = 1; u < waves; ++u) s += red[u * G * 64 + i];
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[r] = to + r < rank ? s[r] * by : 0.0f;
             *(vec_f4 *)(part + (int64_t)list[at] * rp + to) = s;
             if (keep) vec_store<float, 4>(keep + (int64_t)list[at] * rank + to, rank - to, s);
         }
     }
+    __syncthreads();
 }
 
 template <class T, int RK, bool MASK>
-__global__ void __launch_bounds__(64 * AD_DOWN_WAVES)
+__global__ void __launch_bounds__(64 * (RK == 8 ? 4 : AD_DOWN_WAVES))
 k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, const float *__restrict__ scales, float factor, VecMask mask, float *__restrict__ part,
               int64_t part_stride, int rp, int slabs, int per, float *__restrict__ keep) {
     __shared__ uint32_t lists[AD_DOWN_WAVES][64];
-    extern __shared__ __align__(16) unsigned char smem[];  // [waves][4][64] sums
+    extern __shared__ __align__(16) unsigned char smem[];  // [waves][tiles of x and W][128] pieces of sixteen bytes; [waves][4][64] sums
     const int lane = threadIdx.x & 63;
     uint32_t *list = lists[threadIdx.x >> 6];
     const int64_t block = vec_block(), at = slabs == 1 ? block : block / slabs;
@@ -393,7 +440,7 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, co
         const T *w = (const T *)m.p + e * m.stride;
         const float by = scales ? scales[e] * factor : factor;
         for (int j0 = 0; j0 < m.rank; j0 += 16 * RK) {
-#define GO(NT) ad_down<T, RK, NT, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, (int)(at & 0xffff), m.rank, j0, by, list, count, mask, key, (vec_f4 *)smem, part, rp, keep)
+#define GO(NT) ad_down<T, RK, NT, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, (int)(at & 0xffff), m.rank, j0, by, list, count, mask, key, (ad_u4 *)smem, part, rp, keep)
             if (RK <= 2 && count > 32) GO(RK <= 2 ? 4 : 1);
             else if (count > 16) GO(2);
             else GO(1);
@@ -405,43 +452,66 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, co
 // ---------------------------------------------------------------------- up --
 // y_row = base_row + (kept) f_row W_e.  A block takes a tile of positions and 64 AD_COLS columns at a time, a quarter a wave.  The factor f is made ready
 // in LDS once (its parts as the matrix cores take them); a lane reads eight ranks of AD_COLS columns of W, whose columns are put together from
-// their halves by byte permutations.  Lane c reads column group 4 (c % 4) + c / 4, so that the four lanes of a row hold neighbouring groups of the result.
+// their halves by byte permutations.  The products' 16 rows pass through LDS, so that sixteen neighbouring lanes read and write a row's 256 bytes: from
+// the matrix cores' own order, where neighbouring lanes hold different rows, every sixteen bytes would be an access of their own (16,384 x 4096 bf16 at rank 16 60 us, 53
+// this way: 268 MB, the rate of a large copy).
 template <class T, class Y, bool MASK, int E>
 struct AdUp {
+    static constexpr int LD = 16 * E + 4;  // floats between two rows in LDS (lanes of a quarter wave then write to different banks)
     const Y *base;
     Y *y;
     int64_t ld_base, ld_y;
     int d;
     VecMask mask;
     VecKey key;
+    float *lds;  // the wave's own [16][LD]
 
-    // a lane's groups 4 i + lane / 16 of a row
-    __device__ __forceinline__ void read(vec_pack<Y, E> *b, uint32_t row, int c0) const {
-        const int g = (threadIdx.x & 63) >> 4;
+    // a lane's part of four rows: row 4 i + lane / 16, columns c0 + E (lane % 16) and on
+    __device__ __forceinline__ int column(int c0) const { return c0 + E * (threadIdx.x & 15); }
+    __device__ __forceinline__ void read(vec_pack<Y, E> *b, const uint32_t *rows, int c0) const {
         if (!base) return;
-        const Y *p = base + (int64_t)row * ld_base;
+        const int from = ad_from<E>(column(c0), d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) b[i] = ad_load<Y, E>(p, ad_from<E>(c0 + E * (4 * i + g), d));
+        for (int i = 0; i < 4; ++i) b[i] = ad_load<Y, E>(base + (int64_t)rows[i] * ld_base, from);
     }
-    __device__ __forceinline__ void write(const vec_f4 *acc, const vec_pack<Y, E> *b, uint32_t row, int c0) const {  // acc[m]: column m of each
-        const int g = (threadIdx.x & 63) >> 4;
-        Y *p = y + (int64_t)row * ld_y;
+    // acc[m][i]: of row lane % 16, column E (4 (lane / 16) + i) + m
+    __device__ __forceinline__ void write(const vec_f4 *acc, const vec_pack<Y, E> *b, const uint32_t *rows, int left, int c0) const {
+        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, col = column(c0);
+        float *to = lds + c * LD + 4 * E * g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int col = c0 + E * (4 * i + g);
-            if (col >= d) continue;
-            vec_f<E> f;
+            if constexpr (E == 1) {
+                to[i] = acc[0][i];
+            } else {
 #pragma unroll
-            for (int m = 0; m < E; ++m) f[m] = acc[m][i];
+                for (int m = 0; m < E; m += 4) *(vec_f4 *)(to + E * i + m) = (vec_f4){acc[m][i], acc[m + 1][i], acc[m + 2][i], acc[m + 3][i]};
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vec_f<E> f;
+            const float *at = lds + (4 * i + g) * LD + E * c;
+            if constexpr (E == 1) {
+                f[0] = at[0];
+            } else {
+#pragma unroll
+                for (int m = 0; m < E; m += 4) {
+                    const vec_f4 u = *(const vec_f4 *)(at + m);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) f[m + k] = u[k];
+                }
+            }
+            if (4 * i + g >= left || col >= d) continue;
             if (MASK) {
-                const uint32_t kept = ad_kept<E>(key, mask, row, ad_from<E>(col, d));
+                const uint32_t kept = ad_kept<E>(key, mask, rows[i], ad_from<E>(col, d));
 #pragma unroll
                 for (int m = 0; m < E; ++m) f[m] = kept >> m & 1 ? f[m] : 0.0f;
             }
             if (base) f += vec_wide<Y, E>(b[i]);
-            ad_store<Y, E>(p, col, d, f);
-            __builtin_amdgcn_sched_barrier(0);  // (a group after the other: together they take registers that a third wave needs)
+            ad_store<Y, E>(y + (int64_t)rows[i] * ld_y, col, d, f);
         }
+        __builtin_amdgcn_wave_barrier();
     }
 };
 
@@ -484,27 +554,30 @@ struct AdUpPass {
     int count, chunks, c0;
     vec_pack<T, E> raw[8];
     vec_pack<Y, E> b[4];
+    uint32_t at[4];  // the rows of b
 
     // (lanes without a rank read the last one's: their part of the factor is zero)
     __device__ __forceinline__ void weights(int kc) {
-        const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, from = ad_from<E>(c0 + E * (4 * (c & 3) + (c >> 2)), m.d);
+        const int g = (threadIdx.x & 63) >> 4, from = ad_from<E>(up.column(c0), m.d);
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             const int r = 32 * kc + 8 * g + q;
             raw[q] = ad_load<T, E>(w + (int64_t)(r < m.rank ? r : m.rank - 1) * m.ld, from);
         }
     }
-    __device__ __forceinline__ uint32_t row(int t) const {
-        const int i = 16 * t + (threadIdx.x & 15);
-        return list[i < count ? i : 0];
+    __device__ __forceinline__ void rows(int t, uint32_t *to) const {
+        const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = list[16 * t + 4 * i + g < count ? 16 * t + 4 * i + g : 0];
     }
     __device__ __forceinline__ void request(int from) {
         c0 = from;
         if (w) weights(0);
-        up.read(b, row(0), c0);
+        rows(0, at);
+        up.read(b, at, c0);
     }
     __device__ __forceinline__ void run(const ad_u4 *ready) {
-        const int lane = threadIdx.x & 63, c = lane & 15, tiles = (count + 15) / 16;
+        const int lane = threadIdx.x & 63, tiles = (count + 15) / 16;
         auto factor = [&](int kc, int t) {
             AdWide<T> o;
 #pragma unroll
@@ -514,7 +587,11 @@ struct AdUpPass {
         if constexpr (ONE) {
             for (int t = 0; t < tiles; ++t) {
                 vec_pack<Y, E> next[4];
-                if (t + 1 < tiles) up.read(next, row(t + 1), c0);
+                uint32_t then[4];
+                if (t + 1 < tiles) {
+                    rows(t + 1, then);
+                    up.read(next, then, c0);
+                }
                 vec_f4 acc[E];
 #pragma unroll
                 for (int i = 0; i < E; ++i) acc[i] = (vec_f4)0.0f;
@@ -529,9 +606,9 @@ struct AdUpPass {
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-                if (16 * t + c < count) up.write(acc, b, row(t), c0);
+                up.write(acc, b, at, count - 16 * t, c0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = next[i];
+                for (int i = 0; i < 4; ++i) b[i] = next[i], at[i] = then[i];
             }
         } else {  // (tiles of at most 32 positions)
             vec_f4 acc[2][E];
@@ -551,9 +628,12 @@ struct AdUpPass {
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (c < count) up.write(acc[0], b, row(0), c0);
-            if (tiles > 1) up.read(b, row(1), c0);
-            if (16 + c < count) up.write(acc[1], b, row(1), c0);
+            up.write(acc[0], b, at, count, c0);
+            if (tiles > 1) {
+                rows(1, at);
+                up.read(b, at, c0);
+                up.write(acc[1], b, at, count - 16, c0);
+            }
         }
     }
 };
@@ -570,7 +650,8 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
     const int first = (int)(block - at * column_blocks) * 64 * E + wave * 16 * E, step = column_blocks * 64 * E;
     const AdTile tile = ad_tile(rows, at, lane);
     const int chunks = ONE ? 1 : (m.rank + 31) / 32;
-    AdUp<T, Y, MASK, E> up = {base, y, ld_base, ld_y, m.d, mask, {0, 0, 0}};
+    __shared__ __align__(16) float out[4][16 * AdUp<T, Y, MASK, E>::LD];
+    AdUp<T, Y, MASK, E> up = {base, y, ld_base, ld_y, m.d, mask, {0, 0, 0}, out[wave]};
     if (MASK) up.key = vec_key(mask);
     if (block != at * column_blocks) keep = nullptr;  // (a tile's first block writes it)
     if (keep) ad_zeros(__ballot(tile.in && tile.id == rows.adapters), tile.row, list, m.rank, keep);

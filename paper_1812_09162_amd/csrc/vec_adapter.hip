@@ -37,7 +37,7 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     p.rp = (rank + 15) & ~15;
     const int d = grad ? dout : din;
     const int64_t tiles = (n + p.tp - 1) / p.tp;
-    p.waves = d >= 1024 ? 8 : 4;
+    p.waves = d >= 1024 && rank <= 64 ? 8 : 4;
     int64_t slabs = tiles * p.waves >= 1024 ? 1 : 1024 / (tiles * p.waves);
     if (slabs > d / (p.waves * 64)) slabs = d / (p.waves * 64);
     if (slabs > AD_MAX_SLABS) slabs = AD_MAX_SLABS;

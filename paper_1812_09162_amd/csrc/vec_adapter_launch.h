@@ -25,10 +25,17 @@ template <class T>
 void AdLaunch<T>::down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
                        int64_t part_stride, int rp, int waves, int slabs, int per, float *keep, hipStream_t s) {
     const dim3 grid = ad_grid(rows, slabs, 64 * waves);
-    const size_t lds = (size_t)waves * 4096;
+    // tiles of x and W, and at least the sums' four
+    auto lds = [&](int rk) {
+        const int nt = rows.tp > 32 ? 4 : (rows.tp > 16 ? 2 : 1), tiles = nt + rk > 2 ? nt + rk : 2;
+        return (size_t)waves * tiles * 2048;
+    };
 #define GO2(RK, M)                                                                                                         \
-    hipLaunchKernelGGL((k_vec_ad_down<T, RK, M>), grid, dim3(64 * waves), lds, s, rows, (const T *)x, ld_x, m, scales, factor, mask, part, part_stride, rp, slabs, \
-                       per, keep)
+    do {                                                                                                                   \
+        void (*const k)(AdRows, const T *, int64_t, AdMatrix, const float *, float, VecMask, float *, int64_t, int, int, int, float *) = &k_vec_ad_down<T, RK, M>; \
+        if (lds(RK) > 65536) (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds(RK)); \
+        hipLaunchKernelGGL(k, grid, dim3(64 * waves), lds(RK), s, rows, (const T *)x, ld_x, m, scales, factor, mask, part, part_stride, rp, slabs, per, keep); \
+    } while (0)
 #define GO(RK)                           \
     do {                                 \
         if (mask.threshold) GO2(RK, true); \
