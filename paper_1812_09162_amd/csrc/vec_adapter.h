@@ -279,7 +279,7 @@ __device__ __forceinline__ int ad_list(uint64_t bits, uint32_t row, uint32_t *li
 // -------------------------------------------------------------------- down --
 // part[slab][row][rank] = by the sum over the slab's columns of (kept) x_row W_e^T, rows padded to `rp` ranks, with zeros.  A block takes a
 // tile of positions and a slab of columns (one slab unless there are few rows); its waves take turns at 128 bytes of the rows each and join their sums
-// through LDS.  W's rows are the instruction's first factor, so that a lane holds four neighbouring ranks of a row.
+// through LDS, or, where adapters have few rows, take an adapter of the tile each (`own`), without a wait.  W's rows are the instruction's first factor, so that a lane holds four neighbouring ranks of a row.
 //
 // Eight neighbouring lanes read 128 bytes of a row, sixteen bytes each, and pass them through LDS to the lanes that the matrix cores want them in (rows of 128 bytes whose
 // sixteen-byte pieces are exchanged by the row's number, so that neither side meets bank conflicts); read directly in that order, neighbouring lanes
@@ -299,10 +299,10 @@ __device__ __forceinline__ int ad_slot(int r, int p) { return r * 8 + (p ^ (r >>
 
 template <class T, int RK, int NT, bool MASK>
 __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, const T *__restrict__ w, int64_t ld_w, int d, int kb, int ke, int turn, int rank, int j0, float by,
-                                        const uint32_t *list, int count, const VecMask &mask, VecKey key, ad_u4 *lds, float *__restrict__ part, int rp,
+                                        const uint32_t *list, int count, const VecMask &mask, VecKey key, ad_u4 *lds, int wave, int waves, float *__restrict__ part, int rp,
                                         float *__restrict__ keep) {
     constexpr int E = AD_COLS(T), COLS = 8 * E, KS = COLS / 32, N = NT + RK;  // columns of a piece and of a turn; instructions' worth; tiles
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, c = lane & 15, g = lane >> 4, lr = lane >> 3, lp = lane & 7;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, lr = lane >> 3, lp = lane & 7;
     ad_u4 *mine = lds + wave * N * 128;  // [tile][16 rows][8 pieces]
     // (rows without a position and ranks behind the last read another's: what they give is not stored)
     const T *from[N][2];
@@ -363,10 +363,11 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
             }
         }
     };
-    const int span = waves * COLS, whole = ((ke < d ? ke : d / COLS * COLS) - kb) / span;  // turns whose columns are all there
+    const int span = waves * COLS, first = kb + COLS * wave, end = ke < d ? ke : d;
+    const int whole = first + COLS <= end ? (end - first - COLS) / span + 1 : 0;  // the wave's turns whose columns are all there
     if (whole > 0) {
         turn %= whole;
-        int col = kb + turn * span + COLS * wave + E * lp;
+        int col = first + turn * span + E * lp;
         auto request = [&]() {
 #pragma unroll
             for (int t = 0; t < N; ++t)
@@ -377,19 +378,33 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
         for (int i = 0; i < whole; ++i) {
             put(col);
             if (++turn == whole) turn = 0;
-            col = kb + turn * span + COLS * wave + E * lp;
+            col = first + turn * span + E * lp;
             if (i + 1 < whole) request();
             multiply();
         }
     }
-    for (int k = kb + whole * span + COLS * wave; k < ke; k += span) {
-        const int col = k + E * lp;
+    if (first + whole * span < end) {
+        const int col = first + whole * span + E * lp;
 #pragma unroll
         for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[t][h] = vec_load<T, E>(from[t][h] + (col < d ? col : 0), d - col, col);
+            for (int h = 0; h < 2; ++h) v[t][h] = vec_load<T, E>(from[t][h] + (col < end ? col : 0), end - col, col);
         put(col);
         multiply();
+    }
+    auto store = [&](vec_f4 s, int at, int to) {  // ranks to .. + 3 of a row
+        if (at >= count || to >= rp) return;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = to + r < rank ? s[r] * by : 0.0f;
+        *(vec_f4 *)(part + (int64_t)list[at] * rp + to) = s;
+        if (keep) vec_store<float, 4>(keep + (int64_t)list[at] * rank + to, rank - to, s);
+    };
+    if (waves == 1) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < RK; ++j) store(acc[t][j], 16 * t + c, j0 + 16 * j + 4 * g);
+        return;
     }
     // sums of the waves, G pairs of tiles a round
     constexpr int G = NT * RK < 4 ? NT * RK : 4;
@@ -402,14 +417,9 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
         __syncthreads();
         for (int i = threadIdx.x; i < G * 64; i += blockDim.x) {
             const int l = i & 63, q = p0 + (i >> 6);
-            const int at = 16 * (q / RK) + (l & 15), to = j0 + 16 * (q % RK) + 4 * (l >> 4);
-            if (at >= count || to >= rp) continue;
             vec_f4 s = red[i];
             for (int u = 1; u < waves; ++u) s += red[u * G * 64 + i];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[r] = to + r < rank ? s[r] * by : 0.0f;
-            *(vec_f4 *)(part + (int64_t)list[at] * rp + to) = s;
-            if (keep) vec_store<float, 4>(keep + (int64_t)list[at] * rank + to, rank - to, s);
+            store(s, 16 * (q / RK) + (l & 15), j0 + 16 * (q % RK) + 4 * (l >> 4));
         }
     }
     __syncthreads();
@@ -418,11 +428,11 @@ __device__ __forceinline__ void ad_down(const T *__restrict__ x, int64_t ld_x, c
 template <class T, int RK, bool MASK>
 __global__ void __launch_bounds__(64 * (RK == 8 ? 4 : AD_DOWN_WAVES))
 k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, const float *__restrict__ scales, float factor, VecMask mask, float *__restrict__ part,
-              int64_t part_stride, int rp, int slabs, int per, float *__restrict__ keep) {
+              int64_t part_stride, int rp, int slabs, int per, int own, float *__restrict__ keep) {
     __shared__ uint32_t lists[AD_DOWN_WAVES][64];
     extern __shared__ __align__(16) unsigned char smem[];  // [waves][tiles of x and W][128] pieces of sixteen bytes; [waves][4][64] sums
-    const int lane = threadIdx.x & 63;
-    uint32_t *list = lists[threadIdx.x >> 6];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    uint32_t *list = lists[wave];
     const int64_t block = vec_block(), at = slabs == 1 ? block : block / slabs;
     const int slab = (int)(block - at * slabs);
     const AdTile tile = ad_tile(rows, at, lane);
@@ -432,15 +442,19 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, co
     part += slab * part_stride;
     if (keep) ad_zeros(__ballot(tile.in && tile.id == rows.adapters), tile.row, list, m.rank, keep);
     uint64_t todo = __ballot(tile.id < rows.adapters);
-    while (todo) {
+    for (int i = 0; todo; ++i) {
         const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
         const uint64_t bits = __ballot(tile.id == e);
         todo &= ~bits;
+        if (own && i % waves != wave) continue;
         const int count = ad_list(bits, tile.row, list, lane);
         const T *w = (const T *)m.p + e * m.stride;
         const float by = scales ? scales[e] * factor : factor;
         for (int j0 = 0; j0 < m.rank; j0 += 16 * RK) {
-#define GO(NT) ad_down<T, RK, NT, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, (int)(at & 0xffff), m.rank, j0, by, list, count, mask, key, (ad_u4 *)smem, part, rp, keep)
+            // (its own wave: LDS and columns as a block of one)
+#define GO(NT)                                                                                                                                          \
+    ad_down<T, RK, NT, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, (int)(at & 0xffff), m.rank, j0, by, list, count, mask, key,                                 \
+                             (ad_u4 *)smem + (own ? wave * (NT + RK) * 128 : 0), own ? 0 : wave, own ? 1 : waves, part, rp, keep)
             if (RK <= 2 && count > 32) GO(RK <= 2 ? 4 : 1);
             else if (count > 16) GO(2);
             else GO(1);
@@ -679,6 +693,107 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
     }
 }
 
+// The same for few rows of an adapter: on the vector units, without a wait between waves.  A wave takes a tile of at most eight positions and 64 E columns, E a lane;
+// four rows of one adapter share what it reads of W.  Where a tile of the matrix cores would hold three rows of sixteen, the rest of the form above (the parts of the
+// factor, columns put together, LDS) costs more than these products: ABOVE us where this takes FEW.
+#define AD_FEW_POSITIONS 8
+template <class T, class Y, bool MASK, int E>
+__global__ void __launch_bounds__(256, 2)
+k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t f_stride, int f_slabs, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y,
+                VecMask mask, int column_blocks, float *__restrict__ keep) {
+    const int lane = threadIdx.x & 63;
+    const int64_t item = vec_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = item / column_blocks;
+    if (at * rows.tp >= rows.n) return;
+    const int slab = (int)(item - at * column_blocks), col = slab * 64 * E + E * lane, from = ad_from<E>(col, m.d);
+    const AdTile tile = ad_tile(rows, at, lane);
+    VecKey key = {0, 0, 0};
+    if (MASK) key = vec_key(mask);
+    uint64_t todo = __ballot(tile.in);
+    while (todo) {
+        const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
+        const uint64_t bits = __ballot(tile.in && tile.id == e);
+        const bool none = e == rows.adapters;
+        const T *w = (const T *)m.p + (none ? 0 : e * m.stride) + from;
+        // the first four rows of e
+        int row[4], count = 0;
+        uint64_t mine = todo & bits;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            count += mine != 0;
+            row[k] = __builtin_amdgcn_readlane((int)tile.row, mine ? __builtin_ctzll(mine) : __builtin_ctzll(bits));
+            todo &= ~(mine & -mine);
+            mine &= mine - 1;
+        }
+        vec_f<E> acc[4];
+        vec_pack<Y, E> b[4];
+        if (base && !(none && base == y))
+#pragma unroll
+            for (int k = 0; k < 4; ++k) b[k] = ad_load<Y, E>(base + (uint32_t)row[k] * ld_base, from);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] = (vec_f<E>)0.0f;
+        for (int r64 = 0; r64 < m.rank; r64 += 64) {
+            if (none && !(keep && slab == 0)) break;
+            vec_pack<T, E> raw[8];
+            auto request = [&](int r0) {  // (behind the last rank that one again, beside zeros of the factor)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) raw[q] = *(const vec_pack<T, E> *)(w + (int64_t)(r0 + q < m.rank ? r0 + q : m.rank - 1) * m.ld);
+            };
+            if (!none) request(r64);
+            // a lane has one rank of the factor, the sum of its parts
+            float t[4] = {};
+            const int r = r64 + lane;
+            if (!none && r < ld_f) {
+                for (int s = 0; s < f_slabs; s += 4) {  // four on their way
+                    float part[4][4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) part[k][u] = k < count ? f[(s + u < f_slabs ? s + u : s) * f_stride + (uint32_t)row[k] * ld_f + r] : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) t[k] += s + u < f_slabs ? part[k][u] : 0.0f;
+                }
+            }
+            if (keep && slab == 0 && r < m.rank)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k < count) keep[(int64_t)row[k] * m.rank + r] = t[k];
+            if (none) continue;
+            for (int r0 = 0; r0 < 64 && r64 + r0 < m.rank; r0 += 8) {
+                vec_pack<T, E> here[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) here[q] = raw[q];
+                if (r0 + 8 < 64 && r64 + r0 + 8 < m.rank) request(r64 + r0 + 8);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const vec_f<E> v = vec_wide<T, E>(here[q]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < count) {
+                            const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(t[k]), r0 + q));
+#pragma unroll
+                            for (int i = 0; i < E; ++i) acc[k][i] = __fmaf_rn(by, v[i], acc[k][i]);
+                        }
+                }
+            }
+        }
+        if (none && base == y) continue;
+        if (col >= m.d) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k >= count) break;
+            if (MASK) {
+                const uint32_t kept = ad_kept<E>(key, mask, (uint32_t)row[k], from);
+#pragma unroll
+                for (int i = 0; i < E; ++i) acc[k][i] = kept >> i & 1 ? acc[k][i] : 0.0f;
+            }
+            if (base) acc[k] += vec_wide<Y, E>(b[k]);
+            ad_store<Y, E>(y + (uint32_t)row[k] * ld_y, col, m.d, acc[k]);
+        }
+    }
+}
+
 // ------------------------------------------------------------------- outer --
 // G_e[j][col] = sum over the rows of e of f_row[j] (kept) x_row[col].  A block takes `len` sorted positions and 64 AD_COLS columns, a quarter a wave, in steps of 32
 // positions whatever runs of equal ids these hold: the rows of a step are read once, and each run among them takes its own and zeros for the others.  Runs that lie within the block's positions are written; the others' sums go to part[chunk][0] (began before)
@@ -697,20 +812,37 @@ __device__ __forceinline__ void ad_put(O *row, int col, int d, vec_f<E> v, bool 
 }
 
 #define AD_MAX_LEN 1024  // positions of a block at most
+// Both gradients are one launch: db's blocks first, then da's, whose rows are masked.
 #define AD_MAX_LEN 1024  // positions of a block at most
+struct AdSide {
+    AdFactor f;
+    const void *x;
+    int64_t ld_x;
+    int d, len, column_blocks;  // len: positions of a block
+    AdOuter o;
+};
 template <class T, class O, int RK, bool MASK, int E>
 __global__ void __launch_bounds__(256, 2)
-k_vec_ad_outer(AdRows rows, int len, AdFactor f, int rank, const T *__restrict__ x, int64_t ld_x, int d, VecMask mask, AdOuter o, int column_blocks) {
+k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_t blocks_b) {
     constexpr int P = AdWide<T>::parts;
+    int64_t block = vec_block();
+    const bool masked = block >= blocks_b;
+    const AdSide &side = masked ? sa : sb;
+    if (masked) block -= blocks_b;
+    const AdFactor f = side.f;
+    const AdOuter o = side.o;
+    const T *__restrict__ const x = (const T *)side.x;
+    const int64_t ld_x = side.ld_x;
+    const int d = side.d, len = side.len, column_blocks = side.column_blocks;
     __shared__ ad_u4 ready[AD_STAGE / 32 * RK * P * 64];  // [step][16 ranks][part][lane]
     __shared__ uint32_t keys[AD_MAX_LEN], at[AD_MAX_LEN];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
-    const int64_t block = vec_block(), chunk = block / column_blocks, p0 = chunk * len;
+    const int64_t chunk = block / column_blocks, p0 = chunk * len;
     if (p0 >= rows.n) return;
     const int size = (int)(rows.n - p0 < len ? rows.n - p0 : len);
     const int c0 = ((int)(block - chunk * column_blocks) * 4 + wave) * 16 * E, col = c0 + E * (lane & 15), from = ad_from<E>(col, d), j0 = blockIdx.z * 16 * RK;
     VecKey key = {0, 0, 0};
-    if (MASK) key = vec_key(mask);
+    if (MASK && masked) key = vec_key(mask);
     int total = size;
     if (size > 0 && rows.keys[p0 + size - 1] >= (uint32_t)rows.adapters) {  // (rows without an adapter come last)
         total = 0;
@@ -767,7 +899,7 @@ k_vec_ad_outer(AdRows rows, int len, AdFactor f, int rank, const T *__restrict__
             const int here = s0 + 32 * st, behind = here + 32 < total ? here + 32 : total;
             vec_pack<T, E> next[8];
             if (here + 32 < total) request(next, here + 32);
-            if (MASK)
+            if (MASK && masked)
                 ad_drop8<T, E>(raw, key, mask, [&](int q) { return at[here + 8 * g + q < total ? here + 8 * g + q : total - 1]; }, from, whole);
             // the runs that the step holds, or parts of
             const uint32_t mine = keys[here + (lane & 31) < behind ? here + (lane & 31) : behind - 1];

@@ -7,19 +7,23 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 
 #define AD_FEW_ROWS 64  // rows that are not sorted
 #define AD_MAX_SLABS 16
+#define AD_OWN 32768    // rows an adapter times columns below which `down`'s waves take an adapter each
+#define AD_UP_FEW 256   // rows an adapter times ranks below which `up` runs on the vector units
 
 struct AdPlan {
     bool sorted, grouped;      // grouped: by k_vec_ad_group
-    int tp;                    // positions of a tile
+    bool few;                  // `up` on the vector units
+    int tp, tp_up;             // positions of a tile of `down`, of `up`
     int rp;                    // ranks of a row of partial sums
     int waves, slabs, per;     // of the contraction over columns
+    bool own;                  // its waves take an adapter each
     int len_a, len_b;          // positions of a piece of the sums over rows
     int dpad_a, dpad_b;
     size_t part, part_a, part_b, total;  // bytes from the workspace's start
 };
 
-static int ad_len(int64_t n, int d, int rank) {
-    const int64_t across = (int64_t)ad_outer_blocks(d) * ((rank + 63) / 64);
+static int ad_len(int64_t n, int d, int other, int rank) {
+    const int64_t across = (int64_t)ad_outer_blocks(d, other) * ((rank + 63) / 64);
     int len = AD_MAX_LEN;
     while (len > 64 && (n + len - 1) / len * across < 512) len /= 2;
     return len;
@@ -27,19 +31,31 @@ static int ad_len(int64_t n, int d, int rank) {
 
 static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int type, bool grad) {
     AdPlan p = {};
-    // half as many positions a tile as an adapter has rows on average: few tiles then hold more than two or three; and at least 256 tiles, if tiles of sixteen give them
+    // as many positions a tile as the adapters have rows on average, at most; at least 256 tiles, if tiles of sixteen give them
     const int64_t each = n / (adapters > 1 ? adapters : 1);
+    const bool sort = adapters > 1 && n > AD_FEW_ROWS && each > 1;
+    p.sorted = grad || sort;
     p.tp = rank <= 32 && din >= 8 && dout >= 8 ? 64 : 32;  // (of k_vec_ad_up's other form at most 32)
-    while (p.tp > 1 && 2 * p.tp > each) p.tp /= 2;
-    while (p.tp > 16 && n / p.tp < 256) p.tp /= 2;
-    p.sorted = grad || (adapters > 1 && n > AD_FEW_ROWS && p.tp > 1);
+    while (p.tp > 16 && (p.tp > each || n / p.tp < 256)) p.tp /= 2;
+    p.tp_up = p.tp;
+    p.few = p.sorted && each * rank < AD_UP_FEW;
+    if (p.few) {  // tiles of up to eight, fewer where there would be too few waves
+        const int64_t across = ad_column_blocks(grad ? din : dout, (int)vec_bytes(type));
+        p.tp_up = AD_FEW_POSITIONS;
+        while (p.tp_up > 1 && (n + p.tp_up - 1) / p.tp_up * across < 1024) p.tp_up /= 2;
+    }
+    if (adapters > 1 && !p.sorted) p.tp = p.tp_up = 1;
     p.grouped = n <= AD_GROUP_ROWS && adapters <= AD_GROUP_ADAPTERS;
     p.rp = (rank + 15) & ~15;
     const int d = grad ? dout : din;
     const int64_t tiles = (n + p.tp - 1) / p.tp;
     p.waves = d >= 1024 && rank <= 64 ? 8 : 4;
-    int64_t slabs = tiles * p.waves >= 1024 ? 1 : 1024 / (tiles * p.waves);
-    if (slabs > d / (p.waves * 64)) slabs = d / (p.waves * 64);
+    p.own = p.sorted && each * d < AD_OWN;
+    // about 1024 waves, each with at least two turns of 64 columns
+    const int64_t active = tiles * p.waves;
+    int64_t slabs = active >= 1024 ? 1 : 1024 / active;
+    const int64_t most = d / (p.own ? 256 : p.waves * 64);
+    if (slabs > most) slabs = most;
     if (slabs > AD_MAX_SLABS) slabs = AD_MAX_SLABS;
     if (slabs < 1) slabs = 1;
     const int64_t per = ((d + slabs - 1) / slabs + 255) / 256 * 256;
@@ -50,8 +66,8 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     if (p.sorted) at = p.grouped ? 2 * vec_up256((size_t)n * 4) : qadc_vec_sort_bytes(n, adapters);
     p.part = take((size_t)p.slabs * n * p.rp * 4);
     if (grad) {
-        p.len_a = ad_len(n, din, rank);
-        p.len_b = ad_len(n, dout, rank);
+        p.len_a = ad_len(n, din, dout, rank);
+        p.len_b = ad_len(n, dout, din, rank);
         p.dpad_a = (din + 7) & ~7;
         p.dpad_b = (dout + 7) & ~7;
         p.part_a = take((size_t)((n + p.len_a - 1) / p.len_a) * 2 * rank * p.dpad_a * 4);
@@ -93,6 +109,10 @@ static int ad_up_blocks(int64_t n, int tp, int d, int type) {
     return (int)(want < most ? want : most);
 }
 
+static bool ad_fits(const AdPlan &p, int64_t n, int d, int type) {
+    return (n + p.tp - 1) / p.tp * p.slabs <= VEC_MAX_BLOCKS && (n + p.tp_up - 1) / p.tp_up * ad_column_blocks(d, (int)vec_bytes(type)) <= VEC_MAX_BLOCKS;
+}
+
 #define AD_CHECK(name)                                                                                                                              \
     uint32_t threshold;                                                                                                                             \
     float factor;                                                                                                                                   \
@@ -128,8 +148,7 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
                 "vec_adapter: misaligned pointer");
     hipStream_t s = (hipStream_t)stream;
     const AdPlan plan = ad_plan(n, din, dout, rank, adapters, type, false);
-    const int64_t tiles = (n + plan.tp - 1) / plan.tp;
-    VEC_REQUIRE(tiles * plan.slabs <= VEC_MAX_BLOCKS && tiles * ad_up_blocks(n, plan.tp, dout, type) <= VEC_MAX_BLOCKS, "vec_adapter: n=%lld too large for one call", (long long)n);
+    VEC_REQUIRE(ad_fits(plan, n, dout, type), "vec_adapter: n=%lld too large for one call", (long long)n);
     AdRows rows = {ids, id_bytes, plan.tp, n, adapters, nullptr, nullptr};
     char *ws = (char *)workspace;
     float *part = nullptr;
@@ -140,12 +159,13 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
         if (plan.sorted) ad_sort(plan, rows, ws, s);
         const AdMatrix m = {a, ld_a, stride_a, rank, din};
         VEC_TYPED(type, T, AdLaunch<T>::down(rows, x, ld_x, m, scales, factor, mask, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per,
-                                             plan.slabs == 1 ? t : nullptr, s));
+                                             plan.own, plan.slabs == 1 ? t : nullptr, s));
     }
     float *const keep = adapters > 0 && plan.slabs == 1 ? nullptr : t;
+    rows.tp = plan.tp_up;
     const AdFactor f = {part, plan.rp, n * plan.rp, plan.slabs};
     const AdMatrix m = {b, ld_b, stride_b, rank, dout};
-    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, ad_up_blocks(n, plan.tp, dout, type), keep, s));
+    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, plan.few, ad_up_blocks(n, plan.tp_up, dout, type), keep, s));
     QADC_LAUNCH_CHECK("vec_adapter's kernels");
     return PQ_OK;
 }
@@ -180,10 +200,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     if (n > 0) {
         plan = ad_plan(n, din, dout, rank, adapters, type, true);
         rows.tp = plan.tp;
-        const int64_t tiles = (n + plan.tp - 1) / plan.tp;
-        VEC_REQUIRE(tiles * plan.slabs <= VEC_MAX_BLOCKS && tiles * ad_up_blocks(n, plan.tp, din, type) <= VEC_MAX_BLOCKS &&
-                        (n / plan.len_a + 1) * ad_outer_blocks(din) <= VEC_MAX_BLOCKS &&
-                        (n / plan.len_b + 1) * ad_outer_blocks(dout) <= VEC_MAX_BLOCKS, "vec_adapter_grad: n=%lld too large for one call", (long long)n);
+        VEC_REQUIRE(ad_fits(plan, n, din, type) && (n / plan.len_a + 1) * ad_outer_blocks(din, dout) + (n / plan.len_b + 1) * ad_outer_blocks(dout, din) <= VEC_MAX_BLOCKS, "vec_adapter_grad: n=%lld too large for one call", (long long)n);
         char *ws = (char *)workspace;
         const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
         AdFactor u = {nullptr, plan.rp, n * plan.rp, plan.slabs};
@@ -194,13 +211,13 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
             oa.part = (float *)(ws + plan.part_a);
             ob.part = (float *)(ws + plan.part_b);
             ad_sort(plan, rows, ws, s);
-            const AdFactor kept = {t, rank, 0, 1};
-            VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, scales, factor, none, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per, nullptr, s);
-                      AdLaunch<T>::outer(rows, plan.len_b, kept, rank, dy, ld_dy, dout, none, ob, narrow, s);
-                      AdLaunch<T>::outer(rows, plan.len_a, u, rank, x, ld_x, din, mask, oa, narrow, s));
+            const AdSide sb = {{t, rank, 0, 1}, dy, ld_dy, dout, plan.len_b, ad_outer_blocks(dout, din), ob}, sa = {u, x, ld_x, din, plan.len_a, ad_outer_blocks(din, dout), oa};
+            VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, scales, factor, none, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per, plan.own, nullptr, s);
+                      AdLaunch<T>::outer(rows, rank, mask, sb, sa, narrow, s));
         }
+        rows.tp = plan.tp_up;
         if (dx)
-            VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, mask, ad_up_blocks(n, plan.tp, din, type), nullptr, s));
+            VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, mask, plan.few, ad_up_blocks(n, plan.tp_up, din, type), nullptr, s));
     }
     if (adapters > 0) {
         const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);

@@ -5,17 +5,16 @@
 // blocks of `up` (16 bytes a lane) and `outer` (four columns a lane) that hold d columns
 static inline int ad_blocks(int d, int lane_columns) { return (d + 64 * lane_columns - 1) / (64 * lane_columns); }
 static inline int ad_column_blocks(int d, int bytes) { return ad_blocks(d, d < 16 / bytes ? 1 : 16 / bytes); }
-static inline int ad_outer_blocks(int d) { return ad_blocks(d, d < 4 ? 1 : 4); }
+static inline int ad_outer_blocks(int d, int other) { return ad_blocks(d, d < 4 || other < 4 ? 1 : 4); }  // (one form for both gradients)
 
 template <class T>
 struct AdLaunch {
     static void down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
-                     int64_t part_stride, int rp, int waves, int slabs, int per, float *keep, hipStream_t s);
+                     int64_t part_stride, int rp, int waves, int slabs, int per, bool own, float *keep, hipStream_t s);
     // narrow: the result is of type T, else float32
     static void up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                   const VecMask &mask, int column_blocks, float *keep, hipStream_t s);
-    static void outer(const AdRows &rows, int len, const AdFactor &f, int rank, const void *x, int64_t ld_x, int d, const VecMask &mask, const AdOuter &o,
-                      bool narrow, hipStream_t s);
+                   const VecMask &mask, bool few, int column_blocks, float *keep, hipStream_t s);
+    static void outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, hipStream_t s);
 };
 
 #ifdef VEC_ADAPTER_SOURCE
@@ -23,18 +22,18 @@ static dim3 ad_grid(const AdRows &rows, int parts, int threads) { return vec_gri
 
 template <class T>
 void AdLaunch<T>::down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
-                       int64_t part_stride, int rp, int waves, int slabs, int per, float *keep, hipStream_t s) {
+                       int64_t part_stride, int rp, int waves, int slabs, int per, bool own, float *keep, hipStream_t s) {
     const dim3 grid = ad_grid(rows, slabs, 64 * waves);
-    // tiles of x and W, and at least the sums' four
+    // tiles of x and W, and at least the sums' four kilobytes a wave
     auto lds = [&](int rk) {
-        const int nt = rows.tp > 32 ? 4 : (rows.tp > 16 ? 2 : 1), tiles = nt + rk > 2 ? nt + rk : 2;
-        return (size_t)waves * tiles * 2048;
+        const int nt = rows.tp > 32 ? 4 : (rows.tp > 16 ? 2 : 1);
+        return (size_t)waves * (nt + rk) * 2048;
     };
 #define GO2(RK, M)                                                                                                         \
     do {                                                                                                                   \
-        void (*const k)(AdRows, const T *, int64_t, AdMatrix, const float *, float, VecMask, float *, int64_t, int, int, int, float *) = &k_vec_ad_down<T, RK, M>; \
+        void (*const k)(AdRows, const T *, int64_t, AdMatrix, const float *, float, VecMask, float *, int64_t, int, int, int, int, float *) = &k_vec_ad_down<T, RK, M>; \
         if (lds(RK) > 65536) (void)hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds(RK)); \
-        hipLaunchKernelGGL(k, grid, dim3(64 * waves), lds(RK), s, rows, (const T *)x, ld_x, m, scales, factor, mask, part, part_stride, rp, slabs, per, keep); \
+        hipLaunchKernelGGL(k, grid, dim3(64 * waves), lds(RK), s, rows, (const T *)x, ld_x, m, scales, factor, mask, part, part_stride, rp, slabs, per, (int)own, keep); \
     } while (0)
 #define GO(RK)                           \
     do {                                 \
@@ -51,7 +50,26 @@ void AdLaunch<T>::down(const AdRows &rows, const void *x, int64_t ld_x, const Ad
 
 template <class T>
 void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                     const VecMask &mask, int column_blocks, float *keep, hipStream_t s) {
+                     const VecMask &mask, bool few, int column_blocks, float *keep, hipStream_t s) {
+    if (few) {
+        const int64_t tiles = (rows.n + rows.tp - 1) / rows.tp;
+        const int cb = ad_column_blocks(m.d, (int)sizeof(T));
+        const dim3 grid = vec_grid((tiles * cb + 3) / 4, 256);
+#define GO(Y, M, E)                                                                                                        \
+    hipLaunchKernelGGL((k_vec_ad_up_few<T, Y, M, E>), grid, dim3(256), 0, s, rows, f.p, f.ld, f.stride, f.slabs, m, (const Y *)base, ld_base, (Y *)y, \
+                       ld_y, mask, cb, keep)
+#define GO2(Y, M)                                              \
+    do {                                                       \
+        if (m.d < AD_COLS(T)) GO(Y, M, 1);                     \
+        else GO(Y, M, AD_COLS(T));                             \
+    } while (0)
+        if (mask.threshold) GO2(T, true);
+        else if (narrow) GO2(T, false);
+        else GO2(float, false);
+#undef GO2
+#undef GO
+        return;
+    }
     const dim3 grid = ad_grid(rows, column_blocks, 256);
     const size_t lds = (size_t)((m.rank + 31) / 32) * ((rows.tp + 15) / 16) * AdWide<T>::parts * 1024;
 #define GO(Y, M, ONE, E)                                                                                                   \
@@ -70,18 +88,18 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
 }
 
 template <class T>
-void AdLaunch<T>::outer(const AdRows &rows, int len, const AdFactor &f, int rank, const void *x, int64_t ld_x, int d, const VecMask &mask, const AdOuter &o,
-                        bool narrow, hipStream_t s) {
-    const int cb = ad_outer_blocks(d);
-    dim3 grid = vec_grid((rows.n + len - 1) / len * cb, 256);
+void AdLaunch<T>::outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, hipStream_t s) {
+    auto blocks = [&](const AdSide &side) { return (rows.n + side.len - 1) / side.len * side.column_blocks; };
+    const int64_t blocks_b = blocks(b);
+    dim3 grid = vec_grid(blocks_b + blocks(a), 256);
 #define GO(O, RK, M, E)                                                                                                    \
     do {                                                                                                                   \
         grid.z = (unsigned)((rank + 16 * RK - 1) / (16 * RK));                                                             \
-        hipLaunchKernelGGL((k_vec_ad_outer<T, O, RK, M, E>), grid, dim3(256), 0, s, rows, len, f, rank, (const T *)x, ld_x, d, mask, o, cb); \
+        hipLaunchKernelGGL((k_vec_ad_outer<T, O, RK, M, E>), grid, dim3(256), 0, s, rows, rank, mask, b, a, blocks_b);      \
     } while (0)
 #define GO2(O, M)                                                                                                          \
     do {                                                                                                                   \
-        if (d < 4) GO(O, 1, M, 1);                                                                                         \
+        if (a.d < 4 || b.d < 4) GO(O, 1, M, 1);                                                                                         \
         else if (rank <= 16) GO(O, 1, M, 4);                                                                               \
         else if (rank <= 32) GO(O, 2, M, 4);                                                                               \
         else GO(O, 4, M, 4);                                                                                                  \
