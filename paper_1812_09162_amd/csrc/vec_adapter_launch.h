@@ -70,6 +70,12 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
 #undef GO
         return;
     }
+    // Eight bytes a lane where sixteen leave few blocks: half the registers and twice the waves.  us with sixteen / eight: 16,384 x 2048 at rank 32 (1024 blocks) 36 / 29, 10,000 x
+    // 1001 at rank 12 (1252) 32 / 25; 16,384 x 4096 at rank 16 (2048) 53 / 53, of 1000 adapters (8192) 104 / 131; single rows of 4096 5.4 / 5.9.  With a mask each of two
+    // neighbouring lanes would make it: 70 / 91.
+    const int64_t tiles = (rows.n + rows.tp - 1) / rows.tp;
+    const bool half = sizeof(T) == 2 && m.rank <= 32 && !mask.threshold && m.d >= AD_COLS(T) && rows.tp >= 16 && tiles * ad_column_blocks(m.d, 2) < 2048;
+    if (half) column_blocks = ad_blocks(m.d, 4);
     const dim3 grid = ad_grid(rows, column_blocks, 256);
     const size_t lds = (size_t)((m.rank + 31) / 32) * ((rows.tp + 15) / 16) * AdWide<T>::parts * 1024;
 #define GO(Y, M, ONE, E)                                                                                                   \
@@ -80,7 +86,10 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
         else if (m.rank <= 32) GO(Y, M, true, AD_COLS(T));                                                                 \
         else GO(Y, M, false, AD_COLS(T));                                                                                              \
     } while (0)
-    if (mask.threshold) GO2(T, true);  // (a gradient of x, which is of its type)
+    if (half) {
+        if (narrow) GO(T, false, true, 4);
+        else GO(float, false, true, 4);
+    } else if (mask.threshold) GO2(T, true);  // (a gradient of x, which is of its type)
     else if (narrow) GO2(T, false);
     else GO2(float, false);
 #undef GO2
