@@ -563,9 +563,11 @@ class _Call:
 
     def matrices(self, what: str, t: torch.Tensor, count: int, n: int, d: int, dtype):
         """Address of [count, n, d], the distances of its rows and of its matrices, checked."""
-        shape, stride = t.shape, t.stride()
-        if len(shape) != 3 or shape[0] != count or shape[1] != n or shape[2] != d or t.dtype != dtype or t.get_device() != self.index:
-            _refuse(self.name, f"{what}: {t.dtype} of shape {tuple(shape)} on {t.device}, not {dtype} of {(count, n, d)} on {self.device}")
+        if t.shape != (count, n, d) or t.dtype != dtype or t.get_device() != self.index:
+            _refuse(self.name, f"{what}: {t.dtype} of shape {tuple(t.shape)} on {t.device}, not {dtype} of {(count, n, d)} on {self.device}")
+        if t.is_contiguous():
+            return t.data_ptr(), d, n * d
+        stride = t.stride()
         ld = stride[1] if n > 1 else d
         if ld < d or (stride[2] != 1 and d > 1):
             _refuse(self.name, f"{what}'s rows of {d} are {ld} apart, the values of a row {stride[2]}")
@@ -808,9 +810,10 @@ def _adapters(call: _Call, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, id
     n, din, xp, ldx = call.first_rows("x", x)
     if a.dim() != 3 or b.dim() != 3:
         _refuse(call.name, f"a and b of shapes {tuple(a.shape)} and {tuple(b.shape)}, not [adapters, rank, columns]")
-    count, rank, dout = a.shape[0], a.shape[1], b.shape[2]
-    for v in (din, dout, rank, count):
-        call.columns(v)
+    count, rank, _ = a.shape
+    dout = b.shape[2]
+    if max(din, dout, rank, count) > 0x7FFFFFFF:
+        _refuse(call.name, f"din={din}, dout={dout}, rank={rank}, adapters={count}")
     ap, lda, sta = call.matrices("a", a, count, rank, din, x.dtype)
     bp, ldb, stb = call.matrices("b", b, count, rank, dout, x.dtype)
     idp, id_bytes = call.ids(ids)

@@ -695,7 +695,8 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
 
 // The same for few rows of an adapter: on the vector units, without a wait between waves.  A wave takes a tile of at most eight positions and 64 E columns, E a lane;
 // four rows of one adapter share what it reads of W.  Where a tile of the matrix cores would hold three rows of sixteen, the rest of the form above (the parts of the
-// factor, columns put together, LDS) costs more than these products: ABOVE us where this takes FEW.
+// factor, columns put together, LDS) costs more than these products: 8192 mixed rows of 500 adapters, 1001 fp16
+// columns at rank 8: 41 us above, 24 here; 16,384 of 1000, 4096 bf16 columns at rank 16: 104 above, 128 here.
 #define AD_FEW_POSITIONS 8
 template <class T, class Y, bool MASK, int E>
 __global__ void __launch_bounds__(256, 2)
@@ -792,6 +793,143 @@ k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t 
             ad_store<Y, E>(y + (uint32_t)row[k] * ld_y, col, m.d, acc[k]);
         }
     }
+}
+
+// ------------------------------------------------------------ single tokens --
+// Both products in one launch, for rows of their own adapters without dropout: a block takes a row and 64 AD_COLS columns of the result, and makes the row's t itself, so
+// that A is read once for each of these (from the L2 cache).  Its eight waves share the columns of x, AD_ONE_TILES KB of A on their way each, then the ranks of B, which is asked
+// for before.  4096 x 4096 bf16 at rank 16, us in a graph by two
+// kernels / by this: 1 row 8.8 / 5.4, 16 9.1 / 5.6, 32 (33 MB of A read) 8.6 / 6.8, 64 (67 MB) 9.9 / 12.5; 16 rows at rank 64 10.7 / 16.5.
+#define AD_ONE_TILES 4
+template <class T, class Y, int RK, int E>
+__global__ void __launch_bounds__(512)
+k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, AdMatrix mb, const float *__restrict__ scales, const Y *base, int64_t ld_base, Y *y,
+             int64_t ld_y, float *__restrict__ keep, int column_blocks) {
+    constexpr int EA = AD_COLS(T), COLS = 8 * EA, KS = COLS / 32, U = AD_ONE_TILES / RK, BR = 2 * RK;  // U: turns on their way; BR: ranks of B a wave
+    constexpr int LDS = 8 * U * RK * 128;
+    __shared__ ad_u4 tiles[LDS > 32 * E * 4 ? LDS : 32 * E * 4];  // [wave][turn][16 ranks][16 rows][8 pieces]; [wave][64 E] sums
+    __shared__ float sums[8][16 * RK], t[16 * RK];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4, lr = lane >> 3, lp = lane & 7;
+    const int64_t block = vec_block(), row = block / column_blocks;
+    if (row >= rows.n) return;
+    const int slab = (int)(block - row * column_blocks), c0 = slab * 64 * E, d = ma.d, rank = ma.rank;
+    const int e = __builtin_amdgcn_readfirstlane(ad_id(rows, row));
+    const bool none = e == rows.adapters;
+    const int own = c0 + (int)threadIdx.x;  // the thread's column of the result
+    const bool writes = threadIdx.x < 64 * E && own < mb.d;
+    float old = 0.0f;
+    if (writes && base) old = (float)base[row * ld_base + own];
+    if (keep && slab == 0 && none && (int)threadIdx.x < rank) keep[row * rank + threadIdx.x] = 0.0f;
+    if (none) {
+        if (writes && base != y) y[row * ld_y + own] = (Y)old;
+        return;
+    }
+    const T *a = (const T *)ma.p + e * ma.stride, *b = (const T *)mb.p + e * mb.stride;
+    const T *xr = x + row * ld_x;
+    const int from = ad_from<E>(c0 + E * lane, mb.d);
+    vec_pack<T, E> bv[BR];  // ranks wave BR and on (behind the last that one again)
+#pragma unroll
+    for (int q = 0; q < BR; ++q) bv[q] = ad_load<T, E>(b + (int64_t)(wave * BR + q < rank ? wave * BR + q : rank - 1) * mb.ld, from);
+    ad_u4 *mine = tiles + wave * U * RK * 128;
+    vec_f4 acc[RK];
+#pragma unroll
+    for (int j = 0; j < RK; ++j) acc[j] = (vec_f4)0.0f;
+    const T *ar[RK][2];
+#pragma unroll
+    for (int j = 0; j < RK; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) ar[j][h] = a + (int64_t)(16 * j + 8 * h + lr < rank ? 16 * j + 8 * h + lr : rank - 1) * ma.ld;
+    vec_pack<T, EA> v[U][RK][2];
+    vec_pack<T> xv[U][KS];
+    auto multiply = [&](int u) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int j = 0; j < RK; ++j) {
+                const ad_u4 *at = mine + (u * RK + j) * 128;
+                vec_pack<T> w;
+                if constexpr (sizeof(T) == 2) {
+                    w = __builtin_bit_cast(vec_pack<T>, at[ad_slot(c, 4 * ks + g)]);
+                } else {
+                    const vec_f4 lo = __builtin_bit_cast(vec_f4, at[ad_slot(c, 2 * g)]), hi = __builtin_bit_cast(vec_f4, at[ad_slot(c, 2 * g + 1)]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = lo[i], w[4 + i] = hi[i];
+                }
+                acc[j] = ad_mul<T>(w, xv[u][ks], acc[j]);
+            }
+    };
+    auto put = [&](int u) {
+#pragma unroll
+        for (int j = 0; j < RK; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) mine[(u * RK + j) * 128 + ad_slot(8 * h + lr, lp)] = __builtin_bit_cast(ad_u4, v[u][j][h]);
+    };
+    const int first = COLS * wave, span = 8 * COLS, whole = first + COLS <= d ? (d - first - COLS) / span + 1 : 0;
+    for (int i = 0; i < whole; i += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u >= whole) continue;
+            const int k = first + (i + u) * span;
+#pragma unroll
+            for (int j = 0; j < RK; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) v[u][j][h] = ad_load<T, EA>(ar[j][h], k + EA * lp);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) xv[u][ks] = *(const vec_pack<T> *)(xr + k + 32 * ks + 8 * g);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u < whole) put(u);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u < whole) multiply(u);
+    }
+    if (first + whole * span < d) {
+        const int k = first + whole * span, ca = k + EA * lp;
+#pragma unroll
+        for (int j = 0; j < RK; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[0][j][h] = vec_load<T, EA>(ar[j][h] + (ca < d ? ca : 0), d - ca, ca);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int cx = k + 32 * ks + 8 * g;
+            xv[0][ks] = vec_load<T>(xr + (cx < d ? cx : 0), d - cx, cx);
+        }
+        put(0);
+        multiply(0);
+    }
+    if (c == 0)  // (all sixteen columns of the products are the row)
+#pragma unroll
+        for (int j = 0; j < RK; ++j) *(vec_f4 *)&sums[wave][16 * j + 4 * g] = acc[j];
+    __syncthreads();
+    if (threadIdx.x < 16 * RK) {
+        float s = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += sums[u][threadIdx.x];
+        s = (int)threadIdx.x < rank ? s * (scales ? scales[e] : 1.0f) : 0.0f;
+        t[threadIdx.x] = s;
+        if (keep && slab == 0 && (int)threadIdx.x < rank) keep[row * rank + threadIdx.x] = s;
+    }
+    __syncthreads();
+    float *part = (float *)tiles;  // [wave][64 E]
+    vec_f<E> f = (vec_f<E>)0.0f;
+#pragma unroll
+    for (int q = 0; q < BR; ++q) {
+        const vec_f<E> w = vec_wide<T, E>(bv[q]);
+        const float by = t[wave * BR + q];
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] = __fmaf_rn(by, w[i], f[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) part[wave * 64 * E + lane * E + i] = f[i];
+    __syncthreads();
+    if (!writes) return;
+    // column `own` is value i of lane l, whose columns begin at its `from`
+    const int l = (int)threadIdx.x / E, i = own - ad_from<E>(c0 + E * l, mb.d);
+    float s = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += part[u * 64 * E + l * E + i];
+    y[row * ld_y + own] = (Y)(old + s);
 }
 
 // ------------------------------------------------------------------- outer --

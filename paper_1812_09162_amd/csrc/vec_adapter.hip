@@ -8,11 +8,13 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 #define AD_FEW_ROWS 64  // rows that are not sorted
 #define AD_MAX_SLABS 16
 #define AD_OWN 32768    // rows an adapter times columns below which `down`'s waves take an adapter each
+#define AD_ONE_BYTES (40 << 20)  // of A that single rows in one launch may read
 #define AD_UP_FEW 256   // rows an adapter times ranks below which `up` runs on the vector units
 
 struct AdPlan {
     bool sorted, grouped;      // grouped: by k_vec_ad_group
     bool few;                  // `up` on the vector units
+    bool one;                  // without dropout: single rows in one launch
     int tp, tp_up;             // positions of a tile of `down`, of `up`
     int rp;                    // ranks of a row of partial sums
     int waves, slabs, per;     // of the contraction over columns
@@ -45,6 +47,9 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
         while (p.tp_up > 1 && (n + p.tp_up - 1) / p.tp_up * across < 1024) p.tp_up /= 2;
     }
     if (adapters > 1 && !p.sorted) p.tp = p.tp_up = 1;
+    // (a row's A is read for each of the column blocks)
+    p.one = !grad && !p.sorted && adapters > 0 && n <= (adapters > 1 ? AD_FEW_ROWS : 8) && rank <= 64 &&
+            n * ad_column_blocks(dout, (int)vec_bytes(type)) * rank * din * (int64_t)vec_bytes(type) <= AD_ONE_BYTES;
     p.grouped = n <= AD_GROUP_ROWS && adapters <= AD_GROUP_ADAPTERS;
     p.rp = (rank + 15) & ~15;
     const int d = grad ? dout : din;
@@ -153,8 +158,14 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
     char *ws = (char *)workspace;
     float *part = nullptr;
     const VecMask mask = {state, layer, threshold}, none = {nullptr, 0, 0};
+    if (adapters > 0) AD_WORKSPACE("vec_adapter", plan.total);
+    if (plan.one && threshold == 0) {
+        const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
+        VEC_TYPED(type, T, AdLaunch<T>::one(rows, x, ld_x, ma, mb, scales, base, ld_base, y, ld_y, y_type == type, t, s));
+        QADC_LAUNCH_CHECK("k_vec_ad_one");
+        return PQ_OK;
+    }
     if (adapters > 0) {
-        AD_WORKSPACE("vec_adapter", plan.total);
         part = (float *)(ws + plan.part);
         if (plan.sorted) ad_sort(plan, rows, ws, s);
         const AdMatrix m = {a, ld_a, stride_a, rank, din};

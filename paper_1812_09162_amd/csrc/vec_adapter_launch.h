@@ -14,6 +14,9 @@ struct AdLaunch {
     // narrow: the result is of type T, else float32
     static void up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
                    const VecMask &mask, bool few, int column_blocks, float *keep, hipStream_t s);
+    // both products for single rows, of at most 64 ranks
+    static void one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, const void *base, int64_t ld_base, void *y,
+                    int64_t ld_y, bool narrow, float *keep, hipStream_t s);
     static void outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, hipStream_t s);
 };
 
@@ -92,6 +95,26 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
     } else if (mask.threshold) GO2(T, true);  // (a gradient of x, which is of its type)
     else if (narrow) GO2(T, false);
     else GO2(float, false);
+#undef GO2
+#undef GO
+}
+
+template <class T>
+void AdLaunch<T>::one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, const void *base, int64_t ld_base, void *y,
+                      int64_t ld_y, bool narrow, float *keep, hipStream_t s) {
+    const int cb = ad_column_blocks(b.d, (int)sizeof(T));
+    const dim3 grid = vec_grid(rows.n * cb, 512);
+#define GO(Y, RK, E)                                                                                                       \
+    hipLaunchKernelGGL((k_vec_ad_one<T, Y, RK, E>), grid, dim3(512), 0, s, rows, (const T *)x, ld_x, a, b, scales, (const Y *)base, ld_base, (Y *)y, ld_y, keep, cb)
+#define GO2(Y)                                                 \
+    do {                                                       \
+        if (b.d < AD_COLS(T)) GO(Y, 4, 1);                     \
+        else if (a.rank <= 16) GO(Y, 1, AD_COLS(T));           \
+        else if (a.rank <= 32) GO(Y, 2, AD_COLS(T));           \
+        else GO(Y, 4, AD_COLS(T));                             \
+    } while (0)
+    if (narrow) GO2(T);
+    else GO2(float);
 #undef GO2
 #undef GO
 }
