@@ -1108,13 +1108,15 @@ struct AdJoin {
 };
 template <class O>
 __global__ void __launch_bounds__(256)
-k_vec_ad_join(AdRows rows, int rank, AdJoin ja, AdJoin jb) {
+k_vec_ad_join(AdRows rows, int rank, const uint32_t *__restrict__ starts, AdJoin ja, AdJoin jb) {
     const AdJoin &j = blockIdx.z ? jb : ja;
     const AdOuter &o = j.o;
     __shared__ int64_t found[2];
     const uint32_t e = blockIdx.y;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (wave < 2) {  // the first position whose key is at least e (at least e + 1), a 64th of what is left a round
+    if (starts) {
+        if (threadIdx.x < 2) found[threadIdx.x] = starts[e + threadIdx.x];
+    } else if (wave < 2) {  // the first position whose key is at least e (at least e + 1), a 64th of what is left a round
         int64_t lo = 0, hi = rows.n;
         while (lo < hi) {
             const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
@@ -1128,11 +1130,13 @@ k_vec_ad_join(AdRows rows, int rank, AdJoin ja, AdJoin jb) {
     }
     __syncthreads();
     const int64_t lo = found[0], hi = found[1];
-    const int64_t from = lo / j.len, to = lo < hi ? (hi - 1) / j.len : 0;
+    // (len is a power of two)
+    const int shift = __builtin_ctz(j.len);
+    const int64_t from = lo >> shift, to = lo < hi ? (hi - 1) >> shift : 0;
     if (lo < hi ? from == to : o.accumulate) return;
     const int pieces = o.dpad / 8;
-    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < (int64_t)rank * pieces; i += gridDim.x * 256) {
-        const int r = (int)(i / pieces), col = (int)(i - (int64_t)r * pieces) * 8;
+    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < (uint32_t)rank * pieces; i += gridDim.x * 256) {  // (at most 2^25)
+        const int r = (int)(i / (uint32_t)pieces), col = (int)(i - (uint32_t)r * pieces) * 8;
         vec_f8 sum = (vec_f8)0.0f;
         if (lo < hi) {
             const int64_t each = 2 * (int64_t)rank * o.dpad;
@@ -1156,33 +1160,39 @@ k_vec_ad_join(AdRows rows, int rank, AdJoin ja, AdJoin jb) {
 
 // ----------------------------------------------------------------- grouping --
 // Positions sorted by id (stable), up to AD_GROUP_ROWS rows and AD_GROUP_ADAPTERS adapters: one launch.  A block places AD_GROUP_TILE positions.  It counts all ids itself,
-// those before its own apart (16,384 ids are 128 KB from the L2 cache); neighbours with one id count at once, so that runs do not queue for one counter.
+// those before its own apart (16,384 ids are 128 KB from the L2 cache); of sixty-four neighbours those of two ids count at once, so that runs and few ids do not queue for
+// one counter.  16,384 ids GROUP us (two ids at random TWOIDS), 1024 SMALL: two round trips to memory, and the instructions of sixteen waves on a CU.
 #define AD_GROUP_TILE 256
 #define AD_GROUP_ROWS 65536
 #define AD_GROUP_ADAPTERS 4095
 template <class ID>
 __global__ void __launch_bounds__(1024)
-k_vec_ad_group(const ID *__restrict__ ids, int n, int adapters, uint32_t *__restrict__ keys, uint32_t *__restrict__ pos) {
+k_vec_ad_group(const ID *__restrict__ ids, int n, int adapters, uint32_t *__restrict__ keys, uint32_t *__restrict__ pos, uint32_t *__restrict__ starts) {
     __shared__ uint32_t early[AD_GROUP_ADAPTERS + 1], late[AD_GROUP_ADAPTERS + 1], wide[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = blockIdx.x * AD_GROUP_TILE;
     auto norm = [&](ID id) { return id >= 0 && id < adapters ? (uint32_t)id : (uint32_t)adapters; };
     for (int i = threadIdx.x; i <= adapters; i += 1024) early[i] = late[i] = 0;
     __syncthreads();
-    for (int i0 = wave * 64; i0 < n; i0 += 8 * 1024) {
-        ID id[8];
+    for (int i0 = wave * 64; i0 < n; i0 += 4 * 1024) {
+        ID id[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) id[u] = ids[i0 + u * 1024 + lane < n ? i0 + u * 1024 + lane : n - 1];
+        for (int u = 0; u < 4; ++u) id[u] = ids[i0 + u * 1024 + lane < n ? i0 + u * 1024 + lane : n - 1];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int i = i0 + u * 1024 + lane;
-            const uint32_t key = norm(id[u]), left = (uint32_t)__shfl_up((int)key, 1);
-            const bool in = i < n, head = in && (lane == 0 || left != key);
-            const uint64_t heads = __ballot(head), all = __ballot(in);
-            if (head) {
-                const uint64_t behind = lane == 63 ? 0 : heads >> (lane + 1);
-                const int length = behind ? __builtin_ctzll(behind) + 1 : __popcll(all) - lane;
-                atomicAdd(i < first ? &early[key] : &late[key], (uint32_t)length);
+        for (int u = 0; u < 4; ++u) {
+            const int at = i0 + u * 1024;
+            if (at >= n) break;
+            const uint32_t key = norm(id[u]);
+            uint32_t *count = at < first ? early : late;
+            uint64_t todo = __ballot(at + lane < n);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {  // those of the first lane's id, and of the first other
+                if (!todo) continue;
+                const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)key, __builtin_ctzll(todo));
+                const uint64_t same = __ballot(key == one) & todo;
+                if (lane == 0) atomicAdd(&count[one], (uint32_t)__popcll(same));
+                todo &= ~same;
             }
+            if (todo >> lane & 1) atomicAdd(&count[key], 1u);
         }
     }
     __syncthreads();
@@ -1207,7 +1217,10 @@ k_vec_ad_group(const ID *__restrict__ ids, int n, int adapters, uint32_t *__rest
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         const int b = threadIdx.x * 4 + u;
-        if (b <= adapters) early[b] += at;
+        if (b <= adapters) {
+            early[b] += at;
+            if (starts && blockIdx.x == 0) starts[b] = at;
+        }
         at += mine[u];
     }
     __syncthreads();

@@ -68,7 +68,7 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     p.slabs = (int)((d + per - 1) / per);
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += vec_up256(bytes); return was; };
-    if (p.sorted) at = p.grouped ? 2 * vec_up256((size_t)n * 4) : qadc_vec_sort_bytes(n, adapters);
+    if (p.sorted) at = p.grouped ? 2 * vec_up256((size_t)n * 4) + vec_up256((size_t)(adapters + 1) * 4) : qadc_vec_sort_bytes(n, adapters);
     p.part = take((size_t)p.slabs * n * p.rp * 4);
     if (grad) {
         p.len_a = ad_len(n, din, dout, rank);
@@ -82,17 +82,19 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     return p;
 }
 
-static void ad_sort(const AdPlan &p, AdRows &rows, char *ws, hipStream_t s) {
+// Returns where the adapters' positions begin (adapters + 1 numbers), or null where that is not known.
+static const uint32_t *ad_sort(const AdPlan &p, AdRows &rows, char *ws, hipStream_t s) {
     if (!p.grouped) {
         qadc_vec_sort(rows.ids, rows.id_bytes, rows.n, rows.adapters, ws, &rows.keys, &rows.pos, s);
-        return;
+        return nullptr;
     }
-    uint32_t *keys = (uint32_t *)ws, *pos = (uint32_t *)(ws + vec_up256((size_t)rows.n * 4));
+    uint32_t *keys = (uint32_t *)ws, *pos = (uint32_t *)(ws + vec_up256((size_t)rows.n * 4)), *starts = (uint32_t *)(ws + 2 * vec_up256((size_t)rows.n * 4));
     const dim3 grid((unsigned)((rows.n + AD_GROUP_TILE - 1) / AD_GROUP_TILE));
-    if (rows.id_bytes == 4) hipLaunchKernelGGL((k_vec_ad_group<int32_t>), grid, dim3(1024), 0, s, (const int32_t *)rows.ids, (int)rows.n, rows.adapters, keys, pos);
-    else hipLaunchKernelGGL((k_vec_ad_group<int64_t>), grid, dim3(1024), 0, s, (const int64_t *)rows.ids, (int)rows.n, rows.adapters, keys, pos);
+    if (rows.id_bytes == 4) hipLaunchKernelGGL((k_vec_ad_group<int32_t>), grid, dim3(1024), 0, s, (const int32_t *)rows.ids, (int)rows.n, rows.adapters, keys, pos, starts);
+    else hipLaunchKernelGGL((k_vec_ad_group<int64_t>), grid, dim3(1024), 0, s, (const int64_t *)rows.ids, (int)rows.n, rows.adapters, keys, pos, starts);
     rows.keys = keys;
     rows.pos = pos;
+    return starts;
 }
 
 static bool ad_sizes(int64_t n, int din, int dout, int rank, int adapters) {
@@ -207,6 +209,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     plan.len_a = plan.len_b = AD_MAX_LEN;
     plan.dpad_a = (din + 7) & ~7;
     plan.dpad_b = (dout + 7) & ~7;
+    const uint32_t *starts = nullptr;
     AdOuter oa = {da, ld_da, stride_da, nullptr, plan.dpad_a, accumulate}, ob = {db, ld_db, stride_db, nullptr, plan.dpad_b, accumulate};
     if (n > 0) {
         plan = ad_plan(n, din, dout, rank, adapters, type, true);
@@ -221,7 +224,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
             u.p = part;
             oa.part = (float *)(ws + plan.part_a);
             ob.part = (float *)(ws + plan.part_b);
-            ad_sort(plan, rows, ws, s);
+            starts = ad_sort(plan, rows, ws, s);
             const AdSide sb = {{t, rank, 0, 1}, dy, ld_dy, dout, plan.len_b, ad_outer_blocks(dout, din), ob}, sa = {u, x, ld_x, din, plan.len_a, ad_outer_blocks(din, dout), oa};
             VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, scales, factor, none, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per, plan.own, nullptr, s);
                       AdLaunch<T>::outer(rows, rank, mask, sb, sa, narrow, s));
@@ -234,7 +237,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
         const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
         const dim3 grid((unsigned)(pieces <= 256 * 64 ? (pieces + 255) / 256 : 64), (unsigned)adapters, 2);
         const AdJoin ja = {oa, plan.len_a, din}, jb = {ob, plan.len_b, dout};
-        VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, rank, ja, jb));
+        VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, rank, starts, ja, jb));
     }
     QADC_LAUNCH_CHECK("vec_adapter_grad's kernels");
     return PQ_OK;
