@@ -960,7 +960,7 @@ struct AdSide {
     AdOuter o;
 };
 template <class T, class O, int RK, bool MASK, int E>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, sizeof(T) == 4 && RK == 4 ? 1 : 2)
 k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_t blocks_b) {
     constexpr int P = AdWide<T>::parts;
     int64_t block = vec_block();
@@ -1022,9 +1022,17 @@ k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_
             vec_f8 v;
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = p[(int64_t)at[s0 + (q0 + q < m ? q0 + q : 0)] * f.ld];
-            for (int s = 1; s < f.slabs; ++s)
+            for (int s = 1; s < f.slabs; s += 4) {  // four parts on their way
+                float more[4][8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] += p[s * f.stride + (int64_t)at[s0 + (q0 + q < m ? q0 + q : 0)] * f.ld];
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) more[u][q] = p[(s + u < f.slabs ? s + u : 0) * f.stride + (int64_t)at[s0 + (q0 + q < m ? q0 + q : 0)] * f.ld];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] += s + u < f.slabs ? more[u][q] : 0.0f;
+            }
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = q0 + q < m && r < rank ? __builtin_canonicalizef(v[q]) : 0.0f;
             AdWide<T> w;

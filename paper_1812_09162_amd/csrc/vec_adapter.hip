@@ -24,10 +24,12 @@ struct AdPlan {
     size_t part, part_a, part_b, total;  // bytes from the workspace's start
 };
 
-static int ad_len(int64_t n, int d, int other, int rank) {
+// Positions of a block of `outer`: fewer where there would be few blocks (us, sums and their join, with 128 / 64 / 32 / 16: 10,000 x (1001 + 700) of 200 adapters 40 + 6 / 34 + 7 / 35 + 10; 79 x
+// (84 + 6403) of 38 64: 22 + 4 / 32: 19 + 4 / 16: 17 + 4; 2000 x (1024 + 1024) of 8 - / 10 + 4 / 10 + 5 / 15 + 7).
+static int ad_len(int64_t n, int64_t each, int d, int other, int rank) {
     const int64_t across = (int64_t)ad_outer_blocks(d, other) * ((rank + 63) / 64);
     int len = AD_MAX_LEN;
-    while (len > 64 && (n + len - 1) / len * across < 512) len /= 2;
+    while (len > (each < 16 ? 16 : 32) && (n + len - 1) / len * across < 400) len /= 2;
     return len;
 }
 
@@ -71,8 +73,8 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     if (p.sorted) at = p.grouped ? 2 * vec_up256((size_t)n * 4) + vec_up256((size_t)(adapters + 1) * 4) : qadc_vec_sort_bytes(n, adapters);
     p.part = take((size_t)p.slabs * n * p.rp * 4);
     if (grad) {
-        p.len_a = ad_len(n, din, dout, rank);
-        p.len_b = ad_len(n, dout, din, rank);
+        p.len_a = ad_len(n, each, din, dout, rank);
+        p.len_b = ad_len(n, each, dout, din, rank);
         p.dpad_a = (din + 7) & ~7;
         p.dpad_b = (dout + 7) & ~7;
         p.part_a = take((size_t)((n + p.len_a - 1) / p.len_a) * 2 * rank * p.dpad_a * 4);
@@ -235,7 +237,10 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     }
     if (adapters > 0) {
         const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
-        const dim3 grid((unsigned)(pieces <= 256 * 64 ? (pieces + 255) / 256 : 64), (unsigned)adapters, 2);
+        // about 16,384 blocks at most: of 1000 adapters most have nothing to join (WIDEJOIN us with a block for each 2048 values of 4096 x 16, NARROWJOIN so)
+        int64_t across = (pieces + 255) / 256;
+        if (across > 8192 / adapters + 1) across = 8192 / adapters + 1;
+        const dim3 grid((unsigned)across, (unsigned)adapters, 2);
         const AdJoin ja = {oa, plan.len_a, din}, jb = {ob, plan.len_b, dout};
         VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, rank, starts, ja, jb));
     }
