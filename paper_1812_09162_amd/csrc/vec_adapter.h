@@ -441,6 +441,7 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, co
     const int kb = slab * per, ke = kb + per < m.d ? kb + per : m.d;
     part += slab * part_stride;
     if (keep) ad_zeros(__ballot(tile.in && tile.id == rows.adapters), tile.row, list, m.rank, keep);
+    const int room = ((rows.tp > 32 ? 4 : (rows.tp > 16 ? 2 : 1)) + RK) * 128;  // a wave's LDS: of its largest form, since others may be in another
     uint64_t todo = __ballot(tile.id < rows.adapters);
     for (int i = 0; todo; ++i) {
         const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
@@ -454,7 +455,7 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, co
             // (its own wave: LDS and columns as a block of one)
 #define GO(NT)                                                                                                                                          \
     ad_down<T, RK, NT, MASK>(x, ld_x, w, m.ld, m.d, kb, ke, (int)(at & 0xffff), m.rank, j0, by, list, count, mask, key,                                 \
-                             (ad_u4 *)smem + (own ? wave * (NT + RK) * 128 : 0), own ? 0 : wave, own ? 1 : waves, part, rp, keep)
+                             (ad_u4 *)smem + (own ? wave * room : 0), own ? 0 : wave, own ? 1 : waves, part, rp, keep)
             if (RK <= 2 && count > 32) GO(RK <= 2 ? 4 : 1);
             else if (count > 16) GO(2);
             else GO(1);
