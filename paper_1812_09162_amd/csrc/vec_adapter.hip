@@ -5,11 +5,30 @@
 size_t qadc_vec_sort_bytes(int64_t n, int64_t rows);
 void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char *ws, const uint32_t **keys, const uint32_t **pos, hipStream_t s);
 
-#define AD_FEW_ROWS 64  // rows that are not sorted
+// The rules between the forms.  Times of whole calls in a graph, us, bfloat16 unless said.
+//
+// Rows that are not sorted: each reads its adapter for itself, mostly from the caches.  Sorted / not: 128 x 4096 at rank 16 18.8 / 13.9, 256 x 4096 20.7 / 20.0, 128 x 2048 at rank 64
+// 27 / 13, 256 24 / 19, 512 x 2048 at rank 16 15.9 / 22.1.
+#define AD_FEW_ROWS 256
+// Single rows in one launch (without dropout): what they read of A altogether, from the L2 cache, and how many they are (of one adapter the other form has whole tiles).  By two kernels /
+// by one: 64 x 4096 at rank 16 (67 MB) 9.9 / 12.5, 512 x 1024 at rank 16 (34 MB) 15.6 / 7.8, 2048 x 256 at rank 8 14.9 / 10.6, 4096 15.5 / 18.9; of one adapter 16 x 4096 9.0 / 5.6,
+// 256 x 1024 8.4 / 5.1.
+#define AD_ONE_BYTES (40 << 20)
+#define AD_ONE_ROWS 2048
+#define AD_ONE_SAME 256
+// `down`: a wave takes an adapter of the tile where adapters have few rows (rows an adapter times columns), unless one wave would have too many columns.  Together / a wave each:
+// 4096 rows of 1000 adapters at rank 16, 512 columns 41 / 36, 2048 69 / 65, 4096 125 / 138; 16,384 of 2000, 1024 columns 81 / 69; 16,384 of 1000, 2048 columns 110 / 113.
+#define AD_OWN 32768
+#define AD_OWN_COLUMNS 2048
+// `up`: rows an adapter times ranks below which it runs on the vector units.  Matrix cores / vector units: 8192 of 500 at rank 8, 1001 fp16 columns, 45 / 41;
+// 16,384 of 1000 at rank 16, 4096 columns, 193 / 243; 16,384 of 500 at rank 32, 1024 columns, 57 / 102.
+#define AD_UP_FEW 256
+// Tiles of 32 and 64 positions only if so many are left: of short rows more, since a tile is little work.  At least 256 / 64 tiles: 4096 x 1024 of 8 at rank 16 19.3 / 22.0,
+// 4096 x 4096 38 / 33, 8192 x 4096 52 / 50, 8192 x 2048 34.5 / 33.3, 2048 x 4096 float32 42 / 38.
+#define AD_TILES(din, dout) ((din) + (dout) < 4096 ? 256 : 64)
+// Slabs of `down` where there are fewer waves than this (with 512 / 1024 / 2048 / 4096: 1024 x 4096 at rank 16 22.6 / 20.5 / 19.2 / -; 512 x 4096 - / 16.6 / 17.9 / 17.9; 8192 x 2048 - / 34.5 / 34.5 / 37.2).
+#define AD_WAVES 1024
 #define AD_MAX_SLABS 16
-#define AD_OWN 32768    // rows an adapter times columns below which `down`'s waves take an adapter each
-#define AD_ONE_BYTES (40 << 20)  // of A that single rows in one launch may read
-#define AD_UP_FEW 256   // rows an adapter times ranks below which `up` runs on the vector units
 
 struct AdPlan {
     bool sorted, grouped;      // grouped: by k_vec_ad_group
@@ -35,12 +54,15 @@ static int ad_len(int64_t n, int64_t each, int d, int other, int rank) {
 
 static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int type, bool grad) {
     AdPlan p = {};
-    // as many positions a tile as the adapters have rows on average, at most; at least 256 tiles, if tiles of sixteen give them
     const int64_t each = n / (adapters > 1 ? adapters : 1);
+    // (a row's A is read for each of the column blocks)
+    p.one = !grad && adapters > 0 && n <= (adapters > 1 ? AD_ONE_ROWS : AD_ONE_SAME) && rank <= 64 &&
+            n * ad_column_blocks(dout, (int)vec_bytes(type)) * rank * din * (int64_t)vec_bytes(type) <= AD_ONE_BYTES;
     const bool sort = adapters > 1 && n > AD_FEW_ROWS && each > 1;
     p.sorted = grad || sort;
+    // as many positions a tile as the adapters have rows on average, at most
     p.tp = rank <= 32 && din >= 8 && dout >= 8 ? 64 : 32;  // (of k_vec_ad_up's other form at most 32)
-    while (p.tp > 16 && (p.tp > each || n / p.tp < 256)) p.tp /= 2;
+    while (p.tp > 16 && (p.tp > each || n / p.tp < AD_TILES(din, dout))) p.tp /= 2;
     p.tp_up = p.tp;
     p.few = p.sorted && each * rank < AD_UP_FEW;
     if (p.few) {  // tiles of up to eight, fewer where there would be too few waves
@@ -49,18 +71,15 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
         while (p.tp_up > 1 && (n + p.tp_up - 1) / p.tp_up * across < 1024) p.tp_up /= 2;
     }
     if (adapters > 1 && !p.sorted) p.tp = p.tp_up = 1;
-    // (a row's A is read for each of the column blocks)
-    p.one = !grad && !p.sorted && adapters > 0 && n <= (adapters > 1 ? AD_FEW_ROWS : 8) && rank <= 64 &&
-            n * ad_column_blocks(dout, (int)vec_bytes(type)) * rank * din * (int64_t)vec_bytes(type) <= AD_ONE_BYTES;
     p.grouped = n <= AD_GROUP_ROWS && adapters <= AD_GROUP_ADAPTERS;
     p.rp = (rank + 15) & ~15;
     const int d = grad ? dout : din;
     const int64_t tiles = (n + p.tp - 1) / p.tp;
     p.waves = d >= 1024 && rank <= 64 ? 8 : 4;
-    p.own = p.sorted && each * d < AD_OWN;
-    // about 1024 waves, each with at least two turns of 64 columns
+    p.own = p.sorted && d <= AD_OWN_COLUMNS && each * d < AD_OWN;
+    // (a wave of a slab has at least two turns of 64 columns)
     const int64_t active = tiles * p.waves;
-    int64_t slabs = active >= 1024 ? 1 : 1024 / active;
+    int64_t slabs = active >= AD_WAVES ? 1 : AD_WAVES / active;
     const int64_t most = d / (p.own ? 256 : p.waves * 64);
     if (slabs > most) slabs = most;
     if (slabs > AD_MAX_SLABS) slabs = AD_MAX_SLABS;
@@ -237,7 +256,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     }
     if (adapters > 0) {
         const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
-        // about 16,384 blocks at most: of 1000 adapters most have nothing to join (WIDEJOIN us with a block for each 2048 values of 4096 x 16, NARROWJOIN so)
+        // about 16,384 blocks at most: of 1000 adapters most have nothing to join (4096 rows of 1000, 1001 and 700 columns at rank 12: 33 us with a block for each 2048 values, 22 so)
         int64_t across = (pieces + 255) / 256;
         if (across > 8192 / adapters + 1) across = 8192 / adapters + 1;
         const dim3 grid((unsigned)across, (unsigned)adapters, 2);

@@ -56,6 +56,18 @@ def test_sorted_rows(qb, n, din, dout, r, adapters, kind, p, t, to):
 
 @pytest.mark.parametrize("t,to", [(BF16, F32), (F16, F16), (F32, F32)])
 @pytest.mark.parametrize("n,din,dout,r,adapters,kind,p", [
+    (65, 512, 300, 16, 5, "some", 0.0), (256, 130, 72, 64, 1, "some", 0.0), (257, 130, 72, 64, 1, "some", 0.0),         # one launch and two, of one adapter
+    (2048, 40, 24, 7, 9, "outside", 0.0), (2049, 40, 24, 7, 9, "outside", 0.0), (1500, 3, 2, 60, 2, "alternate", 0.0),  # of several
+    (640, 1024, 512, 32, 20, "skew", 0.0), (641, 1024, 1026, 32, 20, "skew", 0.0),                                      # 40 MB of A, more
+    (256, 300, 200, 20, 8, "even", 0.1), (257, 300, 200, 20, 8, "even", 0.1), (256, 1200, 9, 100, 8, "skew", 0.0), (256, 24, 2050, 200, 3, "some", 0.5),  # unsorted, sorted
+    (4100, 2050, 2049, 8, 3, "skew", 0.0), (2100, 4100, 40, 33, 20, "even", 0.1)])                                     # few large tiles
+def test_between_forms(qb, n, din, dout, r, adapters, kind, p, t, to):
+    check(qb, n, din, dout, r, adapters, kind, t, to, p)
+
+
+@pytest.mark.parametrize("t,to", [(BF16, F32), (F16, F16), (F32, F32)])
+@pytest.mark.parametrize("n,din,dout,r,adapters,kind,p", [
+    (4100, 2050, 2049, 8, 3, "skew", 0.1), (700, 40, 2049, 16, 100, "even", 0.0), (700, 40, 2048, 16, 100, "even", 0.0),
     (79, 84, 3201, 4, 38, "even", 0.1), (40, 2000, 1500, 16, 200, "even", 0.0), (64, 3, 700, 9, 5, "skew", 0.5), (100, 600, 2, 33, 50, "some", 0.0), (33, 2, 3, 70, 8, "even", 0.5),
     (2100, 264, 136, 16, 130, "even", 0.1), (66_000, 24, 40, 4, 100, "skew", 0.1), (9000, 16, 24, 4, 4096, "even", 0.0), (70_000, 8, 8, 2, 65_535, "runs", 0.0),
     (4096, 1030, 514, 17, 2, "alternate", 0.1), (1025, 72, 40, 64, 600, "skew", 0.25)])
