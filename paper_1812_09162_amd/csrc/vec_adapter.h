@@ -464,6 +464,89 @@ k_vec_ad_down(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix m, co
     }
 }
 
+// -------------------------------------------------------------------- join --
+// What `outer` leaves of a gradient: sums of parts of a run.
+struct AdOuter {
+    void *out;
+    int64_t ld, stride;   // of rows, of adapters
+    float *part;          // [chunk][2][rank][dpad]
+    int dpad, accumulate;
+};
+// The sums of ids whose positions several blocks held, and zeros for those without a row; both gradients in one launch, of its own or behind `up`'s blocks.
+struct AdJoin {
+    AdOuter o;
+    int len, d;
+};
+struct AdJoins {
+    AdJoin a, b;
+    const uint32_t *starts;  // where the adapters' positions begin, or null
+    int rank, narrow;        // narrow: the gradients are of type T, else float32
+    int across;              // blocks of an adapter
+};
+template <class O>
+__device__ __forceinline__ void ad_join_write(O *out, int left, int col, vec_f8 sum, bool accumulate) {
+    if (accumulate) sum += vec_wide<O>(vec_load<O>(out, left, col));
+    vec_store<O>(out, left, sum);
+}
+template <class T>
+__device__ __forceinline__ void ad_join(const AdRows &rows, const AdJoins &js, int64_t block) {
+    const int64_t per = (int64_t)js.across * rows.adapters;
+    if (block >= 2 * per) return;
+    const AdJoin &j = block >= per ? js.b : js.a;
+    if (block >= per) block -= per;
+    const AdOuter &o = j.o;
+    __shared__ int64_t found[2];
+    const uint32_t e = (uint32_t)(block / js.across), part = (uint32_t)(block - (int64_t)e * js.across);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (js.starts) {
+        if (threadIdx.x < 2) found[threadIdx.x] = js.starts[e + threadIdx.x];
+    } else if (wave < 2) {  // the first position whose key is at least e (at least e + 1), a 64th of what is left a round
+        int64_t lo = 0, hi = rows.n;
+        while (lo < hi) {
+            const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
+            const uint64_t below = __ballot(p < hi && rows.keys[p < hi ? p : lo] < e + wave);  // (a prefix of the lanes)
+            const int k = __popcll(below);
+            if (k == 0) break;
+            hi = lo + k * step < hi ? lo + k * step : hi;
+            lo += (k - 1) * step + 1;
+        }
+        if (lane == 0) found[wave] = lo;
+    }
+    __syncthreads();
+    const int64_t lo = found[0], hi = found[1];
+    // (len is a power of two)
+    const int shift = __builtin_ctz(j.len);
+    const int64_t from = lo >> shift, to = lo < hi ? (hi - 1) >> shift : 0;
+    if (lo < hi ? from == to : o.accumulate) return;
+    const int pieces = o.dpad / 8;
+    for (uint32_t i = part * 256 + threadIdx.x; i < (uint32_t)js.rank * pieces; i += js.across * 256) {  // (at most 2^25)
+        const int r = (int)(i / (uint32_t)pieces), col = (int)(i - (uint32_t)r * pieces) * 8;
+        vec_f8 sum = (vec_f8)0.0f;
+        if (lo < hi) {
+            const int64_t each = 2 * (int64_t)js.rank * o.dpad;
+            const float *p = o.part + (int64_t)r * o.dpad + col;
+            sum = *(const vec_f8 *)(p + from * each + each / 2);
+            int64_t k = from + 1;
+            for (; k + 8 <= to + 1; k += 8) {
+                vec_f8 v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[u] = *(const vec_f8 *)(p + (k + u) * each);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) sum += v[u];
+            }
+            for (; k <= to; ++k) sum += *(const vec_f8 *)(p + k * each);
+        }
+        const int64_t at = e * o.stride + r * o.ld + col;
+        if (js.narrow) ad_join_write((T *)o.out + at, j.d - col, col, sum, o.accumulate);
+        else ad_join_write((float *)o.out + at, j.d - col, col, sum, o.accumulate);
+    }
+}
+template <class T>
+__global__ void __launch_bounds__(256)
+k_vec_ad_join(AdRows rows, AdJoins js) {
+    ad_join<T>(rows, js, vec_block());
+}
+
 // ---------------------------------------------------------------------- up --
 // y_row = base_row + (kept) f_row W_e.  A block takes a tile of positions and 64 AD_COLS columns at a time, a quarter a wave.  The factor f is made ready
 // in LDS once (its parts as the matrix cores take them); a lane reads eight ranks of AD_COLS columns of W, whose columns are put together from
@@ -653,9 +736,12 @@ struct AdUpPass {
     }
 };
 
-template <class T, class Y, bool MASK, bool ONE, int E>  // ONE: at most 32 ranks
+// ONE: at most 32 ranks.  JOIN: blocks behind `blocks` join the gradients of the factors, which nothing here reads, so that a launch is saved.
+template <class T, class Y, bool MASK, bool ONE, int E, bool JOIN>
 __global__ void __launch_bounds__(256, 2)
-k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y, VecMask mask, int column_blocks, float *__restrict__ keep) {
+k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y, VecMask mask, int column_blocks, float *__restrict__ keep,
+            int64_t blocks, AdJoins js) {
+    if (JOIN && vec_block() >= blocks) return ad_join<T>(rows, js, vec_block() - blocks);
     extern __shared__ __align__(16) unsigned char smem[];
     ad_u4 *ready = (ad_u4 *)smem;  // [chunk][tile][part][lane]
     __shared__ uint32_t lists[4][64];
@@ -699,10 +785,11 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
 // factor, columns put together, LDS) costs more than these products: 8192 mixed rows of 500 adapters, 1001 fp16
 // columns at rank 8: 41 us above, 24 here; 16,384 of 1000, 4096 bf16 columns at rank 16: 104 above, 128 here.
 #define AD_FEW_POSITIONS 8
-template <class T, class Y, bool MASK, int E>
+template <class T, class Y, bool MASK, int E, bool JOIN>
 __global__ void __launch_bounds__(256, 2)
 k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t f_stride, int f_slabs, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y,
-                VecMask mask, int column_blocks, float *__restrict__ keep) {
+                VecMask mask, int column_blocks, float *__restrict__ keep, int64_t blocks, AdJoins js) {
+    if (JOIN && vec_block() >= blocks) return ad_join<T>(rows, js, vec_block() - blocks);
     const int lane = threadIdx.x & 63;
     const int64_t item = vec_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = item / column_blocks;
     if (at * rows.tp >= rows.n) return;
@@ -797,15 +884,15 @@ k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t 
 }
 
 // ------------------------------------------------------------ single tokens --
-// Both products in one launch, for rows of their own adapters without dropout: a block takes a row and 64 AD_COLS columns of the result, and makes the row's t itself, so
+// Both products in one launch, for rows of their own adapters: a block takes a row and 64 AD_COLS columns of the result, and makes the row's t itself, so
 // that A is read once for each of these (from the L2 cache).  Its eight waves share the columns of x, AD_ONE_TILES KB of A on their way each, then the ranks of B, which is asked
 // for before.  4096 x 4096 bf16 at rank 16, us in a graph by two
 // kernels / by this: 1 row 8.8 / 5.4, 16 9.1 / 5.6, 32 (33 MB of A read) 8.6 / 6.8, 64 (67 MB) 9.9 / 12.5; 16 rows at rank 64 10.7 / 16.5.
 #define AD_ONE_TILES 4
 template <class T, class Y, int RK, int E>
 __global__ void __launch_bounds__(512)
-k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, AdMatrix mb, const float *__restrict__ scales, const Y *base, int64_t ld_base, Y *y,
-             int64_t ld_y, float *__restrict__ keep, int column_blocks) {
+k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, AdMatrix mb, const float *__restrict__ scales, float factor, VecMask mask, const Y *base,
+             int64_t ld_base, Y *y, int64_t ld_y, float *__restrict__ keep, int column_blocks) {
     constexpr int EA = AD_COLS(T), COLS = 8 * EA, KS = COLS / 32, U = AD_ONE_TILES / RK, BR = 2 * RK;  // U: turns on their way; BR: ranks of B a wave
     constexpr int LDS = 8 * U * RK * 128;
     __shared__ ad_u4 tiles[LDS > 32 * E * 4 ? LDS : 32 * E * 4];  // [wave][turn][16 ranks][16 rows][8 pieces]; [wave][64 E] sums
@@ -842,7 +929,12 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
         for (int h = 0; h < 2; ++h) ar[j][h] = a + (int64_t)(16 * j + 8 * h + lr < rank ? 16 * j + 8 * h + lr : rank - 1) * ma.ld;
     vec_pack<T, EA> v[U][RK][2];
     vec_pack<T> xv[U][KS];
-    auto multiply = [&](int u) {
+    VecKey key = {0, 0, 0};
+    if (mask.threshold) key = vec_key(mask);
+    auto multiply = [&](int u, int k) {  // k: the turn's first column
+        if (mask.threshold)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) xv[u][ks] = vec_drop<T>(xv[u][ks], vec_kept(vec_random(key, mask.layer, (uint32_t)row, (uint32_t)(k + 32 * ks + 8 * g) >> 3), mask.threshold));
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -883,7 +975,7 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
             if (i + u < whole) put(u);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u < whole) multiply(u);
+            if (i + u < whole) multiply(u, first + (i + u) * span);
     }
     if (first + whole * span < d) {
         const int k = first + whole * span, ca = k + EA * lp;
@@ -897,7 +989,7 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
             xv[0][ks] = vec_load<T>(xr + (cx < d ? cx : 0), d - cx, cx);
         }
         put(0);
-        multiply(0);
+        multiply(0, k);
     }
     if (c == 0)  // (all sixteen columns of the products are the row)
 #pragma unroll
@@ -907,7 +999,7 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
         float s = 0.0f;
 #pragma unroll
         for (int u = 0; u < 8; ++u) s += sums[u][threadIdx.x];
-        s = (int)threadIdx.x < rank ? s * (scales ? scales[e] : 1.0f) : 0.0f;
+        s = (int)threadIdx.x < rank ? s * (scales ? scales[e] * factor : factor) : 0.0f;
         t[threadIdx.x] = s;
         if (keep && slab == 0 && (int)threadIdx.x < rank) keep[row * rank + threadIdx.x] = s;
     }
@@ -938,12 +1030,6 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
 // positions whatever runs of equal ids these hold: the rows of a step are read once, and each run among them takes its own and zeros for the others.  Runs that lie within the block's positions are written; the others' sums go to part[chunk][0] (began before)
 // or part[chunk][1], which k_vec_ad_join adds up in order.  Per step a lane reads eight rows of AD_COLS columns.
 #define AD_STAGE 128  // positions whose factors are made ready at once
-struct AdOuter {
-    void *out;
-    int64_t ld, stride;   // of rows, of adapters
-    float *part;          // [chunk][2][rank][dpad]
-    int dpad, accumulate;
-};
 template <class O, int E>
 __device__ __forceinline__ void ad_put(O *row, int col, int d, vec_f<E> v, bool accumulate) {
     if (accumulate) v += vec_wide<O, E>(ad_load<O, E>(row, ad_from<E>(col, d)));
@@ -1106,63 +1192,6 @@ k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_
 #pragma unroll
             for (int q = 0; q < 8; ++q) raw[q] = next[q];
         }
-    }
-}
-
-// The sums of ids whose positions several blocks held, and zeros for those without a row; both gradients in one launch (blockIdx.z).
-struct AdJoin {
-    AdOuter o;
-    int len, d;
-};
-template <class O>
-__global__ void __launch_bounds__(256)
-k_vec_ad_join(AdRows rows, int rank, const uint32_t *__restrict__ starts, AdJoin ja, AdJoin jb) {
-    const AdJoin &j = blockIdx.z ? jb : ja;
-    const AdOuter &o = j.o;
-    __shared__ int64_t found[2];
-    const uint32_t e = blockIdx.y;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (starts) {
-        if (threadIdx.x < 2) found[threadIdx.x] = starts[e + threadIdx.x];
-    } else if (wave < 2) {  // the first position whose key is at least e (at least e + 1), a 64th of what is left a round
-        int64_t lo = 0, hi = rows.n;
-        while (lo < hi) {
-            const int64_t step = (hi - lo + 63) / 64, p = lo + lane * step;
-            const uint64_t below = __ballot(p < hi && rows.keys[p < hi ? p : lo] < e + wave);  // (a prefix of the lanes)
-            const int k = __popcll(below);
-            if (k == 0) break;
-            hi = lo + k * step < hi ? lo + k * step : hi;
-            lo += (k - 1) * step + 1;
-        }
-        if (lane == 0) found[wave] = lo;
-    }
-    __syncthreads();
-    const int64_t lo = found[0], hi = found[1];
-    // (len is a power of two)
-    const int shift = __builtin_ctz(j.len);
-    const int64_t from = lo >> shift, to = lo < hi ? (hi - 1) >> shift : 0;
-    if (lo < hi ? from == to : o.accumulate) return;
-    const int pieces = o.dpad / 8;
-    for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < (uint32_t)rank * pieces; i += gridDim.x * 256) {  // (at most 2^25)
-        const int r = (int)(i / (uint32_t)pieces), col = (int)(i - (uint32_t)r * pieces) * 8;
-        vec_f8 sum = (vec_f8)0.0f;
-        if (lo < hi) {
-            const int64_t each = 2 * (int64_t)rank * o.dpad;
-            const float *p = o.part + (int64_t)r * o.dpad + col;
-            sum = *(const vec_f8 *)(p + from * each + each / 2);
-            int64_t k = from + 1;
-            for (; k + 8 <= to + 1; k += 8) {
-                vec_f8 v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = *(const vec_f8 *)(p + (k + u) * each);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) sum += v[u];
-            }
-            for (; k <= to; ++k) sum += *(const vec_f8 *)(p + k * each);
-        }
-        O *out = (O *)o.out + e * o.stride + r * o.ld + col;
-        if (o.accumulate) sum += vec_wide<O>(vec_load<O>(out, j.d - col, col));
-        vec_store<O>(out, j.d - col, sum);
     }
 }
 

@@ -10,7 +10,7 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 // Rows that are not sorted: each reads its adapter for itself, mostly from the caches.  Sorted / not: 128 x 4096 at rank 16 18.8 / 13.9, 256 x 4096 20.7 / 20.0, 128 x 2048 at rank 64
 // 27 / 13, 256 24 / 19, 512 x 2048 at rank 16 15.9 / 22.1.
 #define AD_FEW_ROWS 256
-// Single rows in one launch (without dropout): what they read of A altogether, from the L2 cache, and how many they are (of one adapter the other form has whole tiles).  By two kernels /
+// Single rows in one launch: what they read of A altogether, from the L2 cache, and how many they are (of one adapter the other form has whole tiles).  By two kernels /
 // by one: 64 x 4096 at rank 16 (67 MB) 9.9 / 12.5, 512 x 1024 at rank 16 (34 MB) 15.6 / 7.8, 2048 x 256 at rank 8 14.9 / 10.6, 4096 15.5 / 18.9; of one adapter 16 x 4096 9.0 / 5.6,
 // 256 x 1024 8.4 / 5.1.
 #define AD_ONE_BYTES (40 << 20)
@@ -33,7 +33,7 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 struct AdPlan {
     bool sorted, grouped;      // grouped: by k_vec_ad_group
     bool few;                  // `up` on the vector units
-    bool one;                  // without dropout: single rows in one launch
+    bool one;                  // single rows in one launch
     int tp, tp_up;             // positions of a tile of `down`, of `up`
     int rp;                    // ranks of a row of partial sums
     int waves, slabs, per;     // of the contraction over columns
@@ -182,9 +182,9 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
     float *part = nullptr;
     const VecMask mask = {state, layer, threshold}, none = {nullptr, 0, 0};
     if (adapters > 0) AD_WORKSPACE("vec_adapter", plan.total);
-    if (plan.one && threshold == 0) {
+    if (plan.one) {
         const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
-        VEC_TYPED(type, T, AdLaunch<T>::one(rows, x, ld_x, ma, mb, scales, base, ld_base, y, ld_y, y_type == type, t, s));
+        VEC_TYPED(type, T, AdLaunch<T>::one(rows, x, ld_x, ma, mb, scales, factor, mask, base, ld_base, y, ld_y, y_type == type, t, s));
         QADC_LAUNCH_CHECK("k_vec_ad_one");
         return PQ_OK;
     }
@@ -199,7 +199,7 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
     rows.tp = plan.tp_up;
     const AdFactor f = {part, plan.rp, n * plan.rp, plan.slabs};
     const AdMatrix m = {b, ld_b, stride_b, rank, dout};
-    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, plan.few, ad_up_blocks(n, plan.tp_up, dout, type), keep, s));
+    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, plan.few, ad_up_blocks(n, plan.tp_up, dout, type), keep, nullptr, s));
     QADC_LAUNCH_CHECK("vec_adapter's kernels");
     return PQ_OK;
 }
@@ -231,14 +231,15 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     plan.dpad_a = (din + 7) & ~7;
     plan.dpad_b = (dout + 7) & ~7;
     const uint32_t *starts = nullptr;
+    const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
+    AdFactor u = {};
     AdOuter oa = {da, ld_da, stride_da, nullptr, plan.dpad_a, accumulate}, ob = {db, ld_db, stride_db, nullptr, plan.dpad_b, accumulate};
     if (n > 0) {
         plan = ad_plan(n, din, dout, rank, adapters, type, true);
         rows.tp = plan.tp;
         VEC_REQUIRE(ad_fits(plan, n, din, type) && (n / plan.len_a + 1) * ad_outer_blocks(din, dout) + (n / plan.len_b + 1) * ad_outer_blocks(dout, din) <= VEC_MAX_BLOCKS, "vec_adapter_grad: n=%lld too large for one call", (long long)n);
         char *ws = (char *)workspace;
-        const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
-        AdFactor u = {nullptr, plan.rp, n * plan.rp, plan.slabs};
+        u = {nullptr, plan.rp, n * plan.rp, plan.slabs};
         if (adapters > 0) {
             AD_WORKSPACE("vec_adapter_grad", plan.total);
             float *part = (float *)(ws + plan.part);
@@ -251,17 +252,17 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
                       AdLaunch<T>::outer(rows, rank, mask, sb, sa, narrow, s));
         }
         rows.tp = plan.tp_up;
-        if (dx)
-            VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, mask, plan.few, ad_up_blocks(n, plan.tp_up, din, type), nullptr, s));
     }
-    if (adapters > 0) {
-        const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
-        // about 16,384 blocks at most: of 1000 adapters most have nothing to join (4096 rows of 1000, 1001 and 700 columns at rank 12: 33 us with a block for each 2048 values, 22 so)
-        int64_t across = (pieces + 255) / 256;
-        if (across > 8192 / adapters + 1) across = 8192 / adapters + 1;
-        const dim3 grid((unsigned)across, (unsigned)adapters, 2);
-        const AdJoin ja = {oa, plan.len_a, din}, jb = {ob, plan.len_b, dout};
-        VEC_TYPED(grad_type, O, hipLaunchKernelGGL((k_vec_ad_join<O>), grid, dim3(256), 0, s, rows, rank, starts, ja, jb));
+    AdJoins joins = {{oa, plan.len_a, din}, {ob, plan.len_b, dout}, starts, rank, narrow, 1};
+    const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
+    // about 16,384 blocks at most: of 1000 adapters most have nothing to join (4096 rows of 1000, 1001 and 700 columns at rank 12: 33 us with a block for each 2048 values, 22 so)
+    joins.across = (int)((pieces + 255) / 256);
+    if (adapters > 0 && joins.across > 8192 / adapters + 1) joins.across = 8192 / adapters + 1;
+    if (n > 0 && dx) {
+        VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, adapters > 0 ? mask : none, plan.few, ad_up_blocks(n, plan.tp_up, din, type),
+                                           nullptr, adapters > 0 ? &joins : nullptr, s));
+    } else if (adapters > 0) {
+        VEC_TYPED(type, T, AdLaunch<T>::join(rows, joins, s));
     }
     QADC_LAUNCH_CHECK("vec_adapter_grad's kernels");
     return PQ_OK;

@@ -11,12 +11,14 @@ template <class T>
 struct AdLaunch {
     static void down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
                      int64_t part_stride, int rp, int waves, int slabs, int per, bool own, float *keep, hipStream_t s);
-    // narrow: the result is of type T, else float32
+    // narrow: the result is of type T, else float32; joins: of the gradients of the factors in the same launch, or null; a mask or joins only with
+    // a narrow result, a mask only with joins (a gradient of x)
     static void up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                   const VecMask &mask, bool few, int column_blocks, float *keep, hipStream_t s);
+                   const VecMask &mask, bool few, int column_blocks, float *keep, const AdJoins *joins, hipStream_t s);
     // both products for single rows, of at most 64 ranks
-    static void one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, const void *base, int64_t ld_base, void *y,
-                    int64_t ld_y, bool narrow, float *keep, hipStream_t s);
+    static void one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, float factor, const VecMask &mask,
+                    const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow, float *keep, hipStream_t s);
+    static void join(const AdRows &rows, const AdJoins &joins, hipStream_t s);
     static void outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, hipStream_t s);
 };
 
@@ -51,24 +53,36 @@ void AdLaunch<T>::down(const AdRows &rows, const void *x, int64_t ld_x, const Ad
 #undef GO2
 }
 
+static int64_t ad_join_blocks(const AdRows &rows, const AdJoins &joins) { return 2ll * joins.across * rows.adapters; }
+
+template <class T>
+void AdLaunch<T>::join(const AdRows &rows, const AdJoins &joins, hipStream_t s) {
+    hipLaunchKernelGGL((k_vec_ad_join<T>), vec_grid(ad_join_blocks(rows, joins), 256), dim3(256), 0, s, rows, joins);
+}
+
 template <class T>
 void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                     const VecMask &mask, bool few, int column_blocks, float *keep, hipStream_t s) {
+                     const VecMask &mask, bool few, int column_blocks, float *keep, const AdJoins *joins, hipStream_t s) {
+    const int64_t tiles = (rows.n + rows.tp - 1) / rows.tp;
+    const AdJoins js = joins ? *joins : AdJoins{};
+    const int64_t more = joins ? ad_join_blocks(rows, js) : 0;
     if (few) {
-        const int64_t tiles = (rows.n + rows.tp - 1) / rows.tp;
         const int cb = ad_column_blocks(m.d, (int)sizeof(T));
-        const dim3 grid = vec_grid((tiles * cb + 3) / 4, 256);
-#define GO(Y, M, E)                                                                                                        \
-    hipLaunchKernelGGL((k_vec_ad_up_few<T, Y, M, E>), grid, dim3(256), 0, s, rows, f.p, f.ld, f.stride, f.slabs, m, (const Y *)base, ld_base, (Y *)y, \
-                       ld_y, mask, cb, keep)
-#define GO2(Y, M)                                              \
+        const int64_t blocks = (tiles * cb + 3) / 4;
+        const dim3 grid = vec_grid(blocks + more, 256);
+#define GO(Y, M, E, J)                                                                                                     \
+    hipLaunchKernelGGL((k_vec_ad_up_few<T, Y, M, E, J>), grid, dim3(256), 0, s, rows, f.p, f.ld, f.stride, f.slabs, m, (const Y *)base, ld_base, (Y *)y, \
+                       ld_y, mask, cb, keep, blocks, js)
+#define GO2(Y, M, J)                                           \
     do {                                                       \
-        if (m.d < AD_COLS(T)) GO(Y, M, 1);                     \
-        else GO(Y, M, AD_COLS(T));                             \
+        if (m.d < AD_COLS(T)) GO(Y, M, 1, J);                  \
+        else GO(Y, M, AD_COLS(T), J);                          \
     } while (0)
-        if (mask.threshold) GO2(T, true);
-        else if (narrow) GO2(T, false);
-        else GO2(float, false);
+        if (joins) {
+            if (mask.threshold) GO2(T, true, true);
+            else GO2(T, false, true);
+        } else if (narrow) GO2(T, false, false);
+        else GO2(float, false, false);
 #undef GO2
 #undef GO
         return;
@@ -76,36 +90,40 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
     // Eight bytes a lane where sixteen leave few blocks: half the registers and twice the waves.  us with sixteen / eight: 16,384 x 2048 at rank 32 (1024 blocks) 36 / 29, 10,000 x
     // 1001 at rank 12 (1252) 32 / 25; 16,384 x 4096 at rank 16 (2048) 53 / 53, of 1000 adapters (8192) 104 / 131; single rows of 4096 5.4 / 5.9.  With a mask each of two
     // neighbouring lanes would make it: 70 / 91.
-    const int64_t tiles = (rows.n + rows.tp - 1) / rows.tp;
     const bool half = sizeof(T) == 2 && m.rank <= 32 && !mask.threshold && m.d >= AD_COLS(T) && rows.tp >= 16 && tiles * ad_column_blocks(m.d, 2) < 2048;
     if (half) column_blocks = ad_blocks(m.d, 4);
-    const dim3 grid = ad_grid(rows, column_blocks, 256);
+    const int64_t blocks = tiles * column_blocks;
+    const dim3 grid = vec_grid(blocks + more, 256);
     const size_t lds = (size_t)((m.rank + 31) / 32) * ((rows.tp + 15) / 16) * AdWide<T>::parts * 1024;
-#define GO(Y, M, ONE, E)                                                                                                   \
-    hipLaunchKernelGGL((k_vec_ad_up<T, Y, M, ONE, E>), grid, dim3(256), lds, s, rows, f, m, (const Y *)base, ld_base, (Y *)y, ld_y, mask, column_blocks, keep)
-#define GO2(Y, M)                                                                                                          \
+#define GO(Y, M, ONE, E, J)                                                                                                \
+    hipLaunchKernelGGL((k_vec_ad_up<T, Y, M, ONE, E, J>), grid, dim3(256), lds, s, rows, f, m, (const Y *)base, ld_base, (Y *)y, ld_y, mask, column_blocks, keep, blocks, js)
+#define GO2(Y, M, J)                                                                                                       \
     do {                                                                                                                   \
-        if (m.d < AD_COLS(T)) GO(Y, M, false, 1);                                                                          \
-        else if (m.rank <= 32) GO(Y, M, true, AD_COLS(T));                                                                 \
-        else GO(Y, M, false, AD_COLS(T));                                                                                              \
+        if (m.d < AD_COLS(T)) GO(Y, M, false, 1, J);                                                                       \
+        else if (m.rank <= 32) GO(Y, M, true, AD_COLS(T), J);                                                              \
+        else GO(Y, M, false, AD_COLS(T), J);                                                                               \
     } while (0)
     if (half) {
-        if (narrow) GO(T, false, true, 4);
-        else GO(float, false, true, 4);
-    } else if (mask.threshold) GO2(T, true);  // (a gradient of x, which is of its type)
-    else if (narrow) GO2(T, false);
-    else GO2(float, false);
+        if (joins) GO(T, false, true, 4, true);
+        else if (narrow) GO(T, false, true, 4, false);
+        else GO(float, false, true, 4, false);
+    } else if (joins) {
+        if (mask.threshold) GO2(T, true, true);
+        else GO2(T, false, true);
+    } else if (narrow) GO2(T, false, false);
+    else GO2(float, false, false);
 #undef GO2
 #undef GO
 }
 
 template <class T>
-void AdLaunch<T>::one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, const void *base, int64_t ld_base, void *y,
-                      int64_t ld_y, bool narrow, float *keep, hipStream_t s) {
+void AdLaunch<T>::one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, float factor, const VecMask &mask,
+                      const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow, float *keep, hipStream_t s) {
     const int cb = ad_column_blocks(b.d, (int)sizeof(T));
     const dim3 grid = vec_grid(rows.n * cb, 512);
 #define GO(Y, RK, E)                                                                                                       \
-    hipLaunchKernelGGL((k_vec_ad_one<T, Y, RK, E>), grid, dim3(512), 0, s, rows, (const T *)x, ld_x, a, b, scales, (const Y *)base, ld_base, (Y *)y, ld_y, keep, cb)
+    hipLaunchKernelGGL((k_vec_ad_one<T, Y, RK, E>), grid, dim3(512), 0, s, rows, (const T *)x, ld_x, a, b, scales, factor, mask, (const Y *)base, ld_base, (Y *)y, ld_y, \
+                       keep, cb)
 #define GO2(Y)                                                 \
     do {                                                       \
         if (b.d < AD_COLS(T)) GO(Y, 4, 1);                     \
