@@ -65,10 +65,12 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     while (p.tp > 16 && (p.tp > each || n / p.tp < AD_TILES(din, dout))) p.tp /= 2;
     p.tp_up = p.tp;
     p.few = p.sorted && each * rank < AD_UP_FEW;
-    if (p.few) {  // tiles of up to eight, fewer where there would be too few waves
+    // tiles of up to eight, fewer where there would be too few waves (with 1024 / 2048 / 4096 waves at least: 4096 rows of 500 at rank 8, 1001 fp16 columns, 41 / 37 / 40; 4096 of
+    // 1000 at rank 16, 512 columns, 36 / 31 / 32; 8192 of 500 at rank 8, 512 columns, 28 / 25 / 28)
+    if (p.few) {
         const int64_t across = ad_column_blocks(grad ? din : dout, (int)vec_bytes(type));
         p.tp_up = AD_FEW_POSITIONS;
-        while (p.tp_up > 1 && (n + p.tp_up - 1) / p.tp_up * across < 1024) p.tp_up /= 2;
+        while (p.tp_up > 1 && (n + p.tp_up - 1) / p.tp_up * across < 2048) p.tp_up /= 2;
     }
     if (adapters > 1 && !p.sorted) p.tp = p.tp_up = 1;
     p.grouped = n <= AD_GROUP_ROWS && adapters <= AD_GROUP_ADAPTERS;
@@ -77,14 +79,15 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     const int64_t tiles = (n + p.tp - 1) / p.tp;
     p.waves = d >= 1024 && rank <= 64 ? 8 : 4;
     p.own = p.sorted && d <= AD_OWN_COLUMNS && each * d < AD_OWN;
-    // (a wave of a slab has at least two turns of 64 columns)
-    const int64_t active = tiles * p.waves;
+    // A wave of a slab has at least two turns of 64 columns.  Of waves with an adapter each about two have one (one slab / so: 4096 rows of 500 at rank 8, 1001 fp16 columns, 41 / 37; 4096
+    // of 1000 at rank 16, 512 columns, 36 / 33; slabs at 8192 rows of 500, 512 columns, too 28 / 29).
+    const int64_t active = tiles * (p.own ? 2 : p.waves);
     int64_t slabs = active >= AD_WAVES ? 1 : AD_WAVES / active;
-    const int64_t most = d / (p.own ? 256 : p.waves * 64);
+    const int64_t most = d / (p.own ? 128 : p.waves * 64);
     if (slabs > most) slabs = most;
     if (slabs > AD_MAX_SLABS) slabs = AD_MAX_SLABS;
     if (slabs < 1) slabs = 1;
-    const int64_t per = ((d + slabs - 1) / slabs + 255) / 256 * 256;
+    const int64_t per = ((d + slabs - 1) / slabs + 127) / 128 * 128;
     p.per = (int)per;
     p.slabs = (int)((d + per - 1) / per);
     size_t at = 0;
