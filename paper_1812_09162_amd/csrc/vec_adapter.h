@@ -201,6 +201,10 @@ __device__ __forceinline__ uint32_t ad_kept(VecKey key, const VecMask &mask, uin
     if (shift + E > 8) b |= ad_bits(key, mask, row, ((uint32_t)from >> 3) + 1) << 8;
     return b >> shift;
 }
+// The same of a position, where `outer` has kept them: a word has eight columns of four positions, [position / 4][column / 8].
+__device__ __forceinline__ uint32_t ad_bits_of(const uint32_t *bits, int64_t position, int d, int from) {
+    return bits[(position >> 2) * (d / 8) + (from >> 3)] >> (8 * ((int)position & 3) + (from & 7));
+}
 // Zeros in place of what is dropped.
 template <class T, int E>
 __device__ __forceinline__ vec_pack<T, E> ad_drop(vec_pack<T, E> v, uint32_t kept) {
@@ -216,14 +220,16 @@ __device__ __forceinline__ vec_pack<T, E> ad_drop(vec_pack<T, E> v, uint32_t kep
         return v;
     }
 }
-// The same for eight rows.  whole: the wave's columns are all there; neighbouring lanes that hold halves of eight columns then make four rows' bits each.
-template <class T, int E, class ROW>
-__device__ __forceinline__ void ad_drop8(vec_pack<T, E> *v, VecKey key, const VecMask &mask, ROW row, int from, bool whole) {
+// The same for eight rows.  whole: lanes have their own columns, all that are stored; neighbouring lanes that hold halves of eight columns then make four rows' bits each, and
+// `store` takes these.
+template <class T, int E, class ROW, class STORE>
+__device__ __forceinline__ void ad_drop8(vec_pack<T, E> *v, VecKey key, const VecMask &mask, ROW row, int from, bool whole, STORE store) {
     if (E == 4 && whole) {
         const int half = threadIdx.x & 1;
         uint32_t mine = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) mine |= ad_bits(key, mask, row(4 * half + q), (uint32_t)from >> 3) << (8 * q);
+        store(half, mine);
         const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0xb1, 0xf, 0xf, true);  // (of the lane beside)
         const uint32_t low = half ? other : mine, high = half ? mine : other;
 #pragma unroll
@@ -553,7 +559,8 @@ k_vec_ad_join(AdRows rows, AdJoins js) {
 // their halves by byte permutations.  The products' 16 rows pass through LDS, so that sixteen neighbouring lanes read and write a row's 256 bytes: from
 // the matrix cores' own order, where neighbouring lanes hold different rows, every sixteen bytes would be an access of their own (16,384 x 4096 bf16 at rank 16 60 us, 53
 // this way: 268 MB, the rate of a large copy).
-template <class T, class Y, bool MASK, int E>
+// MASK: 0 without dropout, 1 the mask is made here, 2 its bits are read.
+template <class T, class Y, int MASK, int E>
 struct AdUp {
     static constexpr int LD = 16 * E + 4;  // floats between two rows in LDS (lanes of a quarter wave then write to different banks)
     const Y *base;
@@ -561,6 +568,7 @@ struct AdUp {
     int64_t ld_base, ld_y;
     int d;
     VecMask mask;
+    const uint32_t *bits;
     VecKey key;
     float *lds;  // the wave's own [16][LD]
 
@@ -573,7 +581,7 @@ struct AdUp {
         for (int i = 0; i < 4; ++i) b[i] = ad_load<Y, E>(base + (int64_t)rows[i] * ld_base, from);
     }
     // acc[m][i]: of row lane % 16, column E (4 (lane / 16) + i) + m
-    __device__ __forceinline__ void write(const vec_f4 *acc, const vec_pack<Y, E> *b, const uint32_t *rows, int left, int c0) const {
+    __device__ __forceinline__ void write(const vec_f4 *acc, const vec_pack<Y, E> *b, const uint32_t *mask_bits, const uint32_t *rows, int left, int c0) const {
         const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, col = column(c0);
         float *to = lds + c * LD + 4 * E * g;
 #pragma unroll
@@ -602,7 +610,7 @@ struct AdUp {
             }
             if (4 * i + g >= left || col >= d) continue;
             if (MASK) {
-                const uint32_t kept = ad_kept<E>(key, mask, rows[i], ad_from<E>(col, d));
+                const uint32_t kept = MASK == 2 ? mask_bits[i] : ad_kept<E>(key, mask, rows[i], ad_from<E>(col, d));
 #pragma unroll
                 for (int m = 0; m < E; ++m) f[m] = kept >> m & 1 ? f[m] : 0.0f;
             }
@@ -642,17 +650,17 @@ __device__ __forceinline__ void ad_ready(const AdFactor &f, int rank, int chunks
 }
 
 // The rows of a list and a wave's 16 E columns from c0 on: requested, then computed.
-template <class T, class Y, bool MASK, bool ONE, int E>
+template <class T, class Y, int MASK, bool ONE, int E>
 struct AdUpPass {
     static constexpr int P = AdWide<T>::parts;
     const AdUp<T, Y, MASK, E> &up;
     const AdMatrix &m;
     const T *w;  // null: no adapter
-    const uint32_t *list;
+    const uint32_t *list, *place;
     int count, chunks, c0;
     vec_pack<T, E> raw[8];
     vec_pack<Y, E> b[4];
-    uint32_t at[4];  // the rows of b
+    uint32_t at[4], kept[4];  // the rows of b, their bits of the mask
 
     // (lanes without a rank read the last one's: their part of the factor is zero)
     __device__ __forceinline__ void weights(int kc) {
@@ -663,15 +671,25 @@ struct AdUpPass {
             raw[q] = ad_load<T, E>(w + (int64_t)(r < m.rank ? r : m.rank - 1) * m.ld, from);
         }
     }
+    __device__ __forceinline__ int entry(int t, int i) const {
+        const int k = 16 * t + 4 * i + ((threadIdx.x & 63) >> 4);
+        return k < count ? k : 0;
+    }
     __device__ __forceinline__ void rows(int t, uint32_t *to) const {
-        const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = list[16 * t + 4 * i + g < count ? 16 * t + 4 * i + g : 0];
+        for (int i = 0; i < 4; ++i) to[i] = list[entry(t, i)];
+    }
+    __device__ __forceinline__ void masks(int t, uint32_t *to) const {
+        if (MASK != 2) return;
+        const int from = ad_from<E>(up.column(c0), m.d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = ad_bits_of(up.bits, place[entry(t, i)], m.d, from);
     }
     __device__ __forceinline__ void request(int from) {
         c0 = from;
         if (w) weights(0);
         rows(0, at);
+        if (ONE) masks(0, kept);
         up.read(b, at, c0);
     }
     __device__ __forceinline__ void run(const ad_u4 *ready) {
@@ -685,9 +703,10 @@ struct AdUpPass {
         if constexpr (ONE) {
             for (int t = 0; t < tiles; ++t) {
                 vec_pack<Y, E> next[4];
-                uint32_t then[4];
+                uint32_t then[4], more[4];
                 if (t + 1 < tiles) {
                     rows(t + 1, then);
+                    masks(t + 1, more);
                     up.read(next, then, c0);
                 }
                 vec_f4 acc[E];
@@ -704,9 +723,9 @@ struct AdUpPass {
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
-                up.write(acc, b, at, count - 16 * t, c0);
+                up.write(acc, b, kept, at, count - 16 * t, c0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = next[i], at[i] = then[i];
+                for (int i = 0; i < 4; ++i) b[i] = next[i], at[i] = then[i], kept[i] = more[i];
             }
         } else {  // (tiles of at most 32 positions)
             vec_f4 acc[2][E];
@@ -726,25 +745,27 @@ struct AdUpPass {
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            up.write(acc[0], b, at, count, c0);
+            masks(0, kept);
+            up.write(acc[0], b, kept, at, count, c0);
             if (tiles > 1) {
                 rows(1, at);
+                masks(1, kept);
                 up.read(b, at, c0);
-                up.write(acc[1], b, at, count - 16, c0);
+                up.write(acc[1], b, kept, at, count - 16, c0);
             }
         }
     }
 };
 
 // ONE: at most 32 ranks.  JOIN: blocks behind `blocks` join the gradients of the factors, which nothing here reads, so that a launch is saved.
-template <class T, class Y, bool MASK, bool ONE, int E, bool JOIN>
+template <class T, class Y, int MASK, bool ONE, int E, bool JOIN>
 __global__ void __launch_bounds__(256, 2)
 k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y, VecMask mask, int column_blocks, float *__restrict__ keep,
-            int64_t blocks, AdJoins js) {
+            const uint32_t *__restrict__ bits, int64_t blocks, AdJoins js) {
     if (JOIN && vec_block() >= blocks) return ad_join<T>(rows, js, vec_block() - blocks);
     extern __shared__ __align__(16) unsigned char smem[];
     ad_u4 *ready = (ad_u4 *)smem;  // [chunk][tile][part][lane]
-    __shared__ uint32_t lists[4][64];
+    __shared__ uint32_t lists[4][64], places[4][MASK == 2 ? 64 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t *list = lists[wave];
     const int64_t block = vec_block(), at = block / column_blocks;
@@ -752,21 +773,22 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
     const AdTile tile = ad_tile(rows, at, lane);
     const int chunks = ONE ? 1 : (m.rank + 31) / 32;
     __shared__ __align__(16) float out[4][16 * AdUp<T, Y, MASK, E>::LD];
-    AdUp<T, Y, MASK, E> up = {base, y, ld_base, ld_y, m.d, mask, {0, 0, 0}, out[wave]};
-    if (MASK) up.key = vec_key(mask);
+    AdUp<T, Y, MASK, E> up = {base, y, ld_base, ld_y, m.d, mask, bits, {0, 0, 0}, out[wave]};
+    if (MASK == 1) up.key = vec_key(mask);
     if (block != at * column_blocks) keep = nullptr;  // (a tile's first block writes it)
     if (keep) ad_zeros(__ballot(tile.in && tile.id == rows.adapters), tile.row, list, m.rank, keep);
     uint64_t todo = __ballot(tile.in);
     while (todo) {
         const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
-        const uint64_t bits = __ballot(tile.in && tile.id == e);
-        todo &= ~bits;
+        const uint64_t same = __ballot(tile.in && tile.id == e);
+        todo &= ~same;
         const bool none = e == rows.adapters;
         if (none && base == y) continue;
-        const int count = ad_list(bits, tile.row, list, lane), tiles = (count + 15) / 16;
+        const int count = ad_list(same, tile.row, list, lane), tiles = (count + 15) / 16;
+        if (MASK == 2) ad_list(same, (uint32_t)(at * rows.tp + lane), places[wave], lane);
         const T *w = none ? nullptr : (const T *)m.p + e * m.stride;
         // what the first tile needs is asked for before the factor is made ready
-        AdUpPass<T, Y, MASK, ONE, E> pass = {up, m, w, list, count, chunks};
+        AdUpPass<T, Y, MASK, ONE, E> pass = {up, m, w, list, places[wave], count, chunks};
         if (first < m.d) pass.request(first);
         if (!none) {
             ad_ready<T>(f, m.rank, chunks, list, count, tiles, ready, keep);
@@ -785,10 +807,10 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
 // factor, columns put together, LDS) costs more than these products: 8192 mixed rows of 500 adapters, 1001 fp16
 // columns at rank 8: 41 us above, 24 here; 16,384 of 1000, 4096 bf16 columns at rank 16: 104 above, 128 here.
 #define AD_FEW_POSITIONS 8
-template <class T, class Y, bool MASK, int E, bool JOIN>
+template <class T, class Y, int MASK, int E, bool JOIN>
 __global__ void __launch_bounds__(256, 2)
 k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t f_stride, int f_slabs, AdMatrix m, const Y *base, int64_t ld_base, Y *y, int64_t ld_y,
-                VecMask mask, int column_blocks, float *__restrict__ keep, int64_t blocks, AdJoins js) {
+                VecMask mask, int column_blocks, float *__restrict__ keep, const uint32_t *__restrict__ bits, int64_t blocks, AdJoins js) {
     if (JOIN && vec_block() >= blocks) return ad_join<T>(rows, js, vec_block() - blocks);
     const int lane = threadIdx.x & 63;
     const int64_t item = vec_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = item / column_blocks;
@@ -796,25 +818,30 @@ k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t 
     const int slab = (int)(item - at * column_blocks), col = slab * 64 * E + E * lane, from = ad_from<E>(col, m.d);
     const AdTile tile = ad_tile(rows, at, lane);
     VecKey key = {0, 0, 0};
-    if (MASK) key = vec_key(mask);
+    if (MASK == 1) key = vec_key(mask);
     uint64_t todo = __ballot(tile.in);
     while (todo) {
         const int e = __builtin_amdgcn_readlane(tile.id, __builtin_ctzll(todo));
-        const uint64_t bits = __ballot(tile.in && tile.id == e);
+        const uint64_t same = __ballot(tile.in && tile.id == e);
         const bool none = e == rows.adapters;
         const T *w = (const T *)m.p + (none ? 0 : e * m.stride) + from;
         // the first four rows of e
-        int row[4], count = 0;
-        uint64_t mine = todo & bits;
+        int row[4], place[4], count = 0;
+        uint64_t mine = todo & same;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             count += mine != 0;
-            row[k] = __builtin_amdgcn_readlane((int)tile.row, mine ? __builtin_ctzll(mine) : __builtin_ctzll(bits));
+            place[k] = mine ? __builtin_ctzll(mine) : __builtin_ctzll(same);
+            row[k] = __builtin_amdgcn_readlane((int)tile.row, place[k]);
             todo &= ~(mine & -mine);
             mine &= mine - 1;
         }
         vec_f<E> acc[4];
         vec_pack<Y, E> b[4];
+        uint32_t kept[4];
+        if (MASK == 2)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) kept[k] = ad_bits_of(bits, at * rows.tp + place[k], m.d, from);
         if (base && !(none && base == y))
 #pragma unroll
             for (int k = 0; k < 4; ++k) b[k] = ad_load<Y, E>(base + (uint32_t)row[k] * ld_base, from);
@@ -873,9 +900,9 @@ k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t 
         for (int k = 0; k < 4; ++k) {
             if (k >= count) break;
             if (MASK) {
-                const uint32_t kept = ad_kept<E>(key, mask, (uint32_t)row[k], from);
+                if (MASK == 1) kept[k] = ad_kept<E>(key, mask, (uint32_t)row[k], from);
 #pragma unroll
-                for (int i = 0; i < E; ++i) acc[k][i] = kept >> i & 1 ? acc[k][i] : 0.0f;
+                for (int i = 0; i < E; ++i) acc[k][i] = kept[k] >> i & 1 ? acc[k][i] : 0.0f;
             }
             if (base) acc[k] += vec_wide<Y, E>(b[k]);
             ad_store<Y, E>(y + (uint32_t)row[k] * ld_y, col, m.d, acc[k]);
@@ -1048,7 +1075,7 @@ struct AdSide {
 };
 template <class T, class O, int RK, bool MASK, int E>
 __global__ void __launch_bounds__(256, sizeof(T) == 4 && RK == 4 ? 1 : 2)
-k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_t blocks_b) {
+k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_t blocks_b, uint32_t *__restrict__ bits) {
     constexpr int P = AdWide<T>::parts;
     int64_t block = vec_block();
     const bool masked = block >= blocks_b;
@@ -1097,7 +1124,7 @@ k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_
     clear();
     vec_pack<T, E> raw[8];
     request(raw, 0);
-    const bool whole = __builtin_amdgcn_readfirstlane(c0) + 16 * E <= d;
+    const bool whole = __builtin_amdgcn_readfirstlane(c0) + 16 * E <= d || d % 8 == 0;  // (then neighbours end together)
     int a = 0;  // where the run in hand begins
     for (int s0 = 0; s0 < total; s0 += AD_STAGE) {
         const int m = total - s0 < AD_STAGE ? total - s0 : AD_STAGE;
@@ -1133,7 +1160,10 @@ k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_
             vec_pack<T, E> next[8];
             if (here + 32 < total) request(next, here + 32);
             if (MASK && masked)
-                ad_drop8<T, E>(raw, key, mask, [&](int q) { return at[here + 8 * g + q < total ? here + 8 * g + q : total - 1]; }, from, whole);
+                ad_drop8<T, E>(raw, key, mask, [&](int q) { return at[here + 8 * g + q < total ? here + 8 * g + q : total - 1]; }, from, whole, [&](int half, uint32_t word) {
+                    const int i = here + 8 * g + 4 * half;
+                    if (bits && blockIdx.z == 0 && col < d && i < total) bits[((p0 + i) >> 2) * (d / 8) + (col >> 3)] = word;
+                });
             // the runs that the step holds, or parts of
             const uint32_t mine = keys[here + (lane & 31) < behind ? here + (lane & 31) : behind - 1];
             const uint64_t heads = __ballot(lane < behind - here && (here + lane == 0 || keys[here + lane > 0 ? here + lane - 1 : 0] != mine)) | 1ull << (behind - here);

@@ -40,7 +40,8 @@ struct AdPlan {
     bool own;                  // its waves take an adapter each
     int len_a, len_b;          // positions of a piece of the sums over rows
     int dpad_a, dpad_b;
-    size_t part, part_a, part_b, total;  // bytes from the workspace's start
+    bool keeps;                // `outer` keeps the mask's bits for `up`
+    size_t part, part_a, part_b, bits, total;  // bytes from the workspace's start
 };
 
 // Positions of a block of `outer`: fewer where there would be few blocks (us, sums and their join, with 128 / 64 / 32 / 16: 10,000 x (1001 + 700) of 200 adapters 40 + 6 / 34 + 7 / 35 + 10; 79 x
@@ -101,6 +102,10 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
         p.dpad_b = (dout + 7) & ~7;
         p.part_a = take((size_t)((n + p.len_a - 1) / p.len_a) * 2 * rank * p.dpad_a * 4);
         p.part_b = take((size_t)((n + p.len_b - 1) / p.len_b) * 2 * rank * p.dpad_b * 4);
+        // (a bit of x each, for the call's duration; where eight columns are no row's end and `outer` has four columns a lane.  `up` with the mask made there again / read, us: 16,384 x 4096 bf16
+        // at rank 16 76 / 68, 16,384 x 2048 at rank 64 65 / 59, 4096 x 1024 of 500 34.7 / 33.4; `outer` takes as long with the stores as without)
+        p.keeps = din % 8 == 0 && dout >= 4;
+        p.bits = take(p.keeps ? (size_t)((n + 3) / 4) * (din / 8) * 4 : 0);
     }
     p.total = at;
     return p;
@@ -202,7 +207,7 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
     rows.tp = plan.tp_up;
     const AdFactor f = {part, plan.rp, n * plan.rp, plan.slabs};
     const AdMatrix m = {b, ld_b, stride_b, rank, dout};
-    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, plan.few, ad_up_blocks(n, plan.tp_up, dout, type), keep, nullptr, s));
+    VEC_TYPED(type, T, AdLaunch<T>::up(rows, f, m, base, ld_base, y, ld_y, y_type == type, none, nullptr, plan.few, ad_up_blocks(n, plan.tp_up, dout, type), keep, nullptr, s));
     QADC_LAUNCH_CHECK("vec_adapter's kernels");
     return PQ_OK;
 }
@@ -236,6 +241,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     const uint32_t *starts = nullptr;
     const AdMatrix ma = {a, ld_a, stride_a, rank, din}, mb = {b, ld_b, stride_b, rank, dout};
     AdFactor u = {};
+    uint32_t *bits = nullptr;
     AdOuter oa = {da, ld_da, stride_da, nullptr, plan.dpad_a, accumulate}, ob = {db, ld_db, stride_db, nullptr, plan.dpad_b, accumulate};
     if (n > 0) {
         plan = ad_plan(n, din, dout, rank, adapters, type, true);
@@ -247,12 +253,13 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
             AD_WORKSPACE("vec_adapter_grad", plan.total);
             float *part = (float *)(ws + plan.part);
             u.p = part;
+            bits = plan.keeps && dx && threshold ? (uint32_t *)(ws + plan.bits) : nullptr;
             oa.part = (float *)(ws + plan.part_a);
             ob.part = (float *)(ws + plan.part_b);
             starts = ad_sort(plan, rows, ws, s);
             const AdSide sb = {{t, rank, 0, 1}, dy, ld_dy, dout, plan.len_b, ad_outer_blocks(dout, din), ob}, sa = {u, x, ld_x, din, plan.len_a, ad_outer_blocks(din, dout), oa};
             VEC_TYPED(type, T, AdLaunch<T>::down(rows, dy, ld_dy, mb, scales, factor, none, part, n * plan.rp, plan.rp, plan.waves, plan.slabs, plan.per, plan.own, nullptr, s);
-                      AdLaunch<T>::outer(rows, rank, mask, sb, sa, narrow, s));
+                      AdLaunch<T>::outer(rows, rank, mask, sb, sa, narrow, bits, s));
         }
         rows.tp = plan.tp_up;
     }
@@ -262,7 +269,7 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     joins.across = (int)((pieces + 255) / 256);
     if (adapters > 0 && joins.across > 8192 / adapters + 1) joins.across = 8192 / adapters + 1;
     if (n > 0 && dx) {
-        VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, adapters > 0 ? mask : none, plan.few, ad_up_blocks(n, plan.tp_up, din, type),
+        VEC_TYPED(type, T, AdLaunch<T>::up(rows, u, ma, dx_base, ld_dx_base, dx, ld_dx, true, adapters > 0 ? mask : none, bits, plan.few, ad_up_blocks(n, plan.tp_up, din, type),
                                            nullptr, adapters > 0 ? &joins : nullptr, s));
     } else if (adapters > 0) {
         VEC_TYPED(type, T, AdLaunch<T>::join(rows, joins, s));

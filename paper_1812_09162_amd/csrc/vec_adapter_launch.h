@@ -12,14 +12,14 @@ struct AdLaunch {
     static void down(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &m, const float *scales, float factor, const VecMask &mask, float *part,
                      int64_t part_stride, int rp, int waves, int slabs, int per, bool own, float *keep, hipStream_t s);
     // narrow: the result is of type T, else float32; joins: of the gradients of the factors in the same launch, or null; a mask or joins only with
-    // a narrow result, a mask only with joins (a gradient of x)
+    // a narrow result, a mask only with joins (a gradient of x); bits: the mask as `outer` kept it (of 8 columns and more), or null
     static void up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                   const VecMask &mask, bool few, int column_blocks, float *keep, const AdJoins *joins, hipStream_t s);
+                   const VecMask &mask, const uint32_t *bits, bool few, int column_blocks, float *keep, const AdJoins *joins, hipStream_t s);
     // both products for single rows, of at most 64 ranks
     static void one(const AdRows &rows, const void *x, int64_t ld_x, const AdMatrix &a, const AdMatrix &b, const float *scales, float factor, const VecMask &mask,
                     const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow, float *keep, hipStream_t s);
     static void join(const AdRows &rows, const AdJoins &joins, hipStream_t s);
-    static void outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, hipStream_t s);
+    static void outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, uint32_t *bits, hipStream_t s);
 };
 
 #ifdef VEC_ADAPTER_SOURCE
@@ -62,7 +62,7 @@ void AdLaunch<T>::join(const AdRows &rows, const AdJoins &joins, hipStream_t s) 
 
 template <class T>
 void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, const void *base, int64_t ld_base, void *y, int64_t ld_y, bool narrow,
-                     const VecMask &mask, bool few, int column_blocks, float *keep, const AdJoins *joins, hipStream_t s) {
+                     const VecMask &mask, const uint32_t *bits, bool few, int column_blocks, float *keep, const AdJoins *joins, hipStream_t s) {
     const int64_t tiles = (rows.n + rows.tp - 1) / rows.tp;
     const AdJoins js = joins ? *joins : AdJoins{};
     const int64_t more = joins ? ad_join_blocks(rows, js) : 0;
@@ -72,17 +72,18 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
         const dim3 grid = vec_grid(blocks + more, 256);
 #define GO(Y, M, E, J)                                                                                                     \
     hipLaunchKernelGGL((k_vec_ad_up_few<T, Y, M, E, J>), grid, dim3(256), 0, s, rows, f.p, f.ld, f.stride, f.slabs, m, (const Y *)base, ld_base, (Y *)y, \
-                       ld_y, mask, cb, keep, blocks, js)
+                       ld_y, mask, cb, keep, bits, blocks, js)
 #define GO2(Y, M, J)                                           \
     do {                                                       \
         if (m.d < AD_COLS(T)) GO(Y, M, 1, J);                  \
         else GO(Y, M, AD_COLS(T), J);                          \
     } while (0)
         if (joins) {
-            if (mask.threshold) GO2(T, true, true);
-            else GO2(T, false, true);
-        } else if (narrow) GO2(T, false, false);
-        else GO2(float, false, false);
+            if (bits) GO(T, 2, AD_COLS(T), true);
+            else if (mask.threshold) GO2(T, 1, true);
+            else GO2(T, 0, true);
+        } else if (narrow) GO2(T, 0, false);
+        else GO2(float, 0, false);
 #undef GO2
 #undef GO
         return;
@@ -96,7 +97,7 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
     const dim3 grid = vec_grid(blocks + more, 256);
     const size_t lds = (size_t)((m.rank + 31) / 32) * ((rows.tp + 15) / 16) * AdWide<T>::parts * 1024;
 #define GO(Y, M, ONE, E, J)                                                                                                \
-    hipLaunchKernelGGL((k_vec_ad_up<T, Y, M, ONE, E, J>), grid, dim3(256), lds, s, rows, f, m, (const Y *)base, ld_base, (Y *)y, ld_y, mask, column_blocks, keep, blocks, js)
+    hipLaunchKernelGGL((k_vec_ad_up<T, Y, M, ONE, E, J>), grid, dim3(256), lds, s, rows, f, m, (const Y *)base, ld_base, (Y *)y, ld_y, mask, column_blocks, keep, bits, blocks, js)
 #define GO2(Y, M, J)                                                                                                       \
     do {                                                                                                                   \
         if (m.d < AD_COLS(T)) GO(Y, M, false, 1, J);                                                                       \
@@ -104,14 +105,16 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
         else GO(Y, M, false, AD_COLS(T), J);                                                                               \
     } while (0)
     if (half) {
-        if (joins) GO(T, false, true, 4, true);
-        else if (narrow) GO(T, false, true, 4, false);
-        else GO(float, false, true, 4, false);
+        if (joins) GO(T, 0, true, 4, true);
+        else if (narrow) GO(T, 0, true, 4, false);
+        else GO(float, 0, true, 4, false);
     } else if (joins) {
-        if (mask.threshold) GO2(T, true, true);
-        else GO2(T, false, true);
-    } else if (narrow) GO2(T, false, false);
-    else GO2(float, false, false);
+        if (bits && m.rank <= 32) GO(T, 2, true, AD_COLS(T), true);
+        else if (bits) GO(T, 2, false, AD_COLS(T), true);
+        else if (mask.threshold) GO2(T, 1, true);
+        else GO2(T, 0, true);
+    } else if (narrow) GO2(T, 0, false);
+    else GO2(float, 0, false);
 #undef GO2
 #undef GO
 }
@@ -138,14 +141,14 @@ void AdLaunch<T>::one(const AdRows &rows, const void *x, int64_t ld_x, const AdM
 }
 
 template <class T>
-void AdLaunch<T>::outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, hipStream_t s) {
+void AdLaunch<T>::outer(const AdRows &rows, int rank, const VecMask &mask, const AdSide &b, const AdSide &a, bool narrow, uint32_t *bits, hipStream_t s) {
     auto blocks = [&](const AdSide &side) { return (rows.n + side.len - 1) / side.len * side.column_blocks; };
     const int64_t blocks_b = blocks(b);
     dim3 grid = vec_grid(blocks_b + blocks(a), 256);
 #define GO(O, RK, M, E)                                                                                                    \
     do {                                                                                                                   \
         grid.z = (unsigned)((rank + 16 * RK - 1) / (16 * RK));                                                             \
-        hipLaunchKernelGGL((k_vec_ad_outer<T, O, RK, M, E>), grid, dim3(256), 0, s, rows, rank, mask, b, a, blocks_b);      \
+        hipLaunchKernelGGL((k_vec_ad_outer<T, O, RK, M, E>), grid, dim3(256), 0, s, rows, rank, mask, b, a, blocks_b, bits);      \
     } while (0)
 #define GO2(O, M)                                                                                                          \
     do {                                                                                                                   \

@@ -1,7 +1,7 @@
 // Random numbers by position: the generator Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3",
 // 2011), whose ten rounds turn a 128-bit counter into four 32-bit words under a 64-bit key.  Counter (j / 8, i, step, layer) gives the
 // sixteen-bit numbers of columns 8 (j / 8) .. + 7 of row i, low halves first: whoever holds eight neighbouring elements, as all kernels on
-// vectors do, makes its part of the mask by one call, in the forward and in the backward pass.  A call is 20 products of 32 bits, which run at a quarter of
+// vectors do, makes its part of the mask by one call, in the forward and again in the backward pass.  A call is 20 products of 32 bits, which run at a quarter of
 // the rate, and about 60 other instructions: for 16,384 x 4096 elements 17 us of a kernel that the vector units bound, less where memory does.
 #pragma once
 #include "vec_device.h"
