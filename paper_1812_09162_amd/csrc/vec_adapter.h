@@ -913,8 +913,8 @@ k_vec_ad_up_few(AdRows rows, const float *__restrict__ f, int64_t ld_f, int64_t 
 // ------------------------------------------------------------ single tokens --
 // Both products in one launch, for rows of their own adapters: a block takes a row and 64 AD_COLS columns of the result, and makes the row's t itself, so
 // that A is read once for each of these (from the L2 cache).  Its eight waves share the columns of x, AD_ONE_TILES KB of A on their way each, then the ranks of B, which is asked
-// for before.  4096 x 4096 bf16 at rank 16, us in a graph by two
-// kernels / by this: 1 row 8.8 / 5.4, 16 9.1 / 5.6, 32 (33 MB of A read) 8.6 / 6.8, 64 (67 MB) 9.9 / 12.5; 16 rows at rank 64 10.7 / 16.5.
+// for before.  4096 x 4096 bf16 at rank 16, us in a graph by two kernels / by this: 1 row 8.8 / 5.4, 16 9.1 / 5.6, 32 (33 MB of A read) 8.6 / 5.9 (7.0 with a row's blocks on all
+// XCDs, each of which then fetches A), 64 (67 MB) 9.7 / 8.5 (12.5); 16 rows at rank 64 10.7 / 10.3.
 #define AD_ONE_TILES 4
 template <class T, class Y, int RK, int E>
 __global__ void __launch_bounds__(512)
@@ -925,9 +925,10 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
     __shared__ ad_u4 tiles[LDS > 32 * E * 4 ? LDS : 32 * E * 4];  // [wave][turn][16 ranks][16 rows][8 pieces]; [wave][64 E] sums
     __shared__ float sums[8][16 * RK], t[16 * RK];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4, lr = lane >> 3, lp = lane & 7;
-    const int64_t block = vec_block(), row = block / column_blocks;
-    if (row >= rows.n) return;
-    const int slab = (int)(block - row * column_blocks), c0 = slab * 64 * E, d = ma.d, rank = ma.rank;
+    // (eight rows in turn, so that the blocks of a row are on one XCD, whose L2 cache reads A once for them)
+    const int block = (int)vec_block(), eight = block / (8 * column_blocks) * 8, r = block - eight * column_blocks, many = rows.n - eight < 8 ? (int)rows.n - eight : 8;
+    if (eight >= rows.n) return;
+    const int slab = r / many, row = eight + r - slab * many, c0 = slab * 64 * E, d = ma.d, rank = ma.rank;
     const int e = __builtin_amdgcn_readfirstlane(ad_id(rows, row));
     const bool none = e == rows.adapters;
     const int own = c0 + (int)threadIdx.x;  // the thread's column of the result

@@ -10,10 +10,11 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 // Rows that are not sorted: each reads its adapter for itself, mostly from the caches.  Sorted / not: 128 x 4096 at rank 16 18.8 / 13.9, 256 x 4096 20.7 / 20.0, 128 x 2048 at rank 64
 // 27 / 13, 256 24 / 19, 512 x 2048 at rank 16 15.9 / 22.1.
 #define AD_FEW_ROWS 256
-// Single rows in one launch: what they read of A altogether, from the L2 cache, and how many they are (of one adapter the other form has whole tiles).  By two kernels /
-// by one: 64 x 4096 at rank 16 (67 MB) 9.9 / 12.5, 512 x 1024 at rank 16 (34 MB) 15.6 / 7.8, 2048 x 256 at rank 8 14.9 / 10.6, 4096 15.5 / 18.9; of one adapter 16 x 4096 9.0 / 5.6,
-// 256 x 1024 8.4 / 5.1.
-#define AD_ONE_BYTES (40 << 20)
+// Single rows in one launch: what they read of A altogether, mostly from the L2 cache, and how many they are (of one adapter the other form has whole tiles).  By two kernels / by one:
+// 64 x 4096 at rank 16 (67 MB) 9.7 / 8.5, 128 (134 MB) 14.5 / 14.5, 128 x 2048 at rank 64 (134 MB) 13.1 / 15, 512 x 1024 at rank 16 (34 MB) 15.6 / 8.0, 1024 (67 MB) 15.9 / 14.0, 2048 (134
+// MB) 18.6 / 29, 2048 x 256 at rank 8 14.9 / 10.6, 4096 15.5 / 18.9; of one adapter 16 x 4096 9.0 / 5.6, 256 x 1024 (17 MB) 8.4 / 5.1, 256 x 2048 (67 MB) 8.4 / 9.7.
+#define AD_ONE_BYTES (72 << 20)
+#define AD_ONE_SAME_BYTES (40 << 20)
 #define AD_ONE_ROWS 2048
 #define AD_ONE_SAME 256
 // `down`: a wave takes an adapter of the tile where adapters have few rows (rows an adapter times columns), unless one wave would have too many columns.  Together / a wave each:
@@ -58,7 +59,7 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     const int64_t each = n / (adapters > 1 ? adapters : 1);
     // (a row's A is read for each of the column blocks)
     p.one = !grad && adapters > 0 && n <= (adapters > 1 ? AD_ONE_ROWS : AD_ONE_SAME) && rank <= 64 &&
-            n * ad_column_blocks(dout, (int)vec_bytes(type)) * rank * din * (int64_t)vec_bytes(type) <= AD_ONE_BYTES;
+            n * ad_column_blocks(dout, (int)vec_bytes(type)) * rank * din * (int64_t)vec_bytes(type) <= (adapters > 1 ? AD_ONE_BYTES : AD_ONE_SAME_BYTES);
     const bool sort = adapters > 1 && n > AD_FEW_ROWS && each > 1;
     p.sorted = grad || sort;
     // as many positions a tile as the adapters have rows on average, at most

@@ -58,7 +58,8 @@ def test_sorted_rows(qb, n, din, dout, r, adapters, kind, p, t, to):
 @pytest.mark.parametrize("n,din,dout,r,adapters,kind,p", [
     (65, 512, 300, 16, 5, "some", 0.0), (256, 130, 72, 64, 1, "some", 0.0), (257, 130, 72, 64, 1, "some", 0.0),         # one launch and two, of one adapter
     (2048, 40, 24, 7, 9, "outside", 0.0), (2049, 40, 24, 7, 9, "outside", 0.0), (1500, 3, 2, 60, 2, "alternate", 0.0),  # of several
-    (640, 1024, 512, 32, 20, "skew", 0.0), (641, 1024, 1026, 32, 20, "skew", 0.0),                                      # 40 MB of A, more
+    (1152, 1024, 512, 32, 20, "skew", 0.0), (1153, 1024, 512, 32, 20, "skew", 0.0), (13, 264, 1600, 20, 9, "some", 0.1), (21, 100, 3100, 16, 5, "outside", 0.0),  # 72 MB of A, more; rows by eight
+    (640, 1024, 512, 32, 20, "skew", 0.0), (641, 1024, 1026, 32, 20, "skew", 0.0),                                      # 40 and 80 MB
     (256, 300, 200, 20, 8, "even", 0.1), (257, 300, 200, 20, 8, "even", 0.1), (256, 1200, 9, 100, 8, "skew", 0.0), (256, 24, 2050, 200, 3, "some", 0.5),  # unsorted, sorted
     (4100, 2050, 2049, 8, 3, "skew", 0.0), (2100, 4100, 40, 33, 20, "even", 0.1)])                                     # few large tiles
 def test_between_forms(qb, n, din, dout, r, adapters, kind, p, t, to):
