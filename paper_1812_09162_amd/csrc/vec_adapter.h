@@ -74,6 +74,20 @@ __device__ __forceinline__ uint32_t ad_high(float hi, float lo) {  // the upper 
 }
 __device__ __forceinline__ float ad_cut(float f) { return __uint_as_float(__float_as_uint(f) & 0xffff0000u); }
 
+// Some of eight values along the contraction: all bits of those, none of the others'.
+template <class T>
+struct AdNamed {
+    ad_u4 m;
+    __device__ __forceinline__ void set(uint32_t bits) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = (bits >> (2 * i) & 1 ? 0xffffu : 0u) | (bits >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
+    }
+};
+template <>
+struct AdNamed<float> {
+    uint32_t m;
+    __device__ __forceinline__ void set(uint32_t bits) { m = bits; }
+};
 // A float32 factor as the matrix cores take it beside values of T.
 template <class T>
 struct AdWide {  // bfloat16, fp16: f = p[0] + p[1] + p[2], each the upper eight bits of what the ones before leave
@@ -89,14 +103,10 @@ struct AdWide {  // bfloat16, fp16: f = p[0] + p[1] + p[2], each the upper eight
                 f[2 * i + 1] -= ad_cut(f[2 * i + 1]);
             }
     }
-    // zeros for those of the eight values whose bit is not set
-    __device__ __forceinline__ void only(uint32_t in) {
+    // zeros for those of the eight values that are not named
+    __device__ __forceinline__ void only(const AdNamed<T> &in) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t m = (in >> (2 * i) & 1 ? 0xffffu : 0u) | (in >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
-#pragma unroll
-            for (int s = 0; s < 3; ++s) p[s][i] &= m;
-        }
+        for (int s = 0; s < 3; ++s) p[s] &= in.m;
     }
 };
 template <>
@@ -107,23 +117,29 @@ struct AdWide<float> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = __float_as_uint(f[i]);
     }
-    __device__ __forceinline__ void only(uint32_t in) {
+    __device__ __forceinline__ void only(const AdNamed<float> &in) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = in >> i & 1 ? p[i >> 2][i & 3] : 0u;
+        for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = in.m >> i & 1 ? p[i >> 2][i & 3] : 0u;
     }
 };
 // Eight values of T (along the contraction) for it: fp16 as two bfloat16 numbers.
 template <class T>
 struct AdNarrow {
     ad_u4 p[1];
+    __device__ __forceinline__ void only(const AdNamed<T> &in) { p[0] &= in.m; }
 };
 template <>
 struct AdNarrow<_Float16> {
     ad_u4 p[2];
+    __device__ __forceinline__ void only(const AdNamed<_Float16> &in) { p[0] &= in.m, p[1] &= in.m; }
 };
 template <>
 struct AdNarrow<float> {
     float p[8];
+    __device__ __forceinline__ void only(const AdNamed<float> &in) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = in.m >> i & 1 ? p[i] : 0.0f;
+    }
 };
 // Rows raw[0..7], E columns each: column m.
 template <class T, int E>
@@ -1057,7 +1073,8 @@ k_vec_ad_one(AdRows rows, const T *__restrict__ x, int64_t ld_x, AdMatrix ma, Ad
 // G_e[j][col] = sum over the rows of e of f_row[j] (kept) x_row[col].  A block takes `len` sorted positions and 256 columns, a quarter a wave, in steps of 32
 // positions whatever runs of equal ids these hold: the rows of a step are read once, and each run among them takes its own and zeros for the others.  Runs that lie within the block's positions are written; the others' sums go to part[chunk][0] (began before)
 // or part[chunk][1], which the join adds up in order.  Per step a lane reads eight rows of four columns.  Bound by the vector units, which put columns together and make the mask:
-// 16,384 x (4096 + 4096) bf16 at rank 16 with dropout 81 us (288 MB read, 66% of the cycles with a vector instruction), 10,000 x (1001 + 700) fp16 of 200 adapters 34, 1024 x (256 + 96) float32 8.
+// 16,384 x (4096 + 4096) bf16 at rank 16 with dropout 81 us (288 MB read, 66% of the cycles with a vector instruction), 10,000 x (1001 + 700) fp16 of 200
+// adapters 27 (34 with columns put together for each run of a step, not once), 1024 x (256 + 96) float32 8.
 #define AD_STAGE 128  // positions whose factors are made ready at once
 template <class O, int E>
 __device__ __forceinline__ void ad_put(O *row, int col, int d, vec_f<E> v, bool accumulate) {
@@ -1168,35 +1185,43 @@ k_vec_ad_outer(AdRows rows, int rank, VecMask mask, AdSide sb, AdSide sa, int64_
             // the runs that the step holds, or parts of
             const uint32_t mine = keys[here + (lane & 31) < behind ? here + (lane & 31) : behind - 1];
             const uint64_t heads = __ballot(lane < behind - here && (here + lane == 0 || keys[here + lane > 0 ? here + lane - 1 : 0] != mine)) | 1ull << (behind - here);
+            AdNarrow<T> v[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = ad_column<T, E>(raw, i);
             for (int lo = here; lo < behind;) {
                 const int hi = here + __builtin_ctzll(heads >> (lo - here + 1)) + (lo - here + 1);
-                const bool alone = lo == here && hi == behind;  // all of the step's rows are of this run
-                uint32_t in = 0xff;
-                AdNarrow<T> v[E];
-                if (alone) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) v[i] = ad_column<T, E>(raw, i);
-                } else {  // others' rows take no part, whatever they hold
-                    vec_pack<T, E> its[8];
-                    in = 0;
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const bool has = here + 8 * g + q >= lo && here + 8 * g + q < hi;
-                        in |= (has ? 1u : 0u) << q;
-                        its[q] = has ? raw[q] : (vec_pack<T, E>)(T)0.0f;
-                    }
-#pragma unroll
-                    for (int i = 0; i < E; ++i) v[i] = ad_column<T, E>(its, i);
-                }
-#pragma unroll
-                for (int j = 0; j < RK; ++j) {
+                auto factor = [&](int j) {
                     AdWide<T> w;
 #pragma unroll
                     for (int s = 0; s < P; ++s) w.p[s] = ready[((st * RK + j) * P + s) * 64 + lane];
-                    if (!alone) w.only(in);
+                    return w;
+                };
+                if (lo == here && hi == behind) {  // all of the step's rows are of this run
 #pragma unroll
-                    for (int i = 0; i < E; ++i) acc[j][i] = ad_mul<T, true>(v[i], w, acc[j][i]);
-                    __builtin_amdgcn_sched_barrier(0);  // (all ranks' factors at once are registers that the rows on their way need)
+                    for (int j = 0; j < RK; ++j) {
+                        const AdWide<T> w = factor(j);
+#pragma unroll
+                        for (int i = 0; i < E; ++i) acc[j][i] = ad_mul<T, true>(v[i], w, acc[j][i]);
+                        __builtin_amdgcn_sched_barrier(0);  // (all ranks' factors at once are registers that the rows on their way need)
+                    }
+                } else {  // others' rows take no part, whatever they hold
+                    uint32_t in = 0;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) in |= (here + 8 * g + q >= lo && here + 8 * g + q < hi ? 1u : 0u) << q;
+                    AdNamed<T> its;
+                    its.set(in);
+#pragma unroll
+                    for (int j = 0; j < RK; ++j) {
+                        AdWide<T> w = factor(j);
+                        w.only(its);
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            AdNarrow<T> o = v[i];
+                            o.only(its);
+                            acc[j][i] = ad_mul<T, true>(o, w, acc[j][i]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
                 const uint32_t e = keys[lo];
                 const bool goes_on = hi < total ? keys[hi] == e : behind_key == e;
