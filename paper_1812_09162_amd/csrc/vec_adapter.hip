@@ -22,7 +22,7 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 #define AD_OWN 32768
 #define AD_OWN_COLUMNS 2048
 // `up`: rows an adapter times ranks below which it runs on the vector units.  Matrix cores / vector units: 8192 of 500 at rank 8, 1001 fp16 columns, 45 / 41;
-// 16,384 of 1000 at rank 16, 4096 columns, 193 / 243; 16,384 of 500 at rank 32, 1024 columns, 57 / 102.
+// 16,384 of 1000 at rank 16, 4096 columns, 193 / 243 (tiles of 16); 16,384 of 500 at rank 32, 1024 columns, 57 / 102.
 #define AD_UP_FEW 256
 // Tiles of 32 and 64 positions only if so many are left: of short rows more, since a tile is little work.  At least 256 / 64 tiles: 4096 x 1024 of 8 at rank 16 19.3 / 22.0,
 // 4096 x 4096 38 / 33, 8192 x 4096 52 / 50, 8192 x 2048 34.5 / 33.3, 2048 x 4096 float32 42 / 38.
@@ -62,9 +62,10 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
             n * ad_column_blocks(dout, (int)vec_bytes(type)) * rank * din * (int64_t)vec_bytes(type) <= (adapters > 1 ? AD_ONE_BYTES : AD_ONE_SAME_BYTES);
     const bool sort = adapters > 1 && n > AD_FEW_ROWS && each > 1;
     p.sorted = grad || sort;
-    // as many positions a tile as the adapters have rows on average, at most
+    // as many positions a tile as two adapters have rows on average, at most (one adapter / two / four: 16,384 x 2048 of 300 at rank 16 65 / 61 / 61, 16,384 x 4096 of 1000 193 / 179 / 173,
+    // 8192 x 4096 of 400 at rank 32 120 / 106 / 113, 20,000 x 1024 of 400 55 / 55 / 55)
     p.tp = rank <= 32 && din >= 8 && dout >= 8 ? 64 : 32;  // (of k_vec_ad_up's other form at most 32)
-    while (p.tp > 16 && (p.tp > each || n / p.tp < AD_TILES(din, dout))) p.tp /= 2;
+    while (p.tp > 16 && (p.tp > 2 * each || n / p.tp < AD_TILES(din, dout))) p.tp /= 2;
     p.tp_up = p.tp;
     p.few = p.sorted && each * rank < AD_UP_FEW;
     // tiles of up to eight, fewer where there would be too few waves (with 1024 / 2048 / 4096 waves at least: 4096 rows of 500 at rank 8, 1001 fp16 columns, 41 / 37 / 40; 4096 of
