@@ -54,6 +54,8 @@ extern "C" int vec_dropout(const void *x, int64_t ld_x, const void *residual, in
     VEC_REQUIRE(threshold == 0 || (state && ((uintptr_t)state & 7u) == 0), "vec_dropout: state null or misaligned");
     if (n == 0) return PQ_OK;
     VEC_REQUIRE(x && y, "vec_dropout: null pointer");
+    // (a row of y would lie over others that are still to be read)
+    VEC_REQUIRE(n <= 1 || ((x != y || ld_x == ld_y) && (residual != y || ld_residual == ld_y)), "vec_dropout: y in place of x or residual with another distance of rows");
     VEC_REQUIRE(vec_aligned(x, type) && vec_aligned(residual, type) && vec_aligned(y, type), "vec_dropout: misaligned pointer");
     const int pieces = (int)((d + 7) / 8), rpb = pieces >= 1024 ? 1 : 1024 / pieces, parts = (pieces + 1023) / 1024;
     const int64_t blocks = parts > 1 ? n * parts : (n + rpb - 1) / rpb;

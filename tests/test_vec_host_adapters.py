@@ -77,3 +77,10 @@ def test_binding_refuses_host_tensors():
         with pytest.raises(qb.QadcError) as e:
             call()
         assert e.value.code == qb.PQ_EINVAL and "GPU" in str(e.value)
+
+
+@pytest.mark.parametrize("kw", [dict(x=P, y=P, r=2 * P, ldy=72), dict(x=P, y=P, r=2 * P, ldx=72), dict(x=2 * P, y=P, r=P, ldy=72), dict(x=2 * P, y=P, r=P, ldr=72),
+                                dict(x=P, y=P, r=None, ldy=72), dict(x=P, y=P, r=P, ldr=72)])
+def test_dropout_in_place_with_other_distances(kw):
+    """A row of y would lie over rows of x or of the residual that are still to be read."""
+    refused(dropout(**kw), "in place")
