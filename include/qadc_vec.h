@@ -136,7 +136,7 @@ int vec_dropout(const void *x, int64_t ld_x, const void *residual, int64_t ld_re
  *   x      [dev][n][din], a [dev][adapters][rank][din], b [dev][adapters][rank][dout], all of `type` F32, BF16 or F16; stride_a and stride_b: the
  *          distance of two adapters in elements, 0 or more
  *   scales [dev][adapters] float32, or NULL (1)           ids [dev][n], int32 or int64, in any order
- *   base   [dev][n][dout] or NULL (0), y [dev][n][dout], of y_type: `type` or F32; y may be base (same pointer and ld)
+ *   base   [dev][n][dout] or NULL (0), y [dev][n][dout], of y_type: `type` or F32; y may be base (same pointer and ld), not x
  *   t      [dev][n][rank] float32 without padding, what the gradient reads, or NULL
  * Products are of the values of `type` with float32 sums; t is not rounded to fewer bits.  An infinity among x, a, b or t gives an infinity or NaN in
  * the results that it enters.

@@ -833,7 +833,7 @@ def vec_adapter(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Te
                 dtype: Optional[torch.dtype] = None, want_t: bool = False, out=None, workspace: Optional[torch.Tensor] = None, stream=None):
     """Low-rank adapters of many requests: y = base + t b[e] with t = scales[e] * dropout(x) a[e]^T and e the row's id, y = base where
     that is outside.  a [adapters, rank, din], b [adapters, rank, dout]; p, state and layer as in vec_dropout.  Returns (y, t), t (float32,
-    for the gradient) where wanted, else None.  `out`: the same two, to be written (y may be base; its type x's or float32)."""
+    for the gradient) where wanted, else None.  `out`: the same two, to be written (y may be base, not x; its type x's or float32)."""
     call = _Call("vec_adapter", x, stream)
     n, din, dout, rank, count, tx, xp, ldx, args = _adapters(call, x, a, b, ids, scales)
     p, statep, layer = call.mask(p, state, layer)

@@ -181,6 +181,8 @@ extern "C" int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t l
     VEC_REQUIRE(base != y || !base || ld_base == ld_y, "vec_adapter: y in place of base with other distances of rows");
     if (n == 0) return PQ_OK;
     VEC_REQUIRE(x && y && ids && (adapters == 0 || (a && b)), "vec_adapter: null pointer");
+    // (a row's blocks of k_vec_ad_one read all of x's row, while others already write theirs of y)
+    VEC_REQUIRE(x != y, "vec_adapter: y in place of x");
     VEC_REQUIRE(vec_aligned(x, type) && vec_aligned(a, type) && vec_aligned(b, type) && vec_aligned(base, y_type) && vec_aligned(y, y_type) &&
                     vec_aligned(scales, VEC_F32) && vec_aligned(t, VEC_F32) && ((uintptr_t)ids & (uintptr_t)(id_bytes - 1)) == 0,
                 "vec_adapter: misaligned pointer");

@@ -84,3 +84,9 @@ def test_binding_refuses_host_tensors():
 def test_dropout_in_place_with_other_distances(kw):
     """A row of y would lie over rows of x or of the residual that are still to be read."""
     refused(dropout(**kw), "in place")
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n=1), dict(base=None), dict(ldy=64), dict(dout=64, ldb=64, stb=512, ldbase=64, ldy=64)])
+def test_adapter_in_place_of_its_input(kw):
+    """Single rows in one launch read x in several blocks, each of which writes a part of y."""
+    refused(adapter(**dict(dict(x=2 * P, y=2 * P), **kw)), "in place of x")
