@@ -90,3 +90,10 @@ def test_dropout_in_place_with_other_distances(kw):
 def test_adapter_in_place_of_its_input(kw):
     """Single rows in one launch read x in several blocks, each of which writes a part of y."""
     refused(adapter(**dict(dict(x=2 * P, y=2 * P), **kw)), "in place of x")
+
+
+def test_pieces_of_the_long_sums_are_those_that_their_tests_mean():
+    from test_gpu_vec_adapter_long import PIECES, pieces, sizes
+    for case, lengths in PIECES:
+        assert pieces(qb.vec_adapter_grad_workspace_bytes(*sizes(case), case[4]), *sizes(case)) == {lengths}, case
+    assert {k for _, lengths in PIECES for k in lengths} >= {32, 256, 512, 1024}
