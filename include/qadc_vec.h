@@ -156,7 +156,8 @@ int vec_adapter(const void *x, int64_t ld_x, const void *a, int64_t ld_a, int64_
  *   da[e] = sum over the rows of e of u[i]^T x'[i]        db[e] = sum over the rows of e of t[i]^T dy[i]
  * da and db of all adapters are written, those without a row with zeros; accumulate: the sums are added to them, and adapters without a row left alone.
  *   dy [dev][n][dout], x, dx_base and dx [dev][n][din] of `type`; dx may be NULL (then dx_base too), dx_base NULL (0) or dx itself (same pointer and ld)
- *   da [dev][adapters][rank][din], db [dev][adapters][rank][dout], of grad_type: `type` or F32; the adapters' must not overlap
+ *   da [dev][adapters][rank][din], db [dev][adapters][rank][dout], of grad_type: `type` or F32; an adapter's rows lie together,
+ *      before the next one's: stride_da >= (rank - 1) ld_da + din, stride_db likewise
  * p, state and layer as in the forward call, with the same state's contents.
  */
 size_t vec_adapter_grad_workspace_bytes(int64_t n, int din, int dout, int rank, int adapters, int type);

@@ -185,7 +185,7 @@ __device__ __forceinline__ vec_f4 ad_mul(const AdNarrow<T> &n, const AdWide<T> &
         auto one = [&](ad_u4 a, ad_u4 b) {
             c = WIDE_FIRST ? ad_mma(__builtin_bit_cast(ad_b8, b), __builtin_bit_cast(ad_b8, a), c) : ad_mma(__builtin_bit_cast(ad_b8, a), __builtin_bit_cast(ad_b8, b), c);
         };
-        if constexpr (__is_same(T, _Float16)) {  // (smallest first; the product of the last parts is below float32's last bit)
+        if constexpr (__is_same(T, _Float16)) {  // (smallest first; the product of the last parts, left out, is below 2^-22 of the whole)
             one(n.p[1], w.p[1]);
             one(n.p[0], w.p[2]);
             one(n.p[1], w.p[0]);
@@ -305,8 +305,9 @@ __device__ __forceinline__ int ad_list(uint64_t bits, uint32_t row, uint32_t *li
 //
 // Eight neighbouring lanes read 128 bytes of a row, sixteen bytes each, and pass them through LDS to the lanes that the matrix cores want them in (rows of 128 bytes whose
 // sixteen-byte pieces are exchanged by the row's number, so that neither side meets bank conflicts); read directly in that order, neighbouring lanes
-// would hold different rows, and the L1 cache take four times the accesses: 16,384 x 4096 bf16 at rank 16 44 us, 40 this way (134 MB, the rate of
-// a cold read); 4096 x 2048 at rank 64 24 and 15.  Neighbouring blocks begin at different columns: rows are
+// would hold different rows, and the L1 cache take four times the accesses: 16,384 x 4096 bf16 at rank 16 44 us, 40 this way (134 MB, 3.4 TB/s);
+// 4096 x 2048 at rank 64 24 and 15.  Bound by waits, not by memory's rate: at 16,384 x 4096 waves wait 57% of their time, vector instructions take 5% of the cycles and the matrix
+// cores 3%, with one block a CU (84 KB of LDS each), two waves a SIMD; above 64 ranks 300 registers leave one.  Neighbouring blocks begin at different columns: rows are
 // often a multiple of 4 KB apart, and blocks that read the same columns at the same time would ask few of the memory's channels.
 #define AD_DOWN_WAVES 8
 // (rows without an adapter)
@@ -821,7 +822,7 @@ k_vec_ad_up(AdRows rows, AdFactor f, AdMatrix m, const Y *base, int64_t ld_base,
 // The same for few rows of an adapter: on the vector units, without a wait between waves.  A wave takes a tile of at most eight positions and 64 E columns, E a lane;
 // four rows of one adapter share what it reads of W.  Where a tile of the matrix cores would hold three rows of sixteen, the rest of the form above (the parts of the
 // factor, columns put together, LDS) costs more than these products: 8192 mixed rows of 500 adapters, 1001 fp16
-// columns at rank 8: 41 us above, 24 here; 16,384 of 1000, 4096 bf16 columns at rank 16: 104 above, 128 here.
+// columns at rank 8: 26 us above, 21 here; 16,384 of 1000, 4096 bf16 columns at rank 16: 91 above, 151 here.
 #define AD_FEW_POSITIONS 8
 template <class T, class Y, int MASK, int E, bool JOIN>
 __global__ void __launch_bounds__(256, 2)

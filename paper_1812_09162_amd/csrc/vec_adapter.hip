@@ -7,27 +7,30 @@ void qadc_vec_sort(const void *ids, int id_bytes, int64_t n, int64_t rows, char 
 
 // The rules between the forms.  Times of whole calls in a graph, us, bfloat16 unless said.
 //
-// Rows that are not sorted: each reads its adapter for itself, mostly from the caches.  Sorted / not: 128 x 4096 at rank 16 18.8 / 13.9, 256 x 4096 20.7 / 20.0, 128 x 2048 at rank 64
-// 27 / 13, 256 24 / 19, 512 x 2048 at rank 16 15.9 / 22.1.
+// Rows that are not sorted: each reads its adapter for itself, mostly from the caches.  Of 16 adapters, sorted / not: 128 x 4096 at rank 16 18.7 / 13.4, 256 x 4096 20.6 / 19.5, 300 x 4096
+// 20.0 / 29.2, 128 x 2048 at rank 64 29.7 / 13.0, 256 24.3 / 18.8, 512 x 2048 at rank 16 15.8 / 21.9.  Of less than two rows an adapter none are sorted, which up to about 1000 rows is
+// the faster side and beyond the slower one: 300 x 4096 of 300 at rank 16 44 / 32, 600 x 2048 of 500 at rank 32 39 / 40, 1000 x 4096 of 1000 at rank 16 72 / 69, 1999 x 4096 of 1000
+// 104 / 124, 4000 x 2048 of 3000 98 / 147, 8000 x 512 of 7000 65 / 89.
 #define AD_FEW_ROWS 256
 // Single rows in one launch: what they read of A altogether, mostly from the L2 cache, and how many they are (of one adapter the other form has whole tiles).  By two kernels / by one:
-// 64 x 4096 at rank 16 (67 MB) 9.7 / 8.5, 128 (134 MB) 14.5 / 14.5, 128 x 2048 at rank 64 (134 MB) 13.1 / 15, 512 x 1024 at rank 16 (34 MB) 15.6 / 8.0, 1024 (67 MB) 15.9 / 14.0, 2048 (134
-// MB) 18.6 / 29, 2048 x 256 at rank 8 14.9 / 10.6, 4096 15.5 / 18.9; of one adapter 16 x 4096 9.0 / 5.6, 256 x 1024 (17 MB) 8.4 / 5.1, 256 x 2048 (67 MB) 8.4 / 9.7.
+// 64 x 4096 at rank 16 (67 MB) 9.7 / 8.3, 128 (134 MB) 13.5 / 13.4, 128 x 2048 at rank 64 (134 MB) 12.8 / 14.4, 512 x 1024 at rank 16 (34 MB) 15.4 / 8.3, 1024 (67 MB) 16.0 / 14.0, 2048 (134
+// MB) 17.0 / 25.4, 2048 x 256 at rank 8 14.8 / 11.4, 4096 15.5 / 20.3; of one adapter 16 x 4096 8.9 / 5.6, 256 x 1024 (17 MB) 8.3 / 5.3, 256 x 2048 (67 MB) 8.4 / 9.5.
 #define AD_ONE_BYTES (72 << 20)
 #define AD_ONE_SAME_BYTES (40 << 20)
 #define AD_ONE_ROWS 2048
 #define AD_ONE_SAME 256
 // `down`: a wave takes an adapter of the tile where adapters have few rows (rows an adapter times columns), unless one wave would have too many columns.  Together / a wave each:
-// 4096 rows of 1000 adapters at rank 16, 512 columns 41 / 36, 2048 69 / 65, 4096 125 / 138; 16,384 of 2000, 1024 columns 81 / 69; 16,384 of 1000, 2048 columns 110 / 113.
+// 4096 rows of 1000 adapters at rank 16, 512 columns 36.5 / 28.9, 2048 69 / 58; 16,384 of 2000 at rank 8, 1024 columns, 81 / 66; beyond the rule, where it would still be faster, 4096
+// columns 124 / 112 and 16,384 of 1000, 2048 columns, 99 / 91.
 #define AD_OWN 32768
 #define AD_OWN_COLUMNS 2048
-// `up`: rows an adapter times ranks below which it runs on the vector units.  Matrix cores / vector units: 8192 of 500 at rank 8, 1001 fp16 columns, 45 / 41;
-// 16,384 of 1000 at rank 16, 4096 columns, 193 / 243 (tiles of 16); 16,384 of 500 at rank 32, 1024 columns, 57 / 102.
+// `up`: rows an adapter times ranks below which it runs on the vector units.  Matrix cores / vector units: 8192 of 500 at rank 8, 1001 fp16 columns, 43 / 37;
+// 4096 of 1000 at rank 16, 512 columns, 36 / 29, 4096 columns 128 / 122; 16,384 of 1000, 4096 columns, 179 / 236; 16,384 of 500 at rank 32, 1024 columns, 51 / 97.
 #define AD_UP_FEW 256
-// Tiles of 32 and 64 positions only if so many are left: of short rows more, since a tile is little work.  At least 256 / 64 tiles: 4096 x 1024 of 8 at rank 16 19.3 / 22.0,
-// 4096 x 4096 38 / 33, 8192 x 4096 52 / 50, 8192 x 2048 34.5 / 33.3, 2048 x 4096 float32 42 / 38.
+// Tiles of 32 and 64 positions only if so many are left: of short rows more, since a tile is little work.  At least 256 / 64 tiles: 4096 x 1024 of 8 at rank 16 19.0 / 22.0,
+// 4096 x 4096 38 / 32, 8192 x 4096 53 / 50, 8192 x 2048 34.3 / 33.2, 2048 x 4096 float32 42 / 38.
 #define AD_TILES(din, dout) ((din) + (dout) < 4096 ? 256 : 64)
-// Slabs of `down` where there are fewer waves than this (with 512 / 1024 / 2048 / 4096: 1024 x 4096 at rank 16 22.6 / 20.5 / 19.2 / -; 512 x 4096 - / 16.6 / 17.9 / 17.9; 8192 x 2048 - / 34.5 / 34.5 / 37.2).
+// Slabs of `down` where there are fewer waves than this (with 512 / 1024 / 2048 / 4096: 1024 x 4096 of 8 at rank 16 22.2 / 20.7 / 19.2 / 23.2; 512 x 4096 17.8 / 16.9 / 18.3 / 18.3; 8192 x 2048 33.1 / 33.3 / 33.4 / 36.0).
 #define AD_WAVES 1024
 #define AD_MAX_SLABS 16
 
@@ -45,8 +48,8 @@ struct AdPlan {
     size_t part, part_a, part_b, bits, total;  // bytes from the workspace's start
 };
 
-// Positions of a block of `outer`: fewer where there would be few blocks (us, sums and their join, with 128 / 64 / 32 / 16: 10,000 x (1001 + 700) of 200 adapters 40 + 6 / 34 + 7 / 35 + 10; 79 x
-// (84 + 6403) of 38 64: 22 + 4 / 32: 19 + 4 / 16: 17 + 4; 2000 x (1024 + 1024) of 8 - / 10 + 4 / 10 + 5 / 15 + 7).
+// Positions of a block of `outer`: fewer where there would be few blocks (us, whole gradients, with 128 / 64 / 32 / 16: 10,000 x (1001 + 700) fp16 of 200 adapters at rank 12
+// 61 / 63 / 66 / 80; 79 x (84 + 6403) of 38 at rank 8 69 / 60 / 47 / 44; 2000 x (1024 + 1024) of 8 at rank 16 27 / 26 / 27 / 33).
 static int ad_len(int64_t n, int64_t each, int d, int other, int rank) {
     const int64_t across = (int64_t)ad_outer_blocks(d, other) * ((rank + 63) / 64);
     int len = AD_MAX_LEN;
@@ -63,13 +66,14 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     const bool sort = adapters > 1 && n > AD_FEW_ROWS && each > 1;
     p.sorted = grad || sort;
     // as many positions a tile as two adapters have rows on average, at most (one adapter / two / four: 16,384 x 2048 of 300 at rank 16 65 / 61 / 61, 16,384 x 4096 of 1000 193 / 179 / 173,
-    // 8192 x 4096 of 400 at rank 32 120 / 106 / 113, 20,000 x 1024 of 400 55 / 55 / 55)
+    // 8192 x 4096 of 400 at rank 32 121 / 105 / 113, 20,000 x 1024 of 400 54 / 54 / 54).  The average is over the adapters that are there, whether the call names them or not: 16,384 x 4096
+    // in sixteen runs, of 64 / of 1000 adapters, at rank 16 97 / 108, at rank 8, where `few` holds for the 1000, 96 / 142.
     p.tp = rank <= 32 && din >= 8 && dout >= 8 ? 64 : 32;  // (of k_vec_ad_up's other form at most 32)
     while (p.tp > 16 && (p.tp > 2 * each || n / p.tp < AD_TILES(din, dout))) p.tp /= 2;
     p.tp_up = p.tp;
     p.few = p.sorted && each * rank < AD_UP_FEW;
-    // tiles of up to eight, fewer where there would be too few waves (with 1024 / 2048 / 4096 waves at least: 4096 rows of 500 at rank 8, 1001 fp16 columns, 41 / 37 / 40; 4096 of
-    // 1000 at rank 16, 512 columns, 36 / 31 / 32; 8192 of 500 at rank 8, 512 columns, 28 / 25 / 28)
+    // tiles of up to eight, fewer where there would be too few waves (with 1024 / 2048 / 4096 waves at least: 4096 rows of 500 at rank 8, 1001 fp16 columns, 34 / 31 / 33; 4096 of
+    // 1000 at rank 16, 512 columns, 33 / 29 / 29; 8192 of 500 at rank 8, 512 columns, 27 / 24 / 28)
     if (p.few) {
         const int64_t across = ad_column_blocks(grad ? din : dout, (int)vec_bytes(type));
         p.tp_up = AD_FEW_POSITIONS;
@@ -82,8 +86,8 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
     const int64_t tiles = (n + p.tp - 1) / p.tp;
     p.waves = d >= 1024 && rank <= 64 ? 8 : 4;
     p.own = p.sorted && d <= AD_OWN_COLUMNS && each * d < AD_OWN;
-    // A wave of a slab has at least two turns of 64 columns.  Of waves with an adapter each about two have one (one slab / so: 4096 rows of 500 at rank 8, 1001 fp16 columns, 41 / 37; 4096
-    // of 1000 at rank 16, 512 columns, 36 / 33; slabs at 8192 rows of 500, 512 columns, too 28 / 29).
+    // A wave of a slab has at least two turns of 64 columns.  Of waves with an adapter each about two have one (one slab / so: 4096 rows of 500 at rank 8, 1001 fp16 columns, 35 / 31; 4096
+    // of 1000 at rank 16, 512 columns, 31.5 / 28.7; 8192 of 500, 512 columns, 25.1 / 24.2).
     const int64_t active = tiles * (p.own ? 2 : p.waves);
     int64_t slabs = active >= AD_WAVES ? 1 : AD_WAVES / active;
     const int64_t most = d / (p.own ? 128 : p.waves * 64);
@@ -104,8 +108,8 @@ static AdPlan ad_plan(int64_t n, int din, int dout, int rank, int adapters, int 
         p.dpad_b = (dout + 7) & ~7;
         p.part_a = take((size_t)((n + p.len_a - 1) / p.len_a) * 2 * rank * p.dpad_a * 4);
         p.part_b = take((size_t)((n + p.len_b - 1) / p.len_b) * 2 * rank * p.dpad_b * 4);
-        // (a bit of x each, for the call's duration; where eight columns are no row's end and `outer` has four columns a lane.  `up` with the mask made there again / read, us: 16,384 x 4096 bf16
-        // at rank 16 76 / 68, 16,384 x 2048 at rank 64 65 / 59, 4096 x 1024 of 500 34.7 / 33.4; `outer` takes as long with the stores as without)
+        // (a bit of x each, for the call's duration; where eight columns are no row's end and `outer` has four columns a lane.  Whole gradients with the mask made again in `up` / read, us: 16,384 x 4096 bf16
+        // of 8 at rank 16 184 / 181, 16,384 x 2048 at rank 64 153 / 147, 4096 x 1024 of 500 73 / 72)
         p.keeps = din % 8 == 0 && dout >= 4;
         p.bits = take(p.keeps ? (size_t)((n + 3) / 4) * (din / 8) * 4 : 0);
     }
@@ -269,7 +273,8 @@ extern "C" int vec_adapter_grad(const void *dy, int64_t ld_dy, const void *x, in
     }
     AdJoins joins = {{oa, plan.len_a, din}, {ob, plan.len_b, dout}, starts, rank, narrow, 1};
     const int64_t pieces = (int64_t)rank * ((plan.dpad_a > plan.dpad_b ? plan.dpad_a : plan.dpad_b) / 8);
-    // about 16,384 blocks at most: of 1000 adapters most have nothing to join (4096 rows of 1000, 1001 and 700 columns at rank 12: 33 us with a block for each 2048 values, 22 so)
+    // 2 (8192 + adapters) blocks at most: of many adapters most have nothing to join (whole gradients with a block for each 2048 values of each / so, us: 4096 rows of 1000, 4096 columns at
+    // rank 16 315 / 286, 16,384 of 4000, 512 columns at rank 64 577 / 466)
     joins.across = (int)((pieces + 255) / 256);
     if (adapters > 0 && joins.across > 8192 / adapters + 1) joins.across = 8192 / adapters + 1;
     if (n > 0 && dx) {

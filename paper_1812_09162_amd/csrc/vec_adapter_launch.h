@@ -88,9 +88,8 @@ void AdLaunch<T>::up(const AdRows &rows, const AdFactor &f, const AdMatrix &m, c
 #undef GO
         return;
     }
-    // Eight bytes a lane where sixteen leave few blocks: half the registers and twice the waves.  us with sixteen / eight: 16,384 x 2048 at rank 32 (1024 blocks) 36 / 29, 10,000 x
-    // 1001 at rank 12 (1252) 32 / 25; 16,384 x 4096 at rank 16 (2048) 53 / 53, of 1000 adapters (8192) 104 / 131; single rows of 4096 5.4 / 5.9.  With a mask each of two
-    // neighbouring lanes would make it: 70 / 91.
+    // Eight bytes a lane where sixteen leave few blocks: half the registers and twice the waves.  Whole calls, us, with sixteen / eight: 16,384 x 2048 of one at rank 32 (1024 blocks) 44.6 / 39.6,
+    // 10,000 x 1001 fp16 of 200 at rank 12 (1252) 45 / 42; 16,384 x 4096 at rank 16 (2048) 96.5 / 97.4, of 1000 adapters (4096) 179 / 189.  With a mask each of two neighbouring lanes would make it.
     const bool half = sizeof(T) == 2 && m.rank <= 32 && !mask.threshold && m.d >= AD_COLS(T) && rows.tp >= 16 && tiles * ad_column_blocks(m.d, 2) < 2048;
     if (half) column_blocks = ad_blocks(m.d, 4);
     const int64_t blocks = tiles * column_blocks;

@@ -2,7 +2,7 @@
 //
 // y = residual + (kept ? factor x : 0); the mask is made where it is used and never stored, so the gradient is the same call on dy.
 // A block takes 1024 pieces of eight elements (whole rows, or part of one), four of them in flight per thread; bound by memory:
-// 16,384 x 2048 bf16 with a residual 35 us (201 MB, 5.7 TB/s, part of it from the caches); 10,000 x 1001 fp16 9.6, 1024 x 256 float32 4.6 (one round trip and a launch).
+// 16,384 x 2048 bf16 with a residual 35 us (201 MB, 5.7 TB/s, part of it from the caches); 10,000 x 1001 fp16 11, 1024 x 256 float32 4.6 (one round trip and a launch).
 #include "vec_random.h"
 
 template <class T, bool RESIDUAL>
